@@ -2,6 +2,8 @@
 
 Modules:
   kvckpt     Python binding of the HIP library (include/lumen_kv_ckpt.h)
+  attn       slot maps, 4-bit paged cache, decode and prompt attention
+             (include/lumen_attn.h)
   build      in-tree hipcc build of the library for gfx950
   workloads  seeded synthetic inputs (cache shapes, ranges, block tables)
 
