@@ -236,6 +236,7 @@ __global__ __launch_bounds__(kThreads) void prompt_kernel(PromptArgs a) {
   {
     const int t = tok < nq ? tok : nq - 1;
     const uint16_t *p = a.q.base + (q0 + t) * a.q.token + hq * a.q.head + 8 * half;
+#pragma unroll
     for (int i = 0; i < D / 16; ++i)
       q[i] = *reinterpret_cast<const frag8 *>(p + 16 * i);
   }
@@ -243,6 +244,7 @@ __global__ __launch_bounds__(kThreads) void prompt_kernel(PromptArgs a) {
   const uint16_t *kb = a.k.base + k0 * a.k.token + hk * a.k.head;
   const uint16_t *vb = a.v.base + k0 * a.v.token + hk * a.v.head;
   const auto load = [&](int step, int buf) {
+#pragma unroll
     for (int i = 0; i < kIssues; ++i) {
       const int at = i * kThreads + wave * 64;
       const int row = (at + lane) / kChunks, pos = (at + lane) % kChunks;
@@ -260,7 +262,9 @@ __global__ __launch_bounds__(kThreads) void prompt_kernel(PromptArgs a) {
   };
 
   f32x16 o[D / 32];
+#pragma unroll
   for (int d = 0; d < D / 32; ++d)
+#pragma unroll
     for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
   float m = -INFINITY, l = 0.0f;
 
@@ -273,9 +277,12 @@ __global__ __launch_bounds__(kThreads) void prompt_kernel(PromptArgs a) {
     if (step >= wave_steps) continue;
     // ---- scores, keys down and queries across
     f32x16 sc[2];
+#pragma unroll
     for (int t = 0; t < 2; ++t) {
+#pragma unroll
       for (int i = 0; i < 16; ++i) sc[t][i] = 0.0f;
       const int row = t * 32 + col;
+#pragma unroll
       for (int i = 0; i < D / 16; ++i) {
         const frag8 k = *reinterpret_cast<const frag8 *>(
             &lds[buf][0][row * D + 8 * ((2 * i + half) ^ swizzle_k<D>(row))]);
@@ -283,7 +290,9 @@ __global__ __launch_bounds__(kThreads) void prompt_kernel(PromptArgs a) {
       }
     }
     if (step * kKeys + kKeys - 1 > w0 + behind) {
+#pragma unroll
       for (int t = 0; t < 2; ++t)
+#pragma unroll
         for (int i = 0; i < 16; ++i) {
           const int key = step * kKeys + t * 32 + 8 * (i / 4) + 4 * half + i % 4;
           if (key > limit) sc[t][i] = -INFINITY;
@@ -291,7 +300,9 @@ __global__ __launch_bounds__(kThreads) void prompt_kernel(PromptArgs a) {
     }
     // ---- running maximum: moved only when a score passes it by kSlack
     float top = -INFINITY;
+#pragma unroll
     for (int t = 0; t < 2; ++t)
+#pragma unroll
       for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[t][i]);
     top = fmaxf(top, other_half(top)) * a.scale_log2;
     if (__any(top > m + kSlack)) {
@@ -299,12 +310,16 @@ __global__ __launch_bounds__(kThreads) void prompt_kernel(PromptArgs a) {
       const float c = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
       m = mn;
       l *= c;
+#pragma unroll
       for (int d = 0; d < D / 32; ++d)
+#pragma unroll
         for (int i = 0; i < 16; ++i) o[d][i] *= c;
     }
     const float ms = m == -INFINITY ? 0.0f : m;
     frag8 p[4];
+#pragma unroll
     for (int t = 0; t < 2; ++t)
+#pragma unroll
       for (int i = 0; i < 16; ++i) {
         const float x =
             __builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][i], a.scale_log2, -ms));
@@ -312,15 +327,19 @@ __global__ __launch_bounds__(kThreads) void prompt_kernel(PromptArgs a) {
         p[2 * t + i / 8][i % 8] = short(rounded<kBf16>(x));
       }
     // ---- weighted values
+#pragma unroll
     for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
       for (int d = 0; d < D / 32; ++d) {
         frag8 v;
+#pragma unroll
         for (int b = 0; b < 2; ++b) {
           const int row = ks * 16 + 8 * b + 4 * half + ((lane & 15) >> 2);
           const int at = d * 32 + (lane & 16) + 4 * (lane & 3);
           const frag4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(
               frag4, &lds[buf][1][row * D + 8 * ((at >> 3) ^ swizzle_v<D>(row)) +
                                   (at & 7)]));
+#pragma unroll
           for (int i = 0; i < 4; ++i) v[4 * b + i] = x[i];
         }
         o[d] = mfma<kBf16>(v, p[ks], o[d]);
@@ -330,9 +349,12 @@ __global__ __launch_bounds__(kThreads) void prompt_kernel(PromptArgs a) {
   l += other_half(l);
   const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
   uint16_t *out = a.out + ((q0 + tok) * a.q_heads + hq) * D;
+#pragma unroll
   for (int d = 0; d < D / 32; ++d)
+#pragma unroll
     for (int g = 0; g < 2; ++g) {
       uint32_t w[4];
+#pragma unroll
       for (int b = 0; b < 4; ++b) {
         const int i = 8 * g + 2 * b;
         w[b] = uint32_t(rounded<kBf16>(o[d][i] * inv)) |
