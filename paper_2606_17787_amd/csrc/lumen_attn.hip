@@ -359,6 +359,7 @@ struct DecodeArgs {
   const uint8_t *k, *v;  // of the layer
   const int32_t *bt;
   int32_t bt_cols, block_size;
+  int32_t block_shift;  // log2 of block_size, or -1
   int64_t num_blocks;
   const int32_t *lens;
   int32_t num_reqs, heads, group;
@@ -367,61 +368,460 @@ struct DecodeArgs {
   float scale_log2;  // scale * log2(e)
   uint16_t *out;
   int32_t *status;
+  int32_t workers;  // workgroups of one head
+  uint32_t *arrived;  // [num_reqs][heads of the grid]
+  float *parts;       // [workers * heads of the grid][2][part_floats(D)]
 };
 
-// One wavefront per (request, query head), a key at a time.
+typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+typedef _Float16 half8v __attribute__((ext_vector_type(8)));
+typedef float float4v __attribute__((ext_vector_type(4)));
+
+constexpr int kDecodeWaves = 4;
+constexpr int kDecodeThreads = kDecodeWaves * kWave;
+constexpr int kBlockKeys = 32;                         // keys a wavefront takes at a time
+constexpr int kUnitKeys = kBlockKeys * kDecodeWaves;   // and its workgroup
+constexpr int kQueries = 16;                           // columns of a product
+// Weights are 2^(s - m + kBias) with s - m at most kRise: within a 16-bit
+// float up to 2^14, and down to 2^-38 of the largest before they vanish.
+constexpr float kRise = 8.0f, kBias = 6.0f;
+
+// Floats of one partial result: D * kQueries sums, then a maximum and a sum
+// for each query.
+constexpr int part_floats(int D) { return D * kQueries + 2 * kQueries; }
+
+__device__ __forceinline__ half2v as_half2(uint32_t x) {
+  return __builtin_bit_cast(half2v, x);
+}
+
+// Codes of four places in each 16-bit half of w (element i of the low half
+// and of the high half in result i) as 64 + q: the code in bits 4..7 of a
+// 16-bit float whose last place is 1/16 of its unit, 2^6 * (1 + q / 64).
+__device__ __forceinline__ void codes4(uint32_t w, half2v *x) {
+  constexpr uint32_t kMask = 0x00f000f0u, kOne = 0x54005400u;
+  x[0] = as_half2(((w << 4) & kMask) | kOne);
+  x[1] = as_half2((w & kMask) | kOne);
+  x[2] = as_half2(((w >> 4) & kMask) | kOne);
+  x[3] = as_half2(((w >> 8) & kMask) | kOne);
+}
+
+// Maximum and sum over the four lanes of one query (l % 16).
+__device__ __forceinline__ float quad_max(float x) {
+  x = fmaxf(x, __shfl_xor(x, 16));
+  return fmaxf(x, __shfl_xor(x, 32));
+}
+__device__ __forceinline__ float quad_sum(float x) {
+  x += __shfl_xor(x, 16);
+  return x + __shfl_xor(x, 32);
+}
+
+// What a wavefront holds of one block of keys before it is used.
+template <int D>
+struct KeyBlock {
+  uint32_t k[2][D / 32], kp[2];              // two tiles of 16 keys: codes, pair
+  uint32_t v[8][D >= 128 ? D / 128 : 1], vp[8];  // eight keys of the lane
+  uint32_t live;                             // keys that count, a bit each
+};
+
+// Decode attention, bound by the cache's bytes: D/2 + 16 a row, read once.
+// Every worker (workgroup) takes an equal share of the requests' key units of
+// 128, whatever their lengths, so a share may start and end inside a request;
+// partial results of a request are joined by the last of its workers to
+// arrive, in a fixed order.  Within a unit each wavefront takes 32 keys and
+// keeps its own running maximum and sums; no LDS is used before the end.
+//
+// One block of 32 keys: scores^T = K Q^T and sums^T = V^T P^T by 16x16x32
+// products of 16-bit floats, queries across (the heads of the group, up to 16).
+// A lane reads its key's codes with one load and holds them in the product's
+// order at once, because the sum over head_dim may run in any order: lanes l /
+// 16 take the four quarters of the row, each with one pair (A, B).  The scores
+// come out as the weights' operand goes in when the keys are taken in the same
+// order again, so the weights never leave their lanes.  For V a lane holds D/16
+// consecutive elements of 8 keys, all of one quarter.  Values are exact: code
+// and pair give the stored value by one fused multiply-add that rounds as the
+// format says.
 template <int D, bool kBf16>
-__global__ __launch_bounds__(kWave) void decode4_kernel(DecodeArgs a) {
-  constexpr int kE = D / 64;  // elements a lane
+__global__ __launch_bounds__(kDecodeThreads, D == 256 ? 2 : 3) void decode4_kernel(DecodeArgs a) {
   constexpr int kRow = D / 2 + 16;
-  const int r = blockIdx.x, hq = blockIdx.y, lane = threadIdx.x;
-  const int h = hq / a.group;
-  const uint16_t *q = a.q.base + int64_t(r) * a.q.token + int64_t(hq) * a.q.head;
-  float x[kE], o[kE];
-  for (int e = 0; e < kE; ++e) {
-    x[e] = value<kBf16>(q[lane * kE + e]) * a.scale_log2;
-    o[e] = 0.0f;
+  constexpr int kSteps = D / 32;  // products over head_dim
+  constexpr int kE = D / 16;      // elements of V a lane holds of a key
+  __shared__ float lds_o[kDecodeWaves - 1][kE][4 * kWave];
+  __shared__ float lds_m[kDecodeWaves][kQueries], lds_l[kDecodeWaves][kQueries];
+  __shared__ uint64_t lds_scan[kDecodeWaves];
+  __shared__ uint64_t lds_first;  // of the request that a share starts in
+  __shared__ int lds_req;
+  __shared__ uint32_t lds_last;
+
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
+  const int n = lane & 15, quad = lane >> 4;
+  const int worker = blockIdx.x % a.workers, hg = blockIdx.x / a.workers;
+  const int tiles = (a.group + kQueries - 1) / kQueries;
+  const int h = hg / tiles, g0 = hg % tiles * kQueries;
+  const int rows = a.group - g0 < kQueries ? a.group - g0 : kQueries;
+  const int num_hg = a.heads * tiles;
+  int err = LUMEN_OK;
+
+  // ---- the share: units [u0, u1) of all requests' units
+  const int64_t cap = int64_t(a.bt_cols) * a.block_size;
+  const auto length = [&](int r) {
+    const int64_t len = a.lens[r];
+    return len < 0 ? int64_t(0) : len < cap ? len : cap;
+  };
+  const auto units_of = [&](int64_t len) {
+    return len <= kUnitKeys ? uint64_t(1)
+                            : uint64_t(len + kUnitKeys - 1) / kUnitKeys;
+  };
+  const int per = (a.num_reqs + kDecodeThreads - 1) / kDecodeThreads;
+  const int ra = tid * per < a.num_reqs ? tid * per : a.num_reqs;
+  const int rb = ra + per < a.num_reqs ? ra + per : a.num_reqs;
+  uint64_t mine = 0;
+  for (int r = ra; r < rb; ++r) {
+    const int len = a.lens[r];
+    if (len < 0 || len > cap) err = LUMEN_ERR_RANGE;
+    mine += units_of(length(r));
   }
-  const int len = a.lens[r];
-  int err = len < 0 ? LUMEN_ERR_RANGE : LUMEN_OK;
-  float m = -INFINITY, l = 0.0f;
-  for (int t = 0; t < len; ++t) {
-    const int page = t / a.block_size;
-    if (page >= a.bt_cols) {
-      err = err < LUMEN_ERR_RANGE ? err : LUMEN_ERR_RANGE;
-      break;
+  uint64_t upto = mine;
+  for (int o = 1; o < kWave; o <<= 1) {
+    const uint64_t x = __shfl_up(upto, o);
+    if (lane >= o) upto += x;
+  }
+  if (lane == kWave - 1) lds_scan[wave] = upto;
+  __syncthreads();
+  uint64_t total = 0;
+  for (int w = 0; w < kDecodeWaves; ++w) {
+    if (w < wave) upto += lds_scan[w];
+    total += lds_scan[w];
+  }
+  const uint64_t shares = total < uint64_t(a.workers) ? total : uint64_t(a.workers);
+  if (uint64_t(worker) >= shares) return;  // the whole workgroup
+  const uint64_t u0 = total * worker / shares, u1 = total * (worker + 1) / shares;
+  if (u0 >= upto - mine && u0 < upto) {
+    uint64_t at = upto - mine;
+    int r = ra;
+    for (;; ++r) {
+      const uint64_t c = units_of(length(r));
+      if (u0 < at + c) break;
+      at += c;
     }
-    const int32_t id = a.bt[int64_t(r) * a.bt_cols + page];
-    if (id < 0 || id >= a.num_blocks) {
-      err = err < LUMEN_ERR_BLOCK_ID ? err : LUMEN_ERR_BLOCK_ID;
-      continue;
-    }
-    const int64_t off = row_offset(int64_t(id) * a.block_size + t % a.block_size,
-                                   a.block_size, h, a.heads, a.hnd, kRow);
-    float kv[2][kE];
-    for (int w = 0; w < 2; ++w) {
-      const uint8_t *row = (w ? a.v : a.k) + off;
-      const uint32_t pair =
-          reinterpret_cast<const uint32_t *>(row + D / 2)[lane / 16];
-      for (int e = 0; e < kE; ++e) {
-        const int n = lane * kE + e;
-        const int code = (row[n / 2] >> (4 * (n & 1))) & 15;
-        kv[w][e] = float(_Float16(float(half_of(pair)) * float(64 + code) +
-                                  float(half_of(pair >> 16))));
+    lds_req = r;
+    lds_first = at;
+  }
+  __syncthreads();
+  int r = __builtin_amdgcn_readfirstlane(lds_req);
+  uint64_t first = lds_first;  // first unit of request r
+  const auto share_of = [&](uint64_t unit) {
+    return int(((unit + 1) * shares + total - 1) / total) - 1;
+  };
+
+  uint64_t u = u0;
+  while (u < u1) {
+    const int64_t len = length(r);
+    const uint64_t units = units_of(len);
+    const uint64_t stop = first + units < u1 ? first + units : u1;
+    const int64_t key_end =
+        int64_t(stop - first) * kUnitKeys < len ? int64_t(stop - first) * kUnitKeys : len;
+    const int64_t key_begin = int64_t(u - first) * kUnitKeys;
+
+    // ---- Q: 16-bit floats under a power of two of the row's own, so that
+    // bf16 and fp16 keep all their bits whatever their range
+    half8v q[kSteps];
+    float cq;
+    {
+      const uint16_t *p = a.q.base + int64_t(r) * a.q.token +
+                          int64_t(h * a.group + g0 + (n < rows ? n : 0)) * a.q.head +
+                          quad * (D / 4);
+      uint4 raw[kSteps];
+      float big = 0.0f, x[8];
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i) {
+        raw[i] = *reinterpret_cast<const uint4 *>(p + 8 * i);
+        unpack8<kBf16>(raw[i], x);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) big = fmaxf(big, fabsf(x[j]));
+      }
+      big = quad_max(big);
+      uint32_t e = __builtin_bit_cast(uint32_t, big) >> 23;  // NaN: not the maximum
+      e = e == 255 ? 140 : e < 14 ? 14 : e;
+      const float up = __builtin_bit_cast(float, (267 - e) << 23);  // to 2^13..2^14
+      cq = a.scale_log2 * __builtin_bit_cast(float, (e - 13) << 23);
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i) {
+        unpack8<kBf16>(raw[i], x);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          q[i][2 * j] = _Float16(x[j] * up);
+          q[i][2 * j + 1] = _Float16(x[j + 4] * up);
+        }
       }
     }
-    float s = 0.0f;
-    for (int e = 0; e < kE; ++e) s += x[e] * kv[0][e];
-    for (int b = 1; b < kWave; b <<= 1) s += __shfl_xor(s, b);
-    const float mn = fmaxf(m, s);
-    const float c = exp2f(m - mn), p = exp2f(s - mn);
-    m = mn;
-    l = l * c + p;
-    for (int e = 0; e < kE; ++e) o[e] = o[e] * c + p * kv[1][e];
+
+    float4v o[kE];
+#pragma unroll
+    for (int j = 0; j < kE; ++j) o[j] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+    float m = -INFINITY, l = 0.0f;
+
+    // Row of the lane's key of a block (lanes 32 to 63 repeat 0 to 31), and
+    // whether it counts.
+    const int32_t *table = a.bt + int64_t(r) * a.bt_cols;
+    const auto row_of = [&](int64_t key0, bool *live) {
+      const int64_t key = key0 + (lane & 31);
+      *live = key < key_end;
+      if (!*live) return 0u;
+      const uint32_t t = uint32_t(key);  // lengths are 32 bits
+      const uint32_t page = a.block_shift >= 0 ? t >> a.block_shift
+                                               : t / uint32_t(a.block_size);
+      const uint32_t pos = t - page * uint32_t(a.block_size);
+      const int32_t id = table[page];
+      if (id < 0 || id >= a.num_blocks) {
+        err = LUMEN_ERR_BLOCK_ID;
+        *live = false;
+        return 0u;
+      }
+      const uint32_t b = uint32_t(id), bs = uint32_t(a.block_size);
+      return a.hnd ? (b * uint32_t(a.heads) + h) * bs + pos
+                   : (b * bs + pos) * uint32_t(a.heads) + h;
+    };
+    const auto fetch = [&](int64_t key0, KeyBlock<D> &kb) {
+      bool live;
+      const uint32_t row = row_of(key0, &live);
+      kb.live = uint32_t(__ballot(live));
+      if (kb.live == 0) return;  // row 0 exists where any row does
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const uint8_t *p = a.k + uint64_t(uint32_t(__shfl(row, 16 * t + n))) * kRow;
+        const uint32_t *c = reinterpret_cast<const uint32_t *>(p + quad * (D / 8));
+        if constexpr (D == 64) {
+          const uint2 x = *reinterpret_cast<const uint2 *>(c);
+          kb.k[t][0] = x.x, kb.k[t][1] = x.y;
+        } else {
+#pragma unroll
+          for (int i = 0; i < kSteps; i += 4) {
+            const uint4 x = *reinterpret_cast<const uint4 *>(c + i);
+            kb.k[t][i] = x.x, kb.k[t][i + 1] = x.y;
+            kb.k[t][i + 2] = x.z, kb.k[t][i + 3] = x.w;
+          }
+        }
+        kb.kp[t] = *reinterpret_cast<const uint32_t *>(p + D / 2 + 4 * quad);
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int key = j < 4 ? 4 * quad + j : 12 + 4 * quad + j;
+        const uint8_t *p = a.v + uint64_t(uint32_t(__shfl(row, key))) * kRow;
+        if constexpr (D == 64) {
+          kb.v[j][0] = *reinterpret_cast<const uint16_t *>(p + 2 * n);
+        } else if constexpr (D == 128) {
+          kb.v[j][0] = *reinterpret_cast<const uint32_t *>(p + 4 * n);
+        } else {
+          const uint2 x = *reinterpret_cast<const uint2 *>(p + 8 * n);
+          kb.v[j][0] = x.x, kb.v[j][kE / 8 - 1] = x.y;
+        }
+        kb.vp[j] = *reinterpret_cast<const uint32_t *>(p + D / 2 + 4 * (n / 4));
+      }
+    };
+    const auto use = [&](KeyBlock<D> &kb) {
+      if (kb.live == 0) return;
+      float4v s[2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        s[t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+        const half2v pair = as_half2(kb.kp[t]);
+        const half2v A = {pair[0], pair[0]}, B = {pair[1], pair[1]};
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+          half2v x[4];
+          codes4(kb.k[t][i], x);
+          half8v f;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const half2v y = __builtin_elementwise_fma(x[j], A, B);
+            f[2 * j] = y[0];
+            f[2 * j + 1] = y[1];
+          }
+          s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f, q[i], s[t], 0, 0, 0);
+        }
+      }
+      if (kb.live != 0xffffffffu) {
+        // a key left out has no score, and no value either: its pair may be NaN
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int key = j < 4 ? 4 * quad + j : 12 + 4 * quad + j;
+          const bool in = (kb.live >> key) & 1;
+          if (!in) s[j / 4][j % 4] = -INFINITY;
+          if (!in) kb.vp[j] = 0;
+        }
+      }
+      float top = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) top = fmaxf(top, s[j / 4][j % 4]);
+      top = quad_max(top) * cq;
+      if (__any(top > m + kRise)) {
+        const float mn = fmaxf(m, top);
+        const float c = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
+        m = mn;
+        l *= c;
+#pragma unroll
+        for (int j = 0; j < kE; ++j) o[j] *= c;
+      }
+      const float shift = kBias - (m == -INFINITY ? 0.0f : m);
+      half8v p;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float x = __builtin_amdgcn_exp2f(
+            __builtin_fmaf(s[j / 4][j % 4], cq, shift));
+        l += x;
+        p[j] = _Float16(x);
+      }
+      half2v A[4], B[4];  // of keys 2j and 2j + 1 of the lane
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        A[j] = as_half2(__builtin_amdgcn_perm(kb.vp[2 * j + 1], kb.vp[2 * j], 0x05040100));
+        B[j] = as_half2(__builtin_amdgcn_perm(kb.vp[2 * j + 1], kb.vp[2 * j], 0x07060302));
+      }
+#pragma unroll
+      for (int w = 0; w < kE / 4; ++w) {  // four elements at a time
+        half8v f[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          half2v x[4];
+          codes4(__builtin_amdgcn_perm(kb.v[2 * j + 1][w / 2], kb.v[2 * j][w / 2],
+                                       w % 2 ? 0x07060302 : 0x05040100), x);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const half2v y = __builtin_elementwise_fma(x[e], A[j], B[j]);
+            f[e][2 * j] = y[0];
+            f[e][2 * j + 1] = y[1];
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          o[4 * w + e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[e], p, o[4 * w + e],
+                                                                0, 0, 0);
+      }
+    };
+
+    KeyBlock<D> cur, next;
+    int64_t key = key_begin + wave * kBlockKeys;
+    fetch(key, cur);
+    for (; key < key_end; key += kUnitKeys) {
+      fetch(key + kUnitKeys, next);
+      use(cur);
+      cur = next;
+    }
+    l = quad_sum(l);
+
+    // Joins the wavefronts' results into wavefront 0's o, m and l.
+    const auto join = [&]() {
+      if (quad == 0) lds_m[wave][n] = m;
+      __syncthreads();
+      float mm = m;
+#pragma unroll
+      for (int w = 0; w < kDecodeWaves; ++w) mm = fmaxf(mm, lds_m[w][n]);
+      const float c = mm == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - mm);
+      m = mm;
+      l *= c;
+      if (quad == 0) lds_l[wave][n] = l;
+#pragma unroll
+      for (int j = 0; j < kE; ++j) {
+        o[j] *= c;
+        if (wave > 0)
+          *reinterpret_cast<float4v *>(&lds_o[wave - 1][j][4 * lane]) = o[j];
+      }
+      __syncthreads();
+      if (wave == 0) {
+#pragma unroll
+        for (int w = 1; w < kDecodeWaves; ++w) {
+          l += lds_l[w][n];
+#pragma unroll
+          for (int j = 0; j < kE; ++j)
+            o[j] += *reinterpret_cast<const float4v *>(&lds_o[w - 1][j][4 * lane]);
+        }
+      }
+    };
+    join();
+
+    const bool whole = u == first && stop == first + units;
+    bool done = whole;
+    if (!whole) {
+      const int wa = share_of(first), wb = share_of(first + units - 1);
+      // a worker's share may end one request and start another: two places
+      const auto part_of = [&](int w) {
+        return a.parts + ((int64_t(hg) * a.workers + w) * 2 + (w == wa)) *
+                             part_floats(D);
+      };
+      if (wave == 0) {
+        float *to = part_of(worker);
+        if (n < rows) {
+#pragma unroll
+          for (int j = 0; j < kE; ++j)
+            *reinterpret_cast<float4v *>(to + (j * kWave + lane) * 4) = o[j];
+          if (quad == 0) {
+            to[D * kQueries + n] = m;
+            to[D * kQueries + kQueries + n] = l;
+          }
+        }
+        __threadfence();
+        if (lane == 0) {
+          uint32_t *count = a.arrived + int64_t(r) * num_hg + hg;
+          const uint32_t before = __hip_atomic_fetch_add(
+              count, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+          lds_last = before == uint32_t(wb - wa);
+          if (before == uint32_t(wb - wa))  // ready for the next call
+            __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+      }
+      __syncthreads();
+      if (lds_last) {
+        __threadfence();
+        done = true;
+#pragma unroll
+        for (int j = 0; j < kE; ++j) o[j] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+        m = -INFINITY, l = 0.0f;
+        for (int w = wa + wave; w <= wb; w += kDecodeWaves) {
+          const float *from = part_of(w);
+          if (n >= rows) continue;
+          const float pm = from[D * kQueries + n];
+          const float pl = from[D * kQueries + kQueries + n];
+          const float mn = fmaxf(m, pm);
+          const float c0 = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
+          const float c1 = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(pm - mn);
+          m = mn;
+          l = l * c0 + pl * c1;
+#pragma unroll
+          for (int j = 0; j < kE; ++j) {
+            const float4v x =
+                *reinterpret_cast<const float4v *>(from + (j * kWave + lane) * 4);
+            o[j] = o[j] * c0 + x * c1;
+          }
+        }
+        join();
+      }
+    }
+    if (done && wave == 0 && n < rows) {
+      const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+      uint16_t *out =
+          a.out + (int64_t(r) * a.heads * a.group + h * a.group + g0 + n) * D;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float x[kE < 8 ? 8 : kE];
+#pragma unroll
+        for (int j = 0; j < kE; ++j) x[j] = o[j][i] * inv;
+        uint16_t *to = out + (4 * quad + i) * kE;
+        if constexpr (kE == 4) {
+          *reinterpret_cast<uint2 *>(to) =
+              uint2{uint32_t(rounded<kBf16>(x[0])) | uint32_t(rounded<kBf16>(x[1])) << 16,
+                    uint32_t(rounded<kBf16>(x[2])) | uint32_t(rounded<kBf16>(x[3])) << 16};
+        } else {
+#pragma unroll
+          for (int j = 0; j < kE; j += 8)
+            *reinterpret_cast<uint4 *>(to + j) = pack8<kBf16>(x + j);
+        }
+      }
+    }
+    u = stop;
+    first += units;
+    ++r;
+    __syncthreads();  // the LDS is used again
   }
-  uint16_t *out = a.out + (int64_t(r) * a.heads * a.group + hq) * D;
-  for (int e = 0; e < kE; ++e)
-    out[lane * kE + e] = rounded<kBf16>(l > 0.0f || l != l ? o[e] / l : 0.0f);
   record_wave(a.status, err);
 }
 
@@ -451,6 +851,35 @@ int check_layout(const lumen_kv_layout *l, int32_t layer, Layer *out) {
   out->k = int64_t(layer) * 2 * half;
   out->v = out->k + half;
   return LUMEN_OK;
+}
+
+// Grid and workspace of a decode call on a device of `cus` compute units.
+struct DecodePlan {
+  int32_t heads;    // KV heads times tiles of 16 query heads
+  int32_t workers;  // workgroups of one of them
+  size_t parts_at, bytes;
+};
+
+// The workspace is sized for the largest device of this architecture, so that
+// its size needs no device.
+constexpr int kMaxUnits = 256;
+
+DecodePlan decode_plan(const lumen_kv_layout *l, int32_t head_dim,
+                       int32_t num_reqs, int32_t num_q_heads, int cus) {
+  const int group = num_q_heads / l->num_kv_heads;
+  DecodePlan p;
+  p.heads = l->num_kv_heads * ((group + kQueries - 1) / kQueries);
+  // as many workgroups as are resident at once, three a CU; a multiple of 8
+  // for each head puts all heads of a share on one XCD, whose L2 then serves
+  // the lines that token-major rows of different heads have in common
+  const int all = (cus < kMaxUnits ? cus : kMaxUnits) * 3;
+  p.workers = all / p.heads;
+  if (p.workers > 8) p.workers &= ~7;
+  if (p.workers < 1) p.workers = 1;
+  p.parts_at = (size_t(num_reqs) * p.heads * sizeof(uint32_t) + 255) & ~size_t(255);
+  p.bytes = p.parts_at + size_t(p.workers) * p.heads * 2 * part_floats(head_dim) *
+                             sizeof(float);
+  return p;
 }
 
 template <bool kAppend>
@@ -587,7 +1016,7 @@ size_t lumen_attn_decode4_workspace_bytes(const lumen_kv_layout *layout,
       num_reqs > LUMEN_ATTN_MAX_REQS || num_q_heads < 1 ||
       num_q_heads % layout->num_kv_heads)
     return 0;
-  return 16;
+  return decode_plan(layout, at.head_dim, num_reqs, num_q_heads, kMaxUnits).bytes;
 }
 
 int lumen_attn_decode4(const lumen_kv_layout *layout, int32_t layer,
@@ -619,12 +1048,22 @@ int lumen_attn_decode4(const lumen_kv_layout *layout, int32_t layer,
       !aligned(d_workspace, 16) || !aligned(d_lens, 4) ||
       !aligned(d_block_tables, 4))
     return LUMEN_ERR_MISALIGNED;
+  if (int64_t(layout->num_blocks) * layout->block_size >
+      int64_t(UINT32_MAX) / layout->num_kv_heads)
+    return LUMEN_ERR_UNSUPPORTED;  // rows are counted in 32 bits
+  int cus = 0;
+  if ((st = compute_units(&cus)) != LUMEN_OK) return st;
   (void)hipGetLastError();
+  const DecodePlan plan =
+      decode_plan(layout, at.head_dim, num_reqs, num_q_heads, cus);
+  uint32_t *arrived = static_cast<uint32_t *>(d_workspace);
+  const int32_t bs = layout->block_size;
   DecodeArgs a{static_cast<const uint8_t *>(d_cache) + at.k,
                static_cast<const uint8_t *>(d_cache) + at.v,
                d_block_tables,
                bt_cols,
-               layout->block_size,
+               bs,
+               (bs & (bs - 1)) == 0 ? __builtin_ctz(unsigned(bs)) : -1,
                layout->num_blocks,
                d_lens,
                num_reqs,
@@ -634,14 +1073,18 @@ int lumen_attn_decode4(const lumen_kv_layout *layout, int32_t layer,
                rows_of(q, 0),
                scale * 1.44269504088896341f,
                static_cast<uint16_t *>(d_out),
-               d_status};
+               d_status,
+               plan.workers,
+               arrived,
+               reinterpret_cast<float *>(static_cast<char *>(d_workspace) +
+                                         plan.parts_at)};
   const bool bf = dtype == LUMEN_ATTN_BF16;
   void (*kernel)(DecodeArgs) =
       at.head_dim == 64    ? (bf ? decode4_kernel<64, true> : decode4_kernel<64, false>)
       : at.head_dim == 128 ? (bf ? decode4_kernel<128, true> : decode4_kernel<128, false>)
                            : (bf ? decode4_kernel<256, true> : decode4_kernel<256, false>);
-  hipLaunchKernelGGL(kernel, dim3(unsigned(num_reqs), unsigned(num_q_heads)),
-                     dim3(kWave), 0, static_cast<hipStream_t>(stream), a);
+  hipLaunchKernelGGL(kernel, dim3(unsigned(plan.workers * plan.heads)),
+                     dim3(kDecodeThreads), 0, static_cast<hipStream_t>(stream), a);
   return hipGetLastError() == hipSuccess ? LUMEN_OK : LUMEN_ERR_HIP;
 }
 
