@@ -359,7 +359,7 @@ struct DecodeArgs {
   const uint8_t *k, *v;  // of the layer
   const int32_t *bt;
   int32_t bt_cols, block_size;
-  int32_t block_shift;  // log2 of block_size, or -1
+  int32_t block_shift;  // log2 of block_size where that is whole
   int64_t num_blocks;
   const int32_t *lens;
   int32_t num_reqs, heads, group;
@@ -396,23 +396,25 @@ __device__ __forceinline__ half2v as_half2(uint32_t x) {
 
 // Codes of four places in each 16-bit half of w (element i of the low half
 // and of the high half in result i) as 64 + q: the code in bits 4..7 of a
-// 16-bit float whose last place is 1/16 of its unit, 2^6 * (1 + q / 64).
-__device__ __forceinline__ void codes4(uint32_t w, half2v *x) {
-  constexpr uint32_t kMask = 0x00f000f0u, kOne = 0x54005400u;
-  x[0] = as_half2(((w << 4) & kMask) | kOne);
-  x[1] = as_half2((w & kMask) | kOne);
-  x[2] = as_half2(((w >> 4) & kMask) | kOne);
-  x[3] = as_half2(((w >> 8) & kMask) | kOne);
+// 16-bit float whose last place is 1/16 of its unit, 2^6 * (1 + q / 64).  `one`
+// is kCodeOne, `mask` kCodeMask, in registers: an and-or takes no literals.
+constexpr uint32_t kCodeMask = 0x00f000f0u, kCodeOne = 0x54005400u;
+__device__ __forceinline__ void codes4(uint32_t w, uint32_t mask, uint32_t one,
+                                       half2v *x) {
+  x[0] = as_half2(((w << 4) & mask) | one);
+  x[1] = as_half2((w & mask) | one);
+  x[2] = as_half2(((w >> 4) & mask) | one);
+  x[3] = as_half2(((w >> 8) & mask) | one);
 }
 
 // Maximum and sum over the four lanes of one query (l % 16).
 __device__ __forceinline__ float quad_max(float x) {
-  x = fmaxf(x, __shfl_xor(x, 16));
-  return fmaxf(x, __shfl_xor(x, 32));
+  x = fmaxf(x, swapped<16>(x));
+  return fmaxf(x, swapped<32>(x));
 }
 __device__ __forceinline__ float quad_sum(float x) {
-  x += __shfl_xor(x, 16);
-  return x + __shfl_xor(x, 32);
+  x += swapped<16>(x);
+  return x + swapped<32>(x);
 }
 
 // What a wavefront holds of one block of keys before it is used.
@@ -422,6 +424,19 @@ struct KeyBlock {
   uint32_t v[8][D >= 128 ? D / 128 : 1], vp[8];  // eight keys of the lane
   uint32_t live;                             // keys that count, a bit each
 };
+
+// A value that is the same in all lanes, in scalar registers.
+__device__ __forceinline__ uint64_t uniform(uint64_t x) {
+  return uint64_t(__builtin_amdgcn_readfirstlane(uint32_t(x))) |
+         uint64_t(__builtin_amdgcn_readfirstlane(uint32_t(x >> 32))) << 32;
+}
+
+struct Place {
+  int32_t id[2];  // kAligned
+  int32_t row;    // otherwise: the block of the lane's key
+};
+
+#define CONSTANT_PTR(T, p) ((const __attribute__((address_space(4))) T *)(p))
 
 // Decode attention, bound by the cache's bytes: D/2 + 16 a row, read once.
 // Every worker (workgroup) takes an equal share of the requests' key units of
@@ -440,7 +455,12 @@ struct KeyBlock {
 // consecutive elements of 8 keys, all of one quarter.  Values are exact: code
 // and pair give the stored value by one fused multiply-add that rounds as the
 // format says.
-template <int D, bool kBf16>
+//
+// kAligned: pages are 16 * 2^k tokens, so that a tile of 16 keys lies in one
+// page and its address is the wavefront's, not the lane's: block ids come by
+// scalar loads and the keys' rows from one vector offset.  Other page sizes
+// look each key's row up on a lane of its own and pass it round.
+template <int D, bool kBf16, bool kAligned>
 __global__ __launch_bounds__(kDecodeThreads, D == 256 ? 2 : 3) void decode4_kernel(DecodeArgs a) {
   constexpr int kRow = D / 2 + 16;
   constexpr int kSteps = D / 32;  // products over head_dim
@@ -452,7 +472,8 @@ __global__ __launch_bounds__(kDecodeThreads, D == 256 ? 2 : 3) void decode4_kern
   __shared__ int lds_req;
   __shared__ uint32_t lds_last;
 
-  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
+  const int tid = threadIdx.x, lane = tid & (kWave - 1);
+  const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int n = lane & 15, quad = lane >> 4;
   const int worker = blockIdx.x % a.workers, hg = blockIdx.x / a.workers;
   const int tiles = (a.group + kQueries - 1) / kQueries;
@@ -460,6 +481,9 @@ __global__ __launch_bounds__(kDecodeThreads, D == 256 ? 2 : 3) void decode4_kern
   const int rows = a.group - g0 < kQueries ? a.group - g0 : kQueries;
   const int num_hg = a.heads * tiles;
   int err = LUMEN_OK;
+  uint32_t mask, one;  // not to be folded into literals again
+  asm("s_mov_b32 %0, %1" : "=s"(mask) : "i"(kCodeMask));
+  asm("v_mov_b32 %0, %1" : "=v"(one) : "i"(kCodeOne));
 
   // ---- the share: units [u0, u1) of all requests' units
   const int64_t cap = int64_t(a.bt_cols) * a.block_size;
@@ -492,6 +516,7 @@ __global__ __launch_bounds__(kDecodeThreads, D == 256 ? 2 : 3) void decode4_kern
     if (w < wave) upto += lds_scan[w];
     total += lds_scan[w];
   }
+  total = uniform(total);
   const uint64_t shares = total < uint64_t(a.workers) ? total : uint64_t(a.workers);
   if (uint64_t(worker) >= shares) return;  // the whole workgroup
   const uint64_t u0 = total * worker / shares, u1 = total * (worker + 1) / shares;
@@ -508,7 +533,7 @@ __global__ __launch_bounds__(kDecodeThreads, D == 256 ? 2 : 3) void decode4_kern
   }
   __syncthreads();
   int r = __builtin_amdgcn_readfirstlane(lds_req);
-  uint64_t first = lds_first;  // first unit of request r
+  uint64_t first = uniform(lds_first);  // first unit of request r
   const auto share_of = [&](uint64_t unit) {
     return int(((unit + 1) * shares + total - 1) / total) - 1;
   };
@@ -560,62 +585,105 @@ __global__ __launch_bounds__(kDecodeThreads, D == 256 ? 2 : 3) void decode4_kern
     for (int j = 0; j < kE; ++j) o[j] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
     float m = -INFINITY, l = 0.0f;
 
-    // Row of the lane's key of a block (lanes 32 to 63 repeat 0 to 31), and
-    // whether it counts.
+    // Where a block's keys are: two block ids, or the block of each lane's key
+    // (lanes 32 to 63 repeat 0 to 31); -1 for none.
     const int32_t *table = a.bt + int64_t(r) * a.bt_cols;
-    const auto row_of = [&](int64_t key0, bool *live) {
-      const int64_t key = key0 + (lane & 31);
-      *live = key < key_end;
-      if (!*live) return 0u;
-      const uint32_t t = uint32_t(key);  // lengths are 32 bits
-      const uint32_t page = a.block_shift >= 0 ? t >> a.block_shift
-                                               : t / uint32_t(a.block_size);
-      const uint32_t pos = t - page * uint32_t(a.block_size);
-      const int32_t id = table[page];
-      if (id < 0 || id >= a.num_blocks) {
-        err = LUMEN_ERR_BLOCK_ID;
-        *live = false;
-        return 0u;
+    const auto find = [&](int64_t key0) {
+      Place p;
+      if constexpr (kAligned) {
+        const auto *ids = CONSTANT_PTR(int32_t, table);
+        p.id[0] = key0 < key_end ? ids[uint32_t(key0) >> a.block_shift] : -1;
+        p.id[1] = key0 + 16 < key_end ? ids[uint32_t(key0 + 16) >> a.block_shift] : -1;
+      } else {
+        const int64_t key = key0 + (lane & 31);
+        p.row = -1;
+        if (key < key_end) p.row = table[uint32_t(key) / uint32_t(a.block_size)];
       }
-      const uint32_t b = uint32_t(id), bs = uint32_t(a.block_size);
-      return a.hnd ? (b * uint32_t(a.heads) + h) * bs + pos
-                   : (b * bs + pos) * uint32_t(a.heads) + h;
+      return p;
     };
-    const auto fetch = [&](int64_t key0, KeyBlock<D> &kb) {
-      bool live;
-      const uint32_t row = row_of(key0, &live);
-      kb.live = uint32_t(__ballot(live));
-      if (kb.live == 0) return;  // row 0 exists where any row does
+    const auto fetch = [&](int64_t key0, const Place &at, KeyBlock<D> &kb) {
+      const uint8_t *kp[2], *vp[8];  // row starts, of the lane's keys
+      uint32_t ko, vo;               // and what the lane reads from there
+      if constexpr (kAligned) {
+        kb.live = 0;
+        int32_t id[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const int64_t left = key_end - key0 - 16 * t;
+          id[t] = at.id[t];
+          const bool ok = id[t] >= 0 && id[t] < a.num_blocks;
+          if (!ok) {
+            if (left > 0) err = LUMEN_ERR_BLOCK_ID;
+            id[t] = 0;
+          } else {
+            kb.live |= (left >= 16 ? 0xffffu : (1u << left) - 1) << (16 * t);
+          }
+        }
+        if (kb.live == 0) return;  // block 0 exists where any does
+        const uint32_t stride = a.hnd ? kRow : uint32_t(a.heads) * kRow;
+        ko = n * stride;
+        vo = 4 * quad * stride;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const uint32_t pos =
+              uint32_t(key0 + 16 * t) & (uint32_t(a.block_size) - 1);
+          const uint64_t row =
+              a.hnd ? (uint64_t(id[t]) * a.heads + h) * a.block_size + pos
+                    : (uint64_t(id[t]) * a.block_size + pos) * a.heads + h;
+          kp[t] = a.k + row * kRow;
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            vp[4 * t + j] = a.v + row * kRow + uint64_t(stride) * j;
+        }
+      } else {
+        const int64_t key = key0 + (lane & 31);
+        const bool in = key < key_end;
+        const bool ok = at.row >= 0 && at.row < a.num_blocks;
+        if (in && !ok) err = LUMEN_ERR_BLOCK_ID;
+        const uint32_t bs = uint32_t(a.block_size), b = uint32_t(at.row);
+        const uint32_t pos = uint32_t(key) % bs;
+        uint32_t row = a.hnd ? (b * uint32_t(a.heads) + h) * bs + pos
+                             : (b * bs + pos) * uint32_t(a.heads) + h;
+        row = ok ? row : 0;
+        kb.live = uint32_t(__ballot(ok));
+        if (kb.live == 0) return;  // row 0 exists where any row does
+        ko = vo = 0;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+          kp[t] = a.k + uint64_t(uint32_t(__shfl(row, 16 * t + n))) * kRow;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          vp[j] = a.v + uint64_t(uint32_t(__shfl(
+                            row, 4 * quad + (j < 4 ? j : 12 + j)))) * kRow;
+      }
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        const uint8_t *p = a.k + uint64_t(uint32_t(__shfl(row, 16 * t + n))) * kRow;
-        const uint32_t *c = reinterpret_cast<const uint32_t *>(p + quad * (D / 8));
+        const uint8_t *c = kp[t] + (ko + quad * (D / 8));
         if constexpr (D == 64) {
           const uint2 x = *reinterpret_cast<const uint2 *>(c);
           kb.k[t][0] = x.x, kb.k[t][1] = x.y;
         } else {
 #pragma unroll
           for (int i = 0; i < kSteps; i += 4) {
-            const uint4 x = *reinterpret_cast<const uint4 *>(c + i);
+            const uint4 x = *reinterpret_cast<const uint4 *>(c + 4 * i);
             kb.k[t][i] = x.x, kb.k[t][i + 1] = x.y;
             kb.k[t][i + 2] = x.z, kb.k[t][i + 3] = x.w;
           }
         }
-        kb.kp[t] = *reinterpret_cast<const uint32_t *>(p + D / 2 + 4 * quad);
+        kb.kp[t] = *reinterpret_cast<const uint32_t *>(kp[t] + (ko + 4 * quad) + D / 2);
       }
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const int key = j < 4 ? 4 * quad + j : 12 + 4 * quad + j;
-        const uint8_t *p = a.v + uint64_t(uint32_t(__shfl(row, key))) * kRow;
+        const uint8_t *c = vp[j] + (vo + n * (kE / 2));
         if constexpr (D == 64) {
-          kb.v[j][0] = *reinterpret_cast<const uint16_t *>(p + 2 * n);
+          kb.v[j][0] = *reinterpret_cast<const uint16_t *>(c);
         } else if constexpr (D == 128) {
-          kb.v[j][0] = *reinterpret_cast<const uint32_t *>(p + 4 * n);
+          kb.v[j][0] = *reinterpret_cast<const uint32_t *>(c);
         } else {
-          const uint2 x = *reinterpret_cast<const uint2 *>(p + 8 * n);
+          const uint2 x = *reinterpret_cast<const uint2 *>(c);
           kb.v[j][0] = x.x, kb.v[j][kE / 8 - 1] = x.y;
         }
-        kb.vp[j] = *reinterpret_cast<const uint32_t *>(p + D / 2 + 4 * (n / 4));
+        kb.vp[j] = *reinterpret_cast<const uint32_t *>(vp[j] + (vo + n / 4 * 4) + D / 2);
       }
     };
     const auto use = [&](KeyBlock<D> &kb) {
@@ -629,7 +697,7 @@ __global__ __launch_bounds__(kDecodeThreads, D == 256 ? 2 : 3) void decode4_kern
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
           half2v x[4];
-          codes4(kb.k[t][i], x);
+          codes4(kb.k[t][i], mask, one, x);
           half8v f;
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
@@ -684,7 +752,8 @@ __global__ __launch_bounds__(kDecodeThreads, D == 256 ? 2 : 3) void decode4_kern
         for (int j = 0; j < 4; ++j) {
           half2v x[4];
           codes4(__builtin_amdgcn_perm(kb.v[2 * j + 1][w / 2], kb.v[2 * j][w / 2],
-                                       w % 2 ? 0x07060302 : 0x05040100), x);
+                                       w % 2 ? 0x07060302 : 0x05040100),
+                 mask, one, x);
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const half2v y = __builtin_elementwise_fma(x[e], A[j], B[j]);
@@ -699,13 +768,26 @@ __global__ __launch_bounds__(kDecodeThreads, D == 256 ? 2 : 3) void decode4_kern
       }
     };
 
-    KeyBlock<D> cur, next;
+    // Two blocks in turn, without copies: one is in flight while the other is
+    // used, and the place of the one after them is looked up.
+    KeyBlock<D> b0, b1;
     int64_t key = key_begin + wave * kBlockKeys;
-    fetch(key, cur);
-    for (; key < key_end; key += kUnitKeys) {
-      fetch(key + kUnitKeys, next);
-      use(cur);
-      cur = next;
+    Place at = find(key);
+    if (key < key_end) {
+      const Place then = find(key + kUnitKeys);
+      fetch(key, at, b0);
+      at = then;
+    }
+    while (key < key_end) {
+      Place then = find(key + 2 * kUnitKeys);
+      if (key + kUnitKeys < key_end) fetch(key + kUnitKeys, at, b1);
+      use(b0);
+      key += kUnitKeys;
+      if (key >= key_end) break;
+      at = find(key + 2 * kUnitKeys);
+      if (key + kUnitKeys < key_end) fetch(key + kUnitKeys, then, b0);
+      use(b1);
+      key += kUnitKeys;
     }
     l = quad_sum(l);
 
@@ -851,6 +933,12 @@ int check_layout(const lumen_kv_layout *l, int32_t layer, Layer *out) {
   out->k = int64_t(layer) * 2 * half;
   out->v = out->k + half;
   return LUMEN_OK;
+}
+
+template <int D>
+void (*decode_kernel(bool bf16, bool aligned))(DecodeArgs) {
+  return bf16 ? (aligned ? decode4_kernel<D, true, true> : decode4_kernel<D, true, false>)
+              : (aligned ? decode4_kernel<D, false, true> : decode4_kernel<D, false, false>);
 }
 
 // Grid and workspace of a decode call on a device of `cus` compute units.
@@ -1063,7 +1151,7 @@ int lumen_attn_decode4(const lumen_kv_layout *layout, int32_t layer,
                d_block_tables,
                bt_cols,
                bs,
-               (bs & (bs - 1)) == 0 ? __builtin_ctz(unsigned(bs)) : -1,
+               __builtin_ctz(unsigned(bs)),
                layout->num_blocks,
                d_lens,
                num_reqs,
@@ -1079,10 +1167,11 @@ int lumen_attn_decode4(const lumen_kv_layout *layout, int32_t layer,
                reinterpret_cast<float *>(static_cast<char *>(d_workspace) +
                                          plan.parts_at)};
   const bool bf = dtype == LUMEN_ATTN_BF16;
+  const bool al = bs >= 16 && (bs & (bs - 1)) == 0;
   void (*kernel)(DecodeArgs) =
-      at.head_dim == 64    ? (bf ? decode4_kernel<64, true> : decode4_kernel<64, false>)
-      : at.head_dim == 128 ? (bf ? decode4_kernel<128, true> : decode4_kernel<128, false>)
-                           : (bf ? decode4_kernel<256, true> : decode4_kernel<256, false>);
+      at.head_dim == 64    ? decode_kernel<64>(bf, al)
+      : at.head_dim == 128 ? decode_kernel<128>(bf, al)
+                           : decode_kernel<256>(bf, al);
   hipLaunchKernelGGL(kernel, dim3(unsigned(plan.workers * plan.heads)),
                      dim3(kDecodeThreads), 0, static_cast<hipStream_t>(stream), a);
   return hipGetLastError() == hipSuccess ? LUMEN_OK : LUMEN_ERR_HIP;

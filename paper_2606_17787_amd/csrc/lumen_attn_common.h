@@ -58,6 +58,22 @@ __device__ __forceinline__ uint4 pack8(const float *x) {
 
 // ------------------------------------------------------------ other parts
 
+// x of lane l ^ kLanes (16 or 32).  Two results that the compiler is told to
+// be of the same operand are taken by it for one, hence the empty asm.
+template <int kLanes>
+__device__ __forceinline__ float swapped(float x) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, x);
+  uint32_t w = u;
+  asm("" : "+v"(w));
+  if constexpr (kLanes == 16) {
+    const auto r = __builtin_amdgcn_permlane16_swap(u, w, false, false);
+    return __builtin_bit_cast(float, (threadIdx.x & 16) ? r[0] : r[1]);
+  } else {
+    const auto r = __builtin_amdgcn_permlane32_swap(u, w, false, false);
+    return __builtin_bit_cast(float, (threadIdx.x & 32) ? r[0] : r[1]);
+  }
+}
+
 // lumen_attn_rows, typed.
 struct Rows {
   uint16_t *base;

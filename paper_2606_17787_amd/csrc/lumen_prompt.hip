@@ -50,15 +50,6 @@ constexpr int kThreads = kWaves * kWave;
 constexpr int kKeys = 64;  // keys of a tile
 constexpr float kSlack = 8.0f;
 
-// The maximum and the sum of a query's scores are spread over lanes l and
-// l + 32.
-__device__ __forceinline__ float other_half(float x) {
-  const uint32_t u = __builtin_bit_cast(uint32_t, x);
-  const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-  // lanes below 32 hold their own in r[0] and the other in r[1]
-  return __builtin_bit_cast(float, (threadIdx.x & 32) ? r[0] : r[1]);
-}
-
 template <int D>
 __device__ __forceinline__ int swizzle_k(int row) {
   return D == 128 ? row & 15 : (row >> 1) & 7;
@@ -304,7 +295,7 @@ __global__ __launch_bounds__(kThreads) void prompt_kernel(PromptArgs a) {
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[t][i]);
-    top = fmaxf(top, other_half(top)) * a.scale_log2;
+    top = fmaxf(top, swapped<32>(top)) * a.scale_log2;
     if (__any(top > m + kSlack)) {
       const float mn = fmaxf(m, top);
       const float c = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
@@ -346,7 +337,7 @@ __global__ __launch_bounds__(kThreads) void prompt_kernel(PromptArgs a) {
       }
   }
   if (!here) return;
-  l += other_half(l);
+  l += swapped<32>(l);
   const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
   uint16_t *out = a.out + ((q0 + tok) * a.q_heads + hq) * D;
 #pragma unroll
