@@ -417,24 +417,35 @@ __device__ __forceinline__ float quad_sum(float x) {
   return x + swapped<32>(x);
 }
 
-// What a wavefront holds of one block of keys before it is used.
-template <int D>
-struct KeyBlock {
-  uint32_t k[2][D / 32], kp[2];              // two tiles of 16 keys: codes, pair
-  uint32_t v[8][D >= 128 ? D / 128 : 1], vp[8];  // eight keys of the lane
-  uint32_t live;                             // keys that count, a bit each
-};
+// Starts a load of kBytes a lane from the lane's address into LDS, at `to` +
+// kBytes * lane (`to` the wavefront's).  It is counted like any load, but the
+// compiler does not know of it: wait_loads<n> waits until at most the last n
+// are still under way, and keeps reads of the LDS behind it.  That, unlike the
+// builtin, lets a read wait for its own block alone.
+template <int kBytes>
+__device__ __forceinline__ void load_to_lds(const void *from, void *to) {
+  const uint32_t at = uint32_t(
+      reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) void *)(to)));
+  if constexpr (kBytes == 16)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+                 :: "s"(at), "v"(from) : "memory");
+  else
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off"
+                 :: "s"(at), "v"(from) : "memory");
+}
+template <int kLeft>
+__device__ __forceinline__ void wait_loads() {
+  asm volatile("s_waitcnt vmcnt(%0)" :: "i"(kLeft) : "memory");
+}
+__device__ __forceinline__ void wait_lds() {
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+}
 
 // A value that is the same in all lanes, in scalar registers.
 __device__ __forceinline__ uint64_t uniform(uint64_t x) {
   return uint64_t(__builtin_amdgcn_readfirstlane(uint32_t(x))) |
          uint64_t(__builtin_amdgcn_readfirstlane(uint32_t(x >> 32))) << 32;
 }
-
-struct Place {
-  int32_t id[2];  // kAligned
-  int32_t row;    // otherwise: the block of the lane's key
-};
 
 #define CONSTANT_PTR(T, p) ((const __attribute__((address_space(4))) T *)(p))
 
@@ -443,7 +454,10 @@ struct Place {
 // 128, whatever their lengths, so a share may start and end inside a request;
 // partial results of a request are joined by the last of its workers to
 // arrive, in a fixed order.  Within a unit each wavefront takes 32 keys and
-// keeps its own running maximum and sums; no LDS is used before the end.
+// keeps its own running maximum and sums.  The rows of its keys come straight
+// into LDS, 16 bytes a lane and each byte once, kStages blocks in turn: what
+// is in flight takes no registers, and no two loads ask for one cache line at
+// the same time, on which the first level waits.
 //
 // One block of 32 keys: scores^T = K Q^T and sums^T = V^T P^T by 16x16x32
 // products of 16-bit floats, queries across (the heads of the group, up to 16).
@@ -458,14 +472,24 @@ struct Place {
 //
 // kAligned: pages are 16 * 2^k tokens, so that a tile of 16 keys lies in one
 // page and its address is the wavefront's, not the lane's: block ids come by
-// scalar loads and the keys' rows from one vector offset.  Other page sizes
-// look each key's row up on a lane of its own and pass it round.
+// scalar loads and the keys' rows from vector offsets that do not change.
+// For other page sizes each key's block id comes into LDS, ahead of its row.
 template <int D, bool kBf16, bool kAligned>
-__global__ __launch_bounds__(kDecodeThreads, D == 256 ? 2 : 3) void decode4_kernel(DecodeArgs a) {
+__global__ __launch_bounds__(kDecodeThreads, 2) void decode4_kernel(DecodeArgs a) {
   constexpr int kRow = D / 2 + 16;
   constexpr int kSteps = D / 32;  // products over head_dim
   constexpr int kE = D / 16;      // elements of V a lane holds of a key
-  __shared__ float lds_o[kDecodeWaves - 1][kE][4 * kWave];
+  constexpr int kStages = D == 256 ? 2 : 3;
+  constexpr int kParts = kRow / 16;                  // 16-byte pieces of a row
+  constexpr int kIssues = 2 * kBlockKeys * kParts / kWave;
+  constexpr int kStage = 2 * kBlockKeys * kRow;      // bytes
+  constexpr int kRing = kStages * kStage;
+  // the wavefronts' rings, and after a request their sums
+  __shared__ __attribute__((aligned(16))) uint8_t ring[kDecodeWaves * kRing];
+  __shared__ int32_t id_ring[kAligned ? 1 : kDecodeWaves * 4 * kWave];
+  static_assert((kDecodeWaves - 1) * kE * 4 * kWave * sizeof(float) <= sizeof(ring),
+                "the sums fit the rings");
+  auto &lds_o = *reinterpret_cast<float(*)[kDecodeWaves - 1][kE][4 * kWave]>(ring);
   __shared__ float lds_m[kDecodeWaves][kQueries], lds_l[kDecodeWaves][kQueries];
   __shared__ uint64_t lds_scan[kDecodeWaves];
   __shared__ uint64_t lds_first;  // of the request that a share starts in
@@ -585,119 +609,110 @@ __global__ __launch_bounds__(kDecodeThreads, D == 256 ? 2 : 3) void decode4_kern
     for (int j = 0; j < kE; ++j) o[j] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
     float m = -INFINITY, l = 0.0f;
 
-    // Where a block's keys are: two block ids, or the block of each lane's key
-    // (lanes 32 to 63 repeat 0 to 31); -1 for none.
+    // ---- the rows of a block into its stage of the ring.  Piece c of the
+    // block is 16 bytes: 32 rows of K, then 32 of V.
     const int32_t *table = a.bt + int64_t(r) * a.bt_cols;
-    const auto find = [&](int64_t key0) {
-      Place p;
-      if constexpr (kAligned) {
-        const auto *ids = CONSTANT_PTR(int32_t, table);
-        p.id[0] = key0 < key_end ? ids[uint32_t(key0) >> a.block_shift] : -1;
-        p.id[1] = key0 + 16 < key_end ? ids[uint32_t(key0 + 16) >> a.block_shift] : -1;
-      } else {
-        const int64_t key = key0 + (lane & 31);
-        p.row = -1;
-        if (key < key_end) p.row = table[uint32_t(key) / uint32_t(a.block_size)];
-      }
-      return p;
+    const uint32_t stride = a.hnd ? kRow : uint32_t(a.heads) * kRow;
+    int64_t offset[kIssues];  // kAligned: from the tile's first row of K
+#pragma unroll
+    for (int i = 0; i < kIssues; ++i) {
+      const int c = i * kWave + lane, row = c / kParts % kBlockKeys;
+      offset[i] = (c >= kBlockKeys * kParts ? a.v - a.k : 0) +
+                  (kAligned ? int64_t(row & 15) * stride : 0) + c % kParts * 16;
+    }
+    // The keys of a block that count, a bit each.
+    const auto in_range = [&](int64_t key0) {
+      const int64_t left = key_end - key0;
+      return left >= 32 ? 0xffffffffu : (1u << left) - 1;
     };
-    const auto fetch = [&](int64_t key0, const Place &at, KeyBlock<D> &kb) {
-      const uint8_t *kp[2], *vp[8];  // row starts, of the lane's keys
-      uint32_t ko, vo;               // and what the lane reads from there
+    const auto ids_of = [&](int64_t key0, int32_t *id) {
+      const auto *ids = CONSTANT_PTR(int32_t, table);
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+        id[t] = key0 + 16 * t < key_end ? ids[uint32_t(key0 + 16 * t) >> a.block_shift]
+                                        : -1;
+    };
+    const auto load_ids = [&](int64_t key0, int slot) {
+      int64_t key = key0 + (lane & 31);
+      key = key < key_end ? key : key_end - 1;
+      load_to_lds<4>(table + uint32_t(key) / uint32_t(a.block_size),
+                     &id_ring[(wave * 4 + (slot & 3)) * kWave]);
+    };
+    // Starts a block's loads and returns the bits of its keys that count.
+    const auto fetch = [&](int64_t key0, const int32_t *id, int slot, int stage) {
+      uint32_t live = in_range(key0);
+      uint8_t *to = ring + wave * kRing + stage * kStage;
       if constexpr (kAligned) {
-        kb.live = 0;
-        int32_t id[2];
+        const uint8_t *base[2];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-          const int64_t left = key_end - key0 - 16 * t;
-          id[t] = at.id[t];
+          // a tile out of range repeats some row that exists
           const bool ok = id[t] >= 0 && id[t] < a.num_blocks;
-          if (!ok) {
-            if (left > 0) err = LUMEN_ERR_BLOCK_ID;
-            id[t] = 0;
-          } else {
-            kb.live |= (left >= 16 ? 0xffffu : (1u << left) - 1) << (16 * t);
+          if (!ok && (live >> (16 * t) & 0xffff)) {
+            err = LUMEN_ERR_BLOCK_ID;
+            live &= ~(0xffffu << (16 * t));
           }
-        }
-        if (kb.live == 0) return;  // block 0 exists where any does
-        const uint32_t stride = a.hnd ? kRow : uint32_t(a.heads) * kRow;
-        ko = n * stride;
-        vo = 4 * quad * stride;
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
+          const uint64_t block = ok ? uint32_t(id[t]) : 0;
           const uint32_t pos =
               uint32_t(key0 + 16 * t) & (uint32_t(a.block_size) - 1);
           const uint64_t row =
-              a.hnd ? (uint64_t(id[t]) * a.heads + h) * a.block_size + pos
-                    : (uint64_t(id[t]) * a.block_size + pos) * a.heads + h;
-          kp[t] = a.k + row * kRow;
+              a.hnd ? (block * a.heads + h) * a.block_size + pos
+                    : (block * a.block_size + pos) * a.heads + h;
+          base[t] = a.k + row * kRow;
+        }
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
-            vp[4 * t + j] = a.v + row * kRow + uint64_t(stride) * j;
+        for (int i = 0; i < kIssues; ++i) {
+          const int row = (i * kWave + lane) / kParts % kBlockKeys;
+          load_to_lds<16>((row < 16 ? base[0] : base[1]) + offset[i],
+                          to + i * kWave * 16);
         }
       } else {
-        const int64_t key = key0 + (lane & 31);
-        const bool in = key < key_end;
-        const bool ok = at.row >= 0 && at.row < a.num_blocks;
+        const int32_t block = id_ring[(wave * 4 + (slot & 3)) * kWave + lane];
+        const bool in = live >> (lane & 31) & 1;
+        const bool ok = block >= 0 && block < a.num_blocks;
         if (in && !ok) err = LUMEN_ERR_BLOCK_ID;
-        const uint32_t bs = uint32_t(a.block_size), b = uint32_t(at.row);
-        const uint32_t pos = uint32_t(key) % bs;
-        uint32_t row = a.hnd ? (b * uint32_t(a.heads) + h) * bs + pos
-                             : (b * bs + pos) * uint32_t(a.heads) + h;
-        row = ok ? row : 0;
-        kb.live = uint32_t(__ballot(ok));
-        if (kb.live == 0) return;  // row 0 exists where any row does
-        ko = vo = 0;
+        const uint32_t bs = uint32_t(a.block_size), id = ok ? uint32_t(block) : 0u;
+        const uint32_t pos = uint32_t(key0 + (lane & 31)) % bs;
+        const uint32_t row = a.hnd ? (id * uint32_t(a.heads) + h) * bs + pos
+                                   : (id * bs + pos) * uint32_t(a.heads) + h;
+        live = uint32_t(__ballot(in && ok));
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
-          kp[t] = a.k + uint64_t(uint32_t(__shfl(row, 16 * t + n))) * kRow;
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          vp[j] = a.v + uint64_t(uint32_t(__shfl(
-                            row, 4 * quad + (j < 4 ? j : 12 + j)))) * kRow;
-      }
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const uint8_t *c = kp[t] + (ko + quad * (D / 8));
-        if constexpr (D == 64) {
-          const uint2 x = *reinterpret_cast<const uint2 *>(c);
-          kb.k[t][0] = x.x, kb.k[t][1] = x.y;
-        } else {
-#pragma unroll
-          for (int i = 0; i < kSteps; i += 4) {
-            const uint4 x = *reinterpret_cast<const uint4 *>(c + 4 * i);
-            kb.k[t][i] = x.x, kb.k[t][i + 1] = x.y;
-            kb.k[t][i + 2] = x.z, kb.k[t][i + 3] = x.w;
-          }
+        for (int i = 0; i < kIssues; ++i) {
+          const uint32_t mine =
+              uint32_t(__shfl(row, (i * kWave + lane) / kParts % kBlockKeys));
+          load_to_lds<16>(a.k + uint64_t(mine) * kRow + offset[i],
+                          to + i * kWave * 16);
         }
-        kb.kp[t] = *reinterpret_cast<const uint32_t *>(kp[t] + (ko + 4 * quad) + D / 2);
       }
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const uint8_t *c = vp[j] + (vo + n * (kE / 2));
-        if constexpr (D == 64) {
-          kb.v[j][0] = *reinterpret_cast<const uint16_t *>(c);
-        } else if constexpr (D == 128) {
-          kb.v[j][0] = *reinterpret_cast<const uint32_t *>(c);
-        } else {
-          const uint2 x = *reinterpret_cast<const uint2 *>(c);
-          kb.v[j][0] = x.x, kb.v[j][kE / 8 - 1] = x.y;
-        }
-        kb.vp[j] = *reinterpret_cast<const uint32_t *>(vp[j] + (vo + n / 4 * 4) + D / 2);
-      }
+      return live;
     };
-    const auto use = [&](KeyBlock<D> &kb) {
-      if (kb.live == 0) return;
+    const auto use = [&](const uint8_t *from, uint32_t live) {
+      if (live == 0) return;
+      const uint8_t *kr = from, *vr = from + kBlockKeys * kRow;
       float4v s[2];
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         s[t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
-        const half2v pair = as_half2(kb.kp[t]);
+        const uint8_t *row = kr + (16 * t + n) * kRow;
+        const half2v pair =
+            as_half2(*reinterpret_cast<const uint32_t *>(row + D / 2 + 4 * quad));
+        uint32_t codes[kSteps];
+        row += quad * (D / 8);
+        if constexpr (D == 64) {
+          const uint2 x = *reinterpret_cast<const uint2 *>(row);
+          codes[0] = x.x, codes[1] = x.y;
+        } else {
+#pragma unroll
+          for (int i = 0; i < kSteps; i += 4) {
+            const uint4 x = *reinterpret_cast<const uint4 *>(row + 4 * i);
+            codes[i] = x.x, codes[i + 1] = x.y, codes[i + 2] = x.z, codes[i + 3] = x.w;
+          }
+        }
         const half2v A = {pair[0], pair[0]}, B = {pair[1], pair[1]};
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
           half2v x[4];
-          codes4(kb.k[t][i], mask, one, x);
+          codes4(codes[i], mask, one, x);
           half8v f;
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
@@ -708,14 +723,29 @@ __global__ __launch_bounds__(kDecodeThreads, D == 256 ? 2 : 3) void decode4_kern
           s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f, q[i], s[t], 0, 0, 0);
         }
       }
-      if (kb.live != 0xffffffffu) {
+      // V: the lane's elements of 8 keys
+      uint32_t vc[8][kE >= 8 ? kE / 8 : 1], vp[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const uint8_t *row = vr + (4 * quad + (j < 4 ? j : 12 + j)) * kRow;
+        vp[j] = *reinterpret_cast<const uint32_t *>(row + D / 2 + n / 4 * 4);
+        row += n * (kE / 2);
+        if constexpr (D == 64) {
+          vc[j][0] = *reinterpret_cast<const uint16_t *>(row);
+        } else if constexpr (D == 128) {
+          vc[j][0] = *reinterpret_cast<const uint32_t *>(row);
+        } else {
+          const uint2 x = *reinterpret_cast<const uint2 *>(row);
+          vc[j][0] = x.x, vc[j][kE / 8 - 1] = x.y;
+        }
+      }
+      if (live != 0xffffffffu) {
         // a key left out has no score, and no value either: its pair may be NaN
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const int key = j < 4 ? 4 * quad + j : 12 + 4 * quad + j;
-          const bool in = (kb.live >> key) & 1;
+          const bool in = (live >> (4 * quad + (j < 4 ? j : 12 + j))) & 1;
           if (!in) s[j / 4][j % 4] = -INFINITY;
-          if (!in) kb.vp[j] = 0;
+          if (!in) vp[j] = 0;
         }
       }
       float top = -INFINITY;
@@ -742,8 +772,8 @@ __global__ __launch_bounds__(kDecodeThreads, D == 256 ? 2 : 3) void decode4_kern
       half2v A[4], B[4];  // of keys 2j and 2j + 1 of the lane
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        A[j] = as_half2(__builtin_amdgcn_perm(kb.vp[2 * j + 1], kb.vp[2 * j], 0x05040100));
-        B[j] = as_half2(__builtin_amdgcn_perm(kb.vp[2 * j + 1], kb.vp[2 * j], 0x07060302));
+        A[j] = as_half2(__builtin_amdgcn_perm(vp[2 * j + 1], vp[2 * j], 0x05040100));
+        B[j] = as_half2(__builtin_amdgcn_perm(vp[2 * j + 1], vp[2 * j], 0x07060302));
       }
 #pragma unroll
       for (int w = 0; w < kE / 4; ++w) {  // four elements at a time
@@ -751,7 +781,7 @@ __global__ __launch_bounds__(kDecodeThreads, D == 256 ? 2 : 3) void decode4_kern
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           half2v x[4];
-          codes4(__builtin_amdgcn_perm(kb.v[2 * j + 1][w / 2], kb.v[2 * j][w / 2],
+          codes4(__builtin_amdgcn_perm(vc[2 * j + 1][w / 2], vc[2 * j][w / 2],
                                        w % 2 ? 0x07060302 : 0x05040100),
                  mask, one, x);
 #pragma unroll
@@ -768,29 +798,65 @@ __global__ __launch_bounds__(kDecodeThreads, D == 256 ? 2 : 3) void decode4_kern
       }
     };
 
-    // Two blocks in turn, without copies: one is in flight while the other is
-    // used, and the place of the one after them is looked up.
-    KeyBlock<D> b0, b1;
-    int64_t key = key_begin + wave * kBlockKeys;
-    Place at = find(key);
-    if (key < key_end) {
-      const Place then = find(key + kUnitKeys);
-      fetch(key, at, b0);
-      at = then;
+    // Blocks of this wavefront, kStages - 1 of them in flight while one is used.
+    const int64_t key0 = key_begin + wave * kBlockKeys;
+    const int blocks =
+        a.num_blocks > 0 && key0 < key_end
+            ? int((key_end - key0 + kUnitKeys - 1) / kUnitKeys)
+            : 0;
+    if (a.num_blocks == 0 && key_begin < key_end) err = LUMEN_ERR_BLOCK_ID;
+    const auto key_of = [&](int i) { return key0 + int64_t(i) * kUnitKeys; };
+    uint32_t live[kStages];
+    int32_t id[2] = {-1, -1};
+    if constexpr (kAligned) {
+      if (blocks > 0) ids_of(key0, id);
+    } else {
+      if (blocks > 0) load_ids(key0, 0);
+      if (blocks > 1) load_ids(key_of(1), 1);
+      if (blocks > 2 && kStages > 2) load_ids(key_of(2), 2);
+      wait_loads<0>();
     }
-    while (key < key_end) {
-      Place then = find(key + 2 * kUnitKeys);
-      if (key + kUnitKeys < key_end) fetch(key + kUnitKeys, at, b1);
-      use(b0);
-      key += kUnitKeys;
-      if (key >= key_end) break;
-      at = find(key + 2 * kUnitKeys);
-      if (key + kUnitKeys < key_end) fetch(key + kUnitKeys, then, b0);
-      use(b1);
-      key += kUnitKeys;
+    int started = 0;  // blocks, and their stage of the ring
+    const auto start = [&](int stage) {
+      if (started < blocks) {
+        int32_t then[2] = {-1, -1};
+        if constexpr (kAligned) {
+          if (started + 1 < blocks) ids_of(key_of(started + 1), then);
+        }
+        live[stage] = fetch(key_of(started), id, started, stage);
+        id[0] = then[0], id[1] = then[1];
+        // the ids of the block that the next start but kStages - 1 fetches
+        if constexpr (!kAligned) {
+          int64_t ahead = key_of(started + kStages);
+          load_ids(ahead < key_end ? ahead : key_begin, started + kStages);
+        }
+      }
+      ++started;
+    };
+    constexpr int kLoads = kIssues + (kAligned ? 0 : 1);  // of one start
+#pragma unroll
+    for (int i = 0; i < kStages - 1; ++i) start(i);
+    for (int i = 0; i < blocks; i += kStages) {
+#pragma unroll
+      for (int t = 0; t < kStages; ++t) {
+        if (i + t < blocks) {
+          wait_lds();  // the stage's last reader is done
+          start((t + kStages - 1) % kStages);
+          const int behind = blocks - 1 - (i + t);  // started after this one
+          if (behind >= kStages - 1)
+            wait_loads<(kStages - 1) * kLoads>();
+          else if (kStages > 2 && behind == 1)
+            wait_loads<kLoads>();
+          else
+            wait_loads<0>();
+          use(ring + wave * kRing + t * kStage, live[t]);
+        }
+      }
     }
+    wait_loads<0>();
     l = quad_sum(l);
 
+    __syncthreads();  // the rings take the sums
     // Joins the wavefronts' results into wavefront 0's o, m and l.
     const auto join = [&]() {
       if (quad == 0) lds_m[wave][n] = m;
@@ -957,10 +1023,10 @@ DecodePlan decode_plan(const lumen_kv_layout *l, int32_t head_dim,
   const int group = num_q_heads / l->num_kv_heads;
   DecodePlan p;
   p.heads = l->num_kv_heads * ((group + kQueries - 1) / kQueries);
-  // as many workgroups as are resident at once, three a CU; a multiple of 8
+  // as many workgroups as are resident at once, two a CU; a multiple of 8
   // for each head puts all heads of a share on one XCD, whose L2 then serves
   // the lines that token-major rows of different heads have in common
-  const int all = (cus < kMaxUnits ? cus : kMaxUnits) * 3;
+  const int all = (cus < kMaxUnits ? cus : kMaxUnits) * 2;
   p.workers = all / p.heads;
   if (p.workers > 8) p.workers &= ~7;
   if (p.workers < 1) p.workers = 1;
