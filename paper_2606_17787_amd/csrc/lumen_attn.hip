@@ -359,35 +359,36 @@ struct DecodeArgs {
   const uint8_t *k, *v;  // of the layer
   const int32_t *bt;
   int32_t bt_cols, block_size;
-  int32_t block_shift;  // log2 of block_size where that is whole
+  int32_t page_shift;  // log2 of block_size, or -1
   int64_t num_blocks;
   const int32_t *lens;
   int32_t num_reqs, heads, group;
-  bool hnd;
+  bool hnd, stream;
   Rows q;
   float scale_log2;  // scale * log2(e)
   uint16_t *out;
   int32_t *status;
-  int32_t workers;  // workgroups of one head
-  uint32_t *arrived;  // [num_reqs][heads of the grid]
-  float *parts;       // [workers * heads of the grid][2][part_floats(D)]
+  int32_t wg_heads, wg_blocks;  // heads and key blocks of a workgroup
+  int32_t workers;              // workgroups of one set of heads
+  int2 *spans;   // [num_reqs] the workers of a request's first and last unit
+  float *parts;  // [sets of heads][workers][2][wg_heads][part_floats(D)]
 };
 
 typedef _Float16 half2v __attribute__((ext_vector_type(2)));
 typedef _Float16 half8v __attribute__((ext_vector_type(8)));
 typedef float float4v __attribute__((ext_vector_type(4)));
 
-constexpr int kDecodeWaves = 4;
+constexpr int kDecodeWaves = 8;
 constexpr int kDecodeThreads = kDecodeWaves * kWave;
-constexpr int kBlockKeys = 32;                         // keys a wavefront takes at a time
-constexpr int kUnitKeys = kBlockKeys * kDecodeWaves;   // and its workgroup
-constexpr int kQueries = 16;                           // columns of a product
+constexpr int kBlockKeys = 32;  // keys a wavefront takes at a time
+constexpr int kUnitBlocks = 4;  // a unit of work, in the workgroup's blocks
+constexpr int kQueries = 16;    // columns of a product
 // Weights are 2^(s - m + kBias) with s - m at most kRise: within a 16-bit
 // float up to 2^14, and down to 2^-38 of the largest before they vanish.
 constexpr float kRise = 8.0f, kBias = 6.0f;
 
-// Floats of one partial result: D * kQueries sums, then a maximum and a sum
-// for each query.
+// Floats of one partial result: kQueries rows of D sums, then a maximum and a
+// sum for each.
 constexpr int part_floats(int D) { return D * kQueries + 2 * kQueries; }
 
 __device__ __forceinline__ half2v as_half2(uint32_t x) {
@@ -418,15 +419,18 @@ __device__ __forceinline__ float quad_sum(float x) {
 }
 
 // Starts a load of kBytes a lane from the lane's address into LDS, at `to` +
-// kBytes * lane (`to` the wavefront's).  It is counted like any load, but the
+// kBytes * lane (`to` the wavefront's; kStream: not to be kept in caches).  It is counted like any load, but the
 // compiler does not know of it: wait_loads<n> waits until at most the last n
 // are still under way, and keeps reads of the LDS behind it.  That, unlike the
 // builtin, lets a read wait for its own block alone.
-template <int kBytes>
+template <int kBytes, bool kStream>
 __device__ __forceinline__ void load_to_lds(const void *from, void *to) {
-  const uint32_t at = uint32_t(
-      reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) void *)(to)));
-  if constexpr (kBytes == 16)
+  const uint32_t at = __builtin_amdgcn_readfirstlane(uint32_t(
+      reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) void *)(to))));
+  if constexpr (kBytes == 16 && kStream)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt"
+                 :: "s"(at), "v"(from) : "memory");
+  else if constexpr (kBytes == 16)
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
                  :: "s"(at), "v"(from) : "memory");
   else
@@ -437,8 +441,9 @@ template <int kLeft>
 __device__ __forceinline__ void wait_loads() {
   asm volatile("s_waitcnt vmcnt(%0)" :: "i"(kLeft) : "memory");
 }
-__device__ __forceinline__ void wait_lds() {
-  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+// A barrier after the wavefront's own LDS reads, with loads under way.
+__device__ __forceinline__ void lds_barrier() {
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
 // A value that is the same in all lanes, in scalar registers.
@@ -447,63 +452,65 @@ __device__ __forceinline__ uint64_t uniform(uint64_t x) {
          uint64_t(__builtin_amdgcn_readfirstlane(uint32_t(x >> 32))) << 32;
 }
 
-#define CONSTANT_PTR(T, p) ((const __attribute__((address_space(4))) T *)(p))
-
 // Decode attention, bound by the cache's bytes: D/2 + 16 a row, read once.
-// Every worker (workgroup) takes an equal share of the requests' key units of
-// 128, whatever their lengths, so a share may start and end inside a request;
-// partial results of a request are joined by the last of its workers to
-// arrive, in a fixed order.  Within a unit each wavefront takes 32 keys and
-// keeps its own running maximum and sums.  The rows of its keys come straight
-// into LDS, 16 bytes a lane and each byte once, kStages blocks in turn: what
-// is in flight takes no registers, and no two loads ask for one cache line at
-// the same time, on which the first level waits.
+//
+// Work.  A workgroup takes wg_heads KV heads, those that lie side by side in a
+// token-major page, times wg_blocks blocks of 32 keys: one head and one block
+// a wavefront.  A worker, one a CU, takes an equal share of the requests' units
+// of kUnitBlocks such steps, whatever the requests' lengths, so a share may
+// start and end inside a request; its partial results go to d_workspace and
+// decode4_join_kernel puts them together in a fixed order.
+//
+// Loads.  The rows of a step come straight into LDS, 16 bytes a lane in the
+// order of their addresses, kStages steps in turn: what is in flight takes no
+// registers, and each cache line is asked for once (a wavefront that reads its
+// own head's 80 bytes out of each 640 makes the first-level cache fetch 1.5
+// lines for 80 bytes: 2.2 TB/s).  Block ids come the same way, kStages steps
+// before the rows they lead to.
 //
 // One block of 32 keys: scores^T = K Q^T and sums^T = V^T P^T by 16x16x32
 // products of 16-bit floats, queries across (the heads of the group, up to 16).
-// A lane reads its key's codes with one load and holds them in the product's
-// order at once, because the sum over head_dim may run in any order: lanes l /
-// 16 take the four quarters of the row, each with one pair (A, B).  The scores
-// come out as the weights' operand goes in when the keys are taken in the same
-// order again, so the weights never leave their lanes.  For V a lane holds D/16
-// consecutive elements of 8 keys, all of one quarter.  Values are exact: code
-// and pair give the stored value by one fused multiply-add that rounds as the
-// format says.
-//
-// kAligned: pages are 16 * 2^k tokens, so that a tile of 16 keys lies in one
-// page and its address is the wavefront's, not the lane's: block ids come by
-// scalar loads and the keys' rows from vector offsets that do not change.
-// For other page sizes each key's block id comes into LDS, ahead of its row.
-template <int D, bool kBf16, bool kAligned>
+// A lane reads its key's codes with one LDS load and holds them in the
+// product's order at once, because the sum over head_dim may run in any order:
+// lanes l / 16 take the four quarters of the row, each with one pair (A, B).
+// The scores come out as the weights' operand goes in when the keys are taken
+// in the same order again, so the weights never leave their lanes.  For V a
+// lane holds D/16 consecutive elements of 8 keys, all of one quarter.  Values
+// are exact: code and pair give the stored value by one fused multiply-add that
+// rounds as the format says.
+template <int D, bool kBf16>
 __global__ __launch_bounds__(kDecodeThreads, 2) void decode4_kernel(DecodeArgs a) {
   constexpr int kRow = D / 2 + 16;
   constexpr int kSteps = D / 32;  // products over head_dim
   constexpr int kE = D / 16;      // elements of V a lane holds of a key
-  constexpr int kStages = D == 256 ? 2 : 3;
-  constexpr int kParts = kRow / 16;                  // 16-byte pieces of a row
+  constexpr int kStages = D == 64 ? 4 : D == 128 ? 3 : 2;
+  constexpr int kParts = kRow / 16;  // 16-byte pieces of a row
   constexpr int kIssues = 2 * kBlockKeys * kParts / kWave;
-  constexpr int kStage = 2 * kBlockKeys * kRow;      // bytes
-  constexpr int kRing = kStages * kStage;
-  // the wavefronts' rings, and after a request their sums
-  __shared__ __attribute__((aligned(16))) uint8_t ring[kDecodeWaves * kRing];
-  __shared__ int32_t id_ring[kAligned ? 1 : kDecodeWaves * 4 * kWave];
-  static_assert((kDecodeWaves - 1) * kE * 4 * kWave * sizeof(float) <= sizeof(ring),
-                "the sums fit the rings");
-  auto &lds_o = *reinterpret_cast<float(*)[kDecodeWaves - 1][kE][4 * kWave]>(ring);
+  constexpr int kStage = kDecodeWaves * 2 * kBlockKeys * kRow;  // bytes
+  constexpr int kSlots = 8;  // of the block ids' ring
+  static_assert(kSlots > kStages, "ids come kStages steps ahead");
+  // the ring, and after a request the wavefronts' sums
+  __shared__ __attribute__((aligned(16))) uint8_t ring[kStages * kStage];
+  __shared__ int32_t id_ring[kSlots][kDecodeWaves * kBlockKeys];
   __shared__ float lds_m[kDecodeWaves][kQueries], lds_l[kDecodeWaves][kQueries];
   __shared__ uint64_t lds_scan[kDecodeWaves];
   __shared__ uint64_t lds_first;  // of the request that a share starts in
   __shared__ int lds_req;
-  __shared__ uint32_t lds_last;
+  static_assert(kDecodeWaves * kE * 4 * kWave * sizeof(float) <= sizeof(ring),
+                "the sums fit the ring");
+  auto &lds_o = *reinterpret_cast<float(*)[kDecodeWaves][kE][4 * kWave]>(ring);
 
   const int tid = threadIdx.x, lane = tid & (kWave - 1);
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int n = lane & 15, quad = lane >> 4;
-  const int worker = blockIdx.x % a.workers, hg = blockIdx.x / a.workers;
+  const int worker = blockIdx.x % a.workers, set = blockIdx.x / a.workers;
   const int tiles = (a.group + kQueries - 1) / kQueries;
-  const int h = hg / tiles, g0 = hg % tiles * kQueries;
+  const int h0 = set / tiles * a.wg_heads, g0 = set % tiles * kQueries;
   const int rows = a.group - g0 < kQueries ? a.group - g0 : kQueries;
-  const int num_hg = a.heads * tiles;
+  const int hi = wave % a.wg_heads, kbi = wave / a.wg_heads;
+  const bool active = kbi < a.wg_blocks;
+  const int step_keys = kBlockKeys * a.wg_blocks;
+  const int unit_keys = step_keys * kUnitBlocks;
   int err = LUMEN_OK;
   uint32_t mask, one;  // not to be folded into literals again
   asm("s_mov_b32 %0, %1" : "=s"(mask) : "i"(kCodeMask));
@@ -516,8 +523,7 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void decode4_kernel(DecodeArgs a
     return len < 0 ? int64_t(0) : len < cap ? len : cap;
   };
   const auto units_of = [&](int64_t len) {
-    return len <= kUnitKeys ? uint64_t(1)
-                            : uint64_t(len + kUnitKeys - 1) / kUnitKeys;
+    return len <= unit_keys ? 1u : uint32_t(len + unit_keys - 1) / uint32_t(unit_keys);
   };
   const int per = (a.num_reqs + kDecodeThreads - 1) / kDecodeThreads;
   const int ra = tid * per < a.num_reqs ? tid * per : a.num_reqs;
@@ -558,8 +564,29 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void decode4_kernel(DecodeArgs a
   __syncthreads();
   int r = __builtin_amdgcn_readfirstlane(lds_req);
   uint64_t first = uniform(lds_first);  // first unit of request r
-  const auto share_of = [&](uint64_t unit) {
-    return int(((unit + 1) * shares + total - 1) / total) - 1;
+
+  // ---- the pieces of a step that this lane loads: 16 bytes c of the rows of K,
+  // then of V, each (token, head, part) in the order of a token-major page
+  const uint64_t page_bytes = uint64_t(a.block_size) * a.heads * kRow;
+  const uint32_t slot_bytes = (a.hnd ? 1 : a.heads) * kRow;
+  int tok[kIssues];
+  int64_t offset[kIssues];
+#pragma unroll
+  for (int i = 0; i < kIssues; ++i) {
+    const int half = step_keys * a.wg_heads * kParts;
+    int c = i * kDecodeThreads + tid;
+    const bool is_v = c >= half;
+    c = is_v ? c - half : c;
+    c = c < half ? c : half - 1;  // lanes past the step's end repeat a piece
+    const int row = c / kParts, t = row / a.wg_heads;
+    tok[i] = t;
+    offset[i] = (is_v ? a.v - a.k : 0) +
+                int64_t(a.hnd ? h0 * a.block_size : h0 + row - t * a.wg_heads) * kRow +
+                c % kParts * 16;
+  }
+  const bool wide = a.page_shift >= 4;  // tiles of 16 keys share a block id
+  const auto page_of = [&](uint32_t key) {
+    return a.page_shift >= 0 ? key >> a.page_shift : key / uint32_t(a.block_size);
   };
 
   uint64_t u = u0;
@@ -567,18 +594,18 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void decode4_kernel(DecodeArgs a
     const int64_t len = length(r);
     const uint64_t units = units_of(len);
     const uint64_t stop = first + units < u1 ? first + units : u1;
-    const int64_t key_end =
-        int64_t(stop - first) * kUnitKeys < len ? int64_t(stop - first) * kUnitKeys : len;
-    const int64_t key_begin = int64_t(u - first) * kUnitKeys;
+    const int64_t end = int64_t(stop - first) * unit_keys;
+    const uint32_t key_end = uint32_t(end < len ? end : len);
+    const uint32_t key_begin = uint32_t(u - first) * uint32_t(unit_keys);
 
     // ---- Q: 16-bit floats under a power of two of the row's own, so that
     // bf16 and fp16 keep all their bits whatever their range
     half8v q[kSteps];
     float cq;
     {
-      const uint16_t *p = a.q.base + int64_t(r) * a.q.token +
-                          int64_t(h * a.group + g0 + (n < rows ? n : 0)) * a.q.head +
-                          quad * (D / 4);
+      const int row = (h0 + hi) * a.group + g0 + (n < rows ? n : 0);
+      const uint16_t *p =
+          a.q.base + int64_t(r) * a.q.token + row * a.q.head + quad * (D / 4);
       uint4 raw[kSteps];
       float big = 0.0f, x[8];
 #pragma unroll
@@ -609,91 +636,52 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void decode4_kernel(DecodeArgs a
     for (int j = 0; j < kE; ++j) o[j] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
     float m = -INFINITY, l = 0.0f;
 
-    // ---- the rows of a block into its stage of the ring.  Piece c of the
-    // block is 16 bytes: 32 rows of K, then 32 of V.
     const int32_t *table = a.bt + int64_t(r) * a.bt_cols;
-    const uint32_t stride = a.hnd ? kRow : uint32_t(a.heads) * kRow;
-    int64_t offset[kIssues];  // kAligned: from the tile's first row of K
-#pragma unroll
-    for (int i = 0; i < kIssues; ++i) {
-      const int c = i * kWave + lane, row = c / kParts % kBlockKeys;
-      offset[i] = (c >= kBlockKeys * kParts ? a.v - a.k : 0) +
-                  (kAligned ? int64_t(row & 15) * stride : 0) + c % kParts * 16;
-    }
-    // The keys of a block that count, a bit each.
-    const auto in_range = [&](int64_t key0) {
-      const int64_t left = key_end - key0;
-      return left >= 32 ? 0xffffffffu : (1u << left) - 1;
-    };
-    const auto ids_of = [&](int64_t key0, int32_t *id) {
-      const auto *ids = CONSTANT_PTR(int32_t, table);
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-        id[t] = key0 + 16 * t < key_end ? ids[uint32_t(key0 + 16 * t) >> a.block_shift]
-                                        : -1;
-    };
-    const auto load_ids = [&](int64_t key0, int slot) {
-      int64_t key = key0 + (lane & 31);
+    const auto key_of = [&](int i) { return key_begin + uint32_t(i) * step_keys; };
+    // ids of a step's tiles (or keys); past the end those of its last key
+    const auto load_ids = [&](int i) {
+      uint32_t key = key_of(i) + (tid % (kDecodeWaves * kBlockKeys) << (wide ? 4 : 0));
       key = key < key_end ? key : key_end - 1;
-      load_to_lds<4>(table + uint32_t(key) / uint32_t(a.block_size),
-                     &id_ring[(wave * 4 + (slot & 3)) * kWave]);
+      load_to_lds<4, false>(table + page_of(key),
+                            &id_ring[i % kSlots][wave % 4 * kWave]);
     };
-    // Starts a block's loads and returns the bits of its keys that count.
-    const auto fetch = [&](int64_t key0, const int32_t *id, int slot, int stage) {
-      uint32_t live = in_range(key0);
-      uint8_t *to = ring + wave * kRing + stage * kStage;
-      if constexpr (kAligned) {
-        const uint8_t *base[2];
+    const auto load_rows = [&](int i, int stage) {
+      uint8_t *to = ring + stage * kStage + wave * kWave * 16;
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          // a tile out of range repeats some row that exists
-          const bool ok = id[t] >= 0 && id[t] < a.num_blocks;
-          if (!ok && (live >> (16 * t) & 0xffff)) {
-            err = LUMEN_ERR_BLOCK_ID;
-            live &= ~(0xffffu << (16 * t));
-          }
-          const uint64_t block = ok ? uint32_t(id[t]) : 0;
-          const uint32_t pos =
-              uint32_t(key0 + 16 * t) & (uint32_t(a.block_size) - 1);
-          const uint64_t row =
-              a.hnd ? (block * a.heads + h) * a.block_size + pos
-                    : (block * a.block_size + pos) * a.heads + h;
-          base[t] = a.k + row * kRow;
-        }
-#pragma unroll
-        for (int i = 0; i < kIssues; ++i) {
-          const int row = (i * kWave + lane) / kParts % kBlockKeys;
-          load_to_lds<16>((row < 16 ? base[0] : base[1]) + offset[i],
-                          to + i * kWave * 16);
-        }
-      } else {
-        const int32_t block = id_ring[(wave * 4 + (slot & 3)) * kWave + lane];
-        const bool in = live >> (lane & 31) & 1;
-        const bool ok = block >= 0 && block < a.num_blocks;
-        if (in && !ok) err = LUMEN_ERR_BLOCK_ID;
-        const uint32_t bs = uint32_t(a.block_size), id = ok ? uint32_t(block) : 0u;
-        const uint32_t pos = uint32_t(key0 + (lane & 31)) % bs;
-        const uint32_t row = a.hnd ? (id * uint32_t(a.heads) + h) * bs + pos
-                                   : (id * bs + pos) * uint32_t(a.heads) + h;
-        live = uint32_t(__ballot(in && ok));
-#pragma unroll
-        for (int i = 0; i < kIssues; ++i) {
-          const uint32_t mine =
-              uint32_t(__shfl(row, (i * kWave + lane) / kParts % kBlockKeys));
-          load_to_lds<16>(a.k + uint64_t(mine) * kRow + offset[i],
-                          to + i * kWave * 16);
-        }
+      for (int c = 0; c < kIssues; ++c) {
+        int32_t id = id_ring[i % kSlots][tok[c] >> (wide ? 4 : 0)];
+        if (id < 0 || id >= a.num_blocks) id = 0;  // some block: the key is left out
+        const uint32_t key = key_of(i) + tok[c];
+        const uint32_t pos = a.page_shift >= 0 ? key & (uint32_t(a.block_size) - 1)
+                                               : key % uint32_t(a.block_size);
+        const uint8_t *from =
+            a.k + uint32_t(id) * page_bytes + uint64_t(pos) * slot_bytes + offset[c];
+        if (a.stream)
+          load_to_lds<16, true>(from, to + c * kDecodeThreads * 16);
+        else
+          load_to_lds<16, false>(from, to + c * kDecodeThreads * 16);
       }
-      return live;
     };
-    const auto use = [&](const uint8_t *from, uint32_t live) {
+    // The wavefront's keys of a step that count, a bit each.
+    const auto live_of = [&](int i) {
+      const int mykey = kbi * kBlockKeys + (lane & 31);
+      const int32_t id = active ? id_ring[i % kSlots][mykey >> (wide ? 4 : 0)] : 0;
+      const bool in = active && key_of(i) + mykey < key_end;
+      const bool ok = id >= 0 && id < a.num_blocks;
+      if (in && !ok) err = LUMEN_ERR_BLOCK_ID;
+      return uint32_t(__ballot(in && ok));
+    };
+    const auto use = [&](const uint8_t *stage, uint32_t live) {
       if (live == 0) return;
-      const uint8_t *kr = from, *vr = from + kBlockKeys * kRow;
+      // rows of the wavefront's block: (key, head)
+      const uint32_t key_bytes = a.wg_heads * kRow;
+      const uint8_t *kr = stage + (kbi * kBlockKeys * a.wg_heads + hi) * kRow;
+      const uint8_t *vr = kr + step_keys * key_bytes;
       float4v s[2];
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         s[t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
-        const uint8_t *row = kr + (16 * t + n) * kRow;
+        const uint8_t *row = kr + (16 * t + n) * key_bytes;
         const half2v pair =
             as_half2(*reinterpret_cast<const uint32_t *>(row + D / 2 + 4 * quad));
         uint32_t codes[kSteps];
@@ -727,7 +715,7 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void decode4_kernel(DecodeArgs a
       uint32_t vc[8][kE >= 8 ? kE / 8 : 1], vp[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const uint8_t *row = vr + (4 * quad + (j < 4 ? j : 12 + j)) * kRow;
+        const uint8_t *row = vr + (4 * quad + (j < 4 ? j : 12 + j)) * key_bytes;
         vp[j] = *reinterpret_cast<const uint32_t *>(row + D / 2 + n / 4 * 4);
         row += n * (kE / 2);
         if constexpr (D == 64) {
@@ -798,72 +786,58 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void decode4_kernel(DecodeArgs a
       }
     };
 
-    // Blocks of this wavefront, kStages - 1 of them in flight while one is used.
-    const int64_t key0 = key_begin + wave * kBlockKeys;
-    const int blocks =
-        a.num_blocks > 0 && key0 < key_end
-            ? int((key_end - key0 + kUnitKeys - 1) / kUnitKeys)
-            : 0;
+    // ---- the steps: kStages - 1 under way while one is used
+    const int steps = a.num_blocks > 0 && key_begin < key_end
+                          ? int((key_end - key_begin + step_keys - 1) / step_keys)
+                          : 0;
     if (a.num_blocks == 0 && key_begin < key_end) err = LUMEN_ERR_BLOCK_ID;
-    const auto key_of = [&](int i) { return key0 + int64_t(i) * kUnitKeys; };
-    uint32_t live[kStages];
-    int32_t id[2] = {-1, -1};
-    if constexpr (kAligned) {
-      if (blocks > 0) ids_of(key0, id);
-    } else {
-      if (blocks > 0) load_ids(key0, 0);
-      if (blocks > 1) load_ids(key_of(1), 1);
-      if (blocks > 2 && kStages > 2) load_ids(key_of(2), 2);
-      wait_loads<0>();
-    }
-    int started = 0;  // blocks, and their stage of the ring
-    const auto start = [&](int stage) {
-      if (started < blocks) {
-        int32_t then[2] = {-1, -1};
-        if constexpr (kAligned) {
-          if (started + 1 < blocks) ids_of(key_of(started + 1), then);
-        }
-        live[stage] = fetch(key_of(started), id, started, stage);
-        id[0] = then[0], id[1] = then[1];
-        // the ids of the block that the next start but kStages - 1 fetches
-        if constexpr (!kAligned) {
-          int64_t ahead = key_of(started + kStages);
-          load_ids(ahead < key_end ? ahead : key_begin, started + kStages);
-        }
+    constexpr int kLoads = kIssues + 1;  // of one start
+    const auto start = [&](int i, int stage) {
+      if (i < steps) {
+        load_rows(i, stage);
+        load_ids(i + kStages);
       }
-      ++started;
     };
-    constexpr int kLoads = kIssues + (kAligned ? 0 : 1);  // of one start
+    if (steps > 0) {
 #pragma unroll
-    for (int i = 0; i < kStages - 1; ++i) start(i);
-    for (int i = 0; i < blocks; i += kStages) {
+      for (int i = 0; i < kStages; ++i) load_ids(i);
+      wait_loads<0>();
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < kStages - 1; ++i) start(i, i);
+    }
+    for (int i = 0; i < steps; i += kStages) {
 #pragma unroll
       for (int t = 0; t < kStages; ++t) {
-        if (i + t < blocks) {
-          wait_lds();  // the stage's last reader is done
-          start((t + kStages - 1) % kStages);
-          const int behind = blocks - 1 - (i + t);  // started after this one
-          if (behind >= kStages - 1)
-            wait_loads<(kStages - 1) * kLoads>();
-          else if (kStages > 2 && behind == 1)
+        const int at = i + t;
+        if (at < steps) {
+          const int behind = steps - 1 - at;  // started after this one
+          if (kStages > 2 && behind >= kStages - 2)
+            wait_loads<(kStages - 2) * kLoads>();
+          else if (kStages > 3 && behind == 1)
             wait_loads<kLoads>();
           else
             wait_loads<0>();
-          use(ring + wave * kRing + t * kStage, live[t]);
+          // everyone's loads of this step have come, and everyone is done with
+          // the stage that the next start fills
+          lds_barrier();
+          start(at + kStages - 1, (t + kStages - 1) % kStages);
+          use(ring + t * kStage, live_of(at));
         }
       }
     }
     wait_loads<0>();
     l = quad_sum(l);
+    __syncthreads();  // the ring takes the sums
 
-    __syncthreads();  // the rings take the sums
-    // Joins the wavefronts' results into wavefront 0's o, m and l.
-    const auto join = [&]() {
+    // ---- the wavefronts of one head together, in the first of them
+    if (a.wg_blocks > 1) {
       if (quad == 0) lds_m[wave][n] = m;
       __syncthreads();
       float mm = m;
-#pragma unroll
-      for (int w = 0; w < kDecodeWaves; ++w) mm = fmaxf(mm, lds_m[w][n]);
+      if (active)
+        for (int w = hi; w < a.wg_heads * a.wg_blocks; w += a.wg_heads)
+          mm = fmaxf(mm, lds_m[w][n]);
       const float c = mm == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - mm);
       m = mm;
       l *= c;
@@ -871,99 +845,60 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void decode4_kernel(DecodeArgs a
 #pragma unroll
       for (int j = 0; j < kE; ++j) {
         o[j] *= c;
-        if (wave > 0)
-          *reinterpret_cast<float4v *>(&lds_o[wave - 1][j][4 * lane]) = o[j];
+        if (kbi > 0) *reinterpret_cast<float4v *>(&lds_o[wave][j][4 * lane]) = o[j];
       }
       __syncthreads();
-      if (wave == 0) {
-#pragma unroll
-        for (int w = 1; w < kDecodeWaves; ++w) {
+      if (kbi == 0)
+        for (int w = wave + a.wg_heads; w < a.wg_heads * a.wg_blocks; w += a.wg_heads) {
           l += lds_l[w][n];
 #pragma unroll
           for (int j = 0; j < kE; ++j)
-            o[j] += *reinterpret_cast<const float4v *>(&lds_o[w - 1][j][4 * lane]);
+            o[j] += *reinterpret_cast<const float4v *>(&lds_o[w][j][4 * lane]);
         }
-      }
-    };
-    join();
-
-    const bool whole = u == first && stop == first + units;
-    bool done = whole;
-    if (!whole) {
-      const int wa = share_of(first), wb = share_of(first + units - 1);
-      // a worker's share may end one request and start another: two places
-      const auto part_of = [&](int w) {
-        return a.parts + ((int64_t(hg) * a.workers + w) * 2 + (w == wa)) *
-                             part_floats(D);
-      };
-      if (wave == 0) {
-        float *to = part_of(worker);
-        if (n < rows) {
+    }
+    if (kbi == 0 && n < rows) {
+      if (u == first && stop == first + units) {  // the whole request
+        const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+        uint16_t *out =
+            a.out +
+            ((int64_t(r) * a.heads + h0 + hi) * a.group + g0 + n) * D + 4 * quad * kE;
 #pragma unroll
-          for (int j = 0; j < kE; ++j)
-            *reinterpret_cast<float4v *>(to + (j * kWave + lane) * 4) = o[j];
-          if (quad == 0) {
-            to[D * kQueries + n] = m;
-            to[D * kQueries + kQueries + n] = l;
+        for (int i = 0; i < 4; ++i) {
+          float x[kE < 8 ? 8 : kE];
+#pragma unroll
+          for (int j = 0; j < kE; ++j) x[j] = o[j][i] * inv;
+          uint16_t *to = out + i * kE;
+          if constexpr (kE == 4) {
+            *reinterpret_cast<uint2 *>(to) = uint2{
+                uint32_t(rounded<kBf16>(x[0])) | uint32_t(rounded<kBf16>(x[1])) << 16,
+                uint32_t(rounded<kBf16>(x[2])) | uint32_t(rounded<kBf16>(x[3])) << 16};
+          } else {
+#pragma unroll
+            for (int j = 0; j < kE; j += 8)
+              *reinterpret_cast<uint4 *>(to + j) = pack8<kBf16>(x + j);
           }
         }
-        __threadfence();
-        if (lane == 0) {
-          uint32_t *count = a.arrived + int64_t(r) * num_hg + hg;
-          const uint32_t before = __hip_atomic_fetch_add(
-              count, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
-          lds_last = before == uint32_t(wb - wa);
-          if (before == uint32_t(wb - wa))  // ready for the next call
-            __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        }
-      }
-      __syncthreads();
-      if (lds_last) {
-        __threadfence();
-        done = true;
+      } else {
+        // a share may end one request and start another: two places
+        float *part =
+            a.parts + (((int64_t(set) * a.workers + worker) * 2 + (u == first)) *
+                           a.wg_heads + hi) * part_floats(D);
+        float *to = part + n * D + 4 * quad * kE;
 #pragma unroll
-        for (int j = 0; j < kE; ++j) o[j] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
-        m = -INFINITY, l = 0.0f;
-        for (int w = wa + wave; w <= wb; w += kDecodeWaves) {
-          const float *from = part_of(w);
-          if (n >= rows) continue;
-          const float pm = from[D * kQueries + n];
-          const float pl = from[D * kQueries + kQueries + n];
-          const float mn = fmaxf(m, pm);
-          const float c0 = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
-          const float c1 = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(pm - mn);
-          m = mn;
-          l = l * c0 + pl * c1;
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-          for (int j = 0; j < kE; ++j) {
-            const float4v x =
-                *reinterpret_cast<const float4v *>(from + (j * kWave + lane) * 4);
-            o[j] = o[j] * c0 + x * c1;
-          }
+          for (int j = 0; j < kE; j += 4)
+            *reinterpret_cast<float4v *>(to + i * kE + j) =
+                float4v{o[j][i], o[j + 1][i], o[j + 2][i], o[j + 3][i]};
+        if (quad == 0) {
+          part[D * kQueries + n] = m;
+          part[D * kQueries + kQueries + n] = l;
         }
-        join();
       }
     }
-    if (done && wave == 0 && n < rows) {
-      const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
-      uint16_t *out =
-          a.out + (int64_t(r) * a.heads * a.group + h * a.group + g0 + n) * D;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float x[kE < 8 ? 8 : kE];
-#pragma unroll
-        for (int j = 0; j < kE; ++j) x[j] = o[j][i] * inv;
-        uint16_t *to = out + (4 * quad + i) * kE;
-        if constexpr (kE == 4) {
-          *reinterpret_cast<uint2 *>(to) =
-              uint2{uint32_t(rounded<kBf16>(x[0])) | uint32_t(rounded<kBf16>(x[1])) << 16,
-                    uint32_t(rounded<kBf16>(x[2])) | uint32_t(rounded<kBf16>(x[3])) << 16};
-        } else {
-#pragma unroll
-          for (int j = 0; j < kE; j += 8)
-            *reinterpret_cast<uint4 *>(to + j) = pack8<kBf16>(x + j);
-        }
-      }
+    if (a.spans && set == 0 && tid == 0 && u == first) {
+      const uint64_t last = (first + units) * shares + total - 1;
+      a.spans[r] = int2{worker, int(last / total) - 1};
     }
     u = stop;
     first += units;
@@ -971,6 +906,60 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void decode4_kernel(DecodeArgs a
     __syncthreads();  // the LDS is used again
   }
   record_wave(a.status, err);
+}
+
+// Partial results of requests that several workers shared, a workgroup for a
+// (request, query head) in turn: its wavefronts take every kJoinWaves-th
+// worker, two or four elements a lane, and wavefront 0 adds them up.
+constexpr int kJoinWaves = 4;
+template <int D, bool kBf16>
+__global__ __launch_bounds__(kJoinWaves *kWave) void decode4_join_kernel(DecodeArgs a) {
+  constexpr int kE = D / kWave;
+  __shared__ float lds_o[kJoinWaves][D], lds_m[kJoinWaves], lds_l[kJoinWaves];
+  const int lane = threadIdx.x & (kWave - 1);
+  const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) / kWave);
+  const int q_heads = a.heads * a.group;
+  const int tiles = (a.group + kQueries - 1) / kQueries;
+  const int64_t items = int64_t(a.num_reqs) * q_heads;
+  for (int64_t i = blockIdx.x; i < items; i += gridDim.x) {
+    const int r = int(i / q_heads), hq = int(i - int64_t(r) * q_heads);
+    const int2 span = a.spans[r];
+    if (span.x == span.y) continue;
+    const int h = hq / a.group, g = hq - h * a.group;
+    const int set = h / a.wg_heads * tiles + g / kQueries;
+    const int hi = h % a.wg_heads, n = g % kQueries;
+    float o[kE], m = -INFINITY, l = 0.0f;
+    for (int e = 0; e < kE; ++e) o[e] = 0.0f;
+    for (int w = span.x + wave; w <= span.y; w += kJoinWaves) {
+      const float *part =
+          a.parts + (((int64_t(set) * a.workers + w) * 2 + (w == span.x)) *
+                         a.wg_heads + hi) * part_floats(D);
+      const float pm = part[D * kQueries + n], pl = part[D * kQueries + kQueries + n];
+      const float mn = fmaxf(m, pm);
+      const float c0 = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
+      const float c1 = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(pm - mn);
+      m = mn;
+      l = l * c0 + pl * c1;
+      for (int e = 0; e < kE; ++e)
+        o[e] = o[e] * c0 + part[n * D + lane * kE + e] * c1;
+    }
+    __syncthreads();  // of the item before
+    for (int e = 0; e < kE; ++e) lds_o[wave][lane * kE + e] = o[e];
+    if (lane == 0) lds_m[wave] = m, lds_l[wave] = l;
+    __syncthreads();
+    if (wave > 0) continue;
+    for (int w = 1; w < kJoinWaves; ++w) m = fmaxf(m, lds_m[w]);
+    l = 0.0f;
+    for (int e = 0; e < kE; ++e) o[e] = 0.0f;
+    for (int w = 0; w < kJoinWaves; ++w) {
+      const float c = m == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(lds_m[w] - m);
+      l += lds_l[w] * c;
+      for (int e = 0; e < kE; ++e) o[e] += lds_o[w][lane * kE + e] * c;
+    }
+    const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+    for (int e = 0; e < kE; ++e)
+      a.out[i * D + lane * kE + e] = rounded<kBf16>(o[e] * inv);
+  }
 }
 
 // ------------------------------------------------------------ host side
@@ -1001,15 +990,10 @@ int check_layout(const lumen_kv_layout *l, int32_t layer, Layer *out) {
   return LUMEN_OK;
 }
 
-template <int D>
-void (*decode_kernel(bool bf16, bool aligned))(DecodeArgs) {
-  return bf16 ? (aligned ? decode4_kernel<D, true, true> : decode4_kernel<D, true, false>)
-              : (aligned ? decode4_kernel<D, false, true> : decode4_kernel<D, false, false>);
-}
-
 // Grid and workspace of a decode call on a device of `cus` compute units.
 struct DecodePlan {
-  int32_t heads;    // KV heads times tiles of 16 query heads
+  int32_t wg_heads, wg_blocks;
+  int32_t sets;     // sets of wg_heads KV heads, times tiles of 16 query heads
   int32_t workers;  // workgroups of one of them
   size_t parts_at, bytes;
 };
@@ -1022,18 +1006,31 @@ DecodePlan decode_plan(const lumen_kv_layout *l, int32_t head_dim,
                        int32_t num_reqs, int32_t num_q_heads, int cus) {
   const int group = num_q_heads / l->num_kv_heads;
   DecodePlan p;
-  p.heads = l->num_kv_heads * ((group + kQueries - 1) / kQueries);
-  // as many workgroups as are resident at once, two a CU; a multiple of 8
-  // for each head puts all heads of a share on one XCD, whose L2 then serves
-  // the lines that token-major rows of different heads have in common
-  const int all = (cus < kMaxUnits ? cus : kMaxUnits) * 2;
-  p.workers = all / p.heads;
-  if (p.workers > 8) p.workers &= ~7;
+  // the most heads whose rows lie together, and blocks of keys for the rest of
+  // the wavefronts
+  p.wg_heads = 1;
+  if (l->cache_order == LUMEN_CACHE_NHD)
+    for (int d = 2; d <= kDecodeWaves; ++d)
+      if (l->num_kv_heads % d == 0) p.wg_heads = d;
+  p.wg_blocks = kDecodeWaves / p.wg_heads;
+  p.sets = l->num_kv_heads / p.wg_heads * ((group + kQueries - 1) / kQueries);
+  p.workers = (cus < kMaxUnits ? cus : kMaxUnits) / p.sets;  // one workgroup a CU
   if (p.workers < 1) p.workers = 1;
-  p.parts_at = (size_t(num_reqs) * p.heads * sizeof(uint32_t) + 255) & ~size_t(255);
-  p.bytes = p.parts_at + size_t(p.workers) * p.heads * 2 * part_floats(head_dim) *
-                             sizeof(float);
+  p.parts_at = (size_t(num_reqs) * sizeof(int2) + 255) & ~size_t(255);
+  p.bytes = p.parts_at + size_t(p.workers) * p.sets * 2 * p.wg_heads *
+                             part_floats(head_dim) * sizeof(float);
   return p;
+}
+
+struct DecodeKernels {
+  void (*main)(DecodeArgs);
+  void (*join)(DecodeArgs);
+};
+
+template <int D>
+DecodeKernels decode_kernels(bool bf16) {
+  return bf16 ? DecodeKernels{decode4_kernel<D, true>, decode4_join_kernel<D, true>}
+              : DecodeKernels{decode4_kernel<D, false>, decode4_join_kernel<D, false>};
 }
 
 template <bool kAppend>
@@ -1210,36 +1207,47 @@ int lumen_attn_decode4(const lumen_kv_layout *layout, int32_t layer,
   (void)hipGetLastError();
   const DecodePlan plan =
       decode_plan(layout, at.head_dim, num_reqs, num_q_heads, cus);
-  uint32_t *arrived = static_cast<uint32_t *>(d_workspace);
   const int32_t bs = layout->block_size;
-  DecodeArgs a{static_cast<const uint8_t *>(d_cache) + at.k,
-               static_cast<const uint8_t *>(d_cache) + at.v,
-               d_block_tables,
-               bt_cols,
-               bs,
-               __builtin_ctz(unsigned(bs)),
-               layout->num_blocks,
-               d_lens,
-               num_reqs,
-               layout->num_kv_heads,
-               num_q_heads / layout->num_kv_heads,
-               layout->cache_order == LUMEN_CACHE_HND,
-               rows_of(q, 0),
-               scale * 1.44269504088896341f,
-               static_cast<uint16_t *>(d_out),
-               d_status,
-               plan.workers,
-               arrived,
-               reinterpret_cast<float *>(static_cast<char *>(d_workspace) +
-                                         plan.parts_at)};
+  const int64_t unit = int64_t(kBlockKeys) * plan.wg_blocks * kUnitBlocks;
+  // no request can be shared: no results to join
+  const bool shared = int64_t(bt_cols) * bs > unit;
+  DecodeArgs a;
+  a.k = static_cast<const uint8_t *>(d_cache) + at.k;
+  a.v = static_cast<const uint8_t *>(d_cache) + at.v;
+  a.bt = d_block_tables;
+  a.bt_cols = bt_cols;
+  a.block_size = bs;
+  a.page_shift = (bs & (bs - 1)) == 0 ? __builtin_ctz(unsigned(bs)) : -1;
+  a.num_blocks = layout->num_blocks;
+  a.lens = d_lens;
+  a.num_reqs = num_reqs;
+  a.heads = layout->num_kv_heads;
+  a.group = num_q_heads / layout->num_kv_heads;
+  a.hnd = layout->cache_order == LUMEN_CACHE_HND;
+  a.q = rows_of(q, 0);
+  a.scale_log2 = scale * 1.44269504088896341f;
+  a.out = static_cast<uint16_t *>(d_out);
+  a.status = d_status;
+  a.wg_heads = plan.wg_heads;
+  a.wg_blocks = plan.wg_blocks;
+  a.workers = plan.workers;
+  // lines that no other workgroup reads pass the caches by
+  a.stream = a.hnd || plan.wg_heads == a.heads;
+  a.spans = shared ? static_cast<int2 *>(d_workspace) : nullptr;
+  a.parts = reinterpret_cast<float *>(static_cast<char *>(d_workspace) + plan.parts_at);
   const bool bf = dtype == LUMEN_ATTN_BF16;
-  const bool al = bs >= 16 && (bs & (bs - 1)) == 0;
-  void (*kernel)(DecodeArgs) =
-      at.head_dim == 64    ? decode_kernel<64>(bf, al)
-      : at.head_dim == 128 ? decode_kernel<128>(bf, al)
-                           : decode_kernel<256>(bf, al);
-  hipLaunchKernelGGL(kernel, dim3(unsigned(plan.workers * plan.heads)),
-                     dim3(kDecodeThreads), 0, static_cast<hipStream_t>(stream), a);
+  const DecodeKernels k = at.head_dim == 64    ? decode_kernels<64>(bf)
+                          : at.head_dim == 128 ? decode_kernels<128>(bf)
+                                               : decode_kernels<256>(bf);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  hipLaunchKernelGGL(k.main, dim3(unsigned(plan.workers * plan.sets)),
+                     dim3(kDecodeThreads), 0, s, a);
+  if (shared) {
+    int64_t items = int64_t(num_reqs) * num_q_heads;
+    const int64_t most = int64_t(cus) * 8;
+    hipLaunchKernelGGL(k.join, dim3(unsigned(items < most ? items : most)),
+                       dim3(kJoinWaves * kWave), 0, s, a);
+  }
   return hipGetLastError() == hipSuccess ? LUMEN_OK : LUMEN_ERR_HIP;
 }
 
