@@ -359,11 +359,10 @@ struct DecodeArgs {
   const uint8_t *k, *v;  // of the layer
   const int32_t *bt;
   int32_t bt_cols, block_size;
-  int32_t page_shift;  // log2 of block_size, or -1
   int64_t num_blocks;
   const int32_t *lens;
   int32_t num_reqs, heads, group;
-  bool hnd, stream;
+  bool hnd, bf16;
   Rows q;
   float scale_log2;  // scale * log2(e)
   uint16_t *out;
@@ -381,11 +380,27 @@ typedef float float4v __attribute__((ext_vector_type(4)));
 constexpr int kDecodeWaves = 8;
 constexpr int kDecodeThreads = kDecodeWaves * kWave;
 constexpr int kBlockKeys = 32;  // keys a wavefront takes at a time
+constexpr int kSegments = kWave;
+// A round's steps, tiles and blocks of 32 keys.
+constexpr int kRoundSteps = 128, kTiles = 1024, kLive = 512, kLast = 256;
 constexpr int kUnitBlocks = 4;  // a unit of work, in the workgroup's blocks
 constexpr int kQueries = 16;    // columns of a product
 // Weights are 2^(s - m + kBias) with s - m at most kRise: within a 16-bit
 // float up to 2^14, and down to 2^-38 of the largest before they vanish.
 constexpr float kRise = 8.0f, kBias = 6.0f;
+
+template <int kE, bool kBf16>
+__device__ __forceinline__ void store_out(uint16_t *to, const float *x) {
+  if constexpr (kE == 4) {
+    *reinterpret_cast<uint2 *>(to) =
+        uint2{uint32_t(rounded<kBf16>(x[0])) | uint32_t(rounded<kBf16>(x[1])) << 16,
+              uint32_t(rounded<kBf16>(x[2])) | uint32_t(rounded<kBf16>(x[3])) << 16};
+  } else {
+#pragma unroll
+    for (int j = 0; j < kE; j += 8)
+      *reinterpret_cast<uint4 *>(to + j) = pack8<kBf16>(x + j);
+  }
+}
 
 // Floats of one partial result: kQueries rows of D sums, then a maximum and a
 // sum for each.
@@ -410,32 +425,31 @@ __device__ __forceinline__ void codes4(uint32_t w, uint32_t mask, uint32_t one,
 
 // Maximum and sum over the four lanes of one query (l % 16).
 __device__ __forceinline__ float quad_max(float x) {
-  x = fmaxf(x, swapped<16>(x));
-  return fmaxf(x, swapped<32>(x));
+  float a, b;
+  both<16>(x, &a, &b);
+  both<32>(fmaxf(a, b), &a, &b);
+  return fmaxf(a, b);
 }
 __device__ __forceinline__ float quad_sum(float x) {
-  x += swapped<16>(x);
-  return x + swapped<32>(x);
+  float a, b;
+  both<16>(x, &a, &b);
+  both<32>(a + b, &a, &b);
+  return a + b;
 }
 
-// Starts a load of kBytes a lane from the lane's address into LDS, at `to` +
-// kBytes * lane (`to` the wavefront's; kStream: not to be kept in caches).  It is counted like any load, but the
+// Starts a load of 16 bytes a lane from the lane's address into LDS, at byte
+// `to` + 16 * lane (`to` the wavefront's; kStream: not to be kept in caches).  It is counted like any load, but the
 // compiler does not know of it: wait_loads<n> waits until at most the last n
 // are still under way, and keeps reads of the LDS behind it.  That, unlike the
 // builtin, lets a read wait for its own block alone.
-template <int kBytes, bool kStream>
-__device__ __forceinline__ void load_to_lds(const void *from, void *to) {
-  const uint32_t at = __builtin_amdgcn_readfirstlane(uint32_t(
-      reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) void *)(to))));
-  if constexpr (kBytes == 16 && kStream)
+template <bool kStream>
+__device__ __forceinline__ void load_to_lds(const void *from, uint32_t to) {
+  if constexpr (kStream)
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt"
-                 :: "s"(at), "v"(from) : "memory");
-  else if constexpr (kBytes == 16)
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
-                 :: "s"(at), "v"(from) : "memory");
+                 :: "s"(to), "v"(from) : "memory");
   else
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off"
-                 :: "s"(at), "v"(from) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+                 :: "s"(to), "v"(from) : "memory");
 }
 template <int kLeft>
 __device__ __forceinline__ void wait_loads() {
@@ -445,6 +459,8 @@ __device__ __forceinline__ void wait_loads() {
 __device__ __forceinline__ void lds_barrier() {
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
+
+#define LDS_PTR(T, p) ((__attribute__((address_space(3))) T *)(p))
 
 // A value that is the same in all lanes, in scalar registers.
 __device__ __forceinline__ uint64_t uniform(uint64_t x) {
@@ -478,7 +494,7 @@ __device__ __forceinline__ uint64_t uniform(uint64_t x) {
 // lane holds D/16 consecutive elements of 8 keys, all of one quarter.  Values
 // are exact: code and pair give the stored value by one fused multiply-add that
 // rounds as the format says.
-template <int D, bool kBf16>
+template <int D, bool kStream>
 __global__ __launch_bounds__(kDecodeThreads, 2) void decode4_kernel(DecodeArgs a) {
   constexpr int kRow = D / 2 + 16;
   constexpr int kSteps = D / 32;  // products over head_dim
@@ -487,18 +503,24 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void decode4_kernel(DecodeArgs a
   constexpr int kParts = kRow / 16;  // 16-byte pieces of a row
   constexpr int kIssues = 2 * kBlockKeys * kParts / kWave;
   constexpr int kStage = kDecodeWaves * 2 * kBlockKeys * kRow;  // bytes
-  constexpr int kSlots = 8;  // of the block ids' ring
-  static_assert(kSlots > kStages, "ids come kStages steps ahead");
-  // the ring, and after a request the wavefronts' sums
   __shared__ __attribute__((aligned(16))) uint8_t ring[kStages * kStage];
-  __shared__ int32_t id_ring[kSlots][kDecodeWaves * kBlockKeys];
+  // of the steps of a round: where their tiles' rows start (bytes from the
+  // layer's K), which keys of each block of 32 count, and the part of the round
+  // that a step belongs to, with kLast in its last step
+  __shared__ uint64_t tile_at[kTiles];
+  __shared__ uint32_t live_keys[kLive];
+  __shared__ int step_part[kRoundSteps];
   __shared__ float lds_m[kDecodeWaves][kQueries], lds_l[kDecodeWaves][kQueries];
   __shared__ uint64_t lds_scan[kDecodeWaves];
   __shared__ uint64_t lds_first;  // of the request that a share starts in
   __shared__ int lds_req;
-  static_assert(kDecodeWaves * kE * 4 * kWave * sizeof(float) <= sizeof(ring),
-                "the sums fit the ring");
-  auto &lds_o = *reinterpret_cast<float(*)[kDecodeWaves][kE][4 * kWave]>(ring);
+  // the next kSegments parts of requests in the share: keys [key0, key1) of
+  // request r, their steps' places in the round, and whether the request
+  // starts (1) and ends (2) in it
+  __shared__ uint32_t seg_key0[kSegments], seg_key1[kSegments];
+  __shared__ int seg_end[kSegments + 1], seg_flags[kSegments];
+  static_assert(kDecodeWaves / 2 * kE * 4 * kWave * int(sizeof(float)) <= kStage,
+                "half of the wavefronts' sums fit a stage");
 
   const int tid = threadIdx.x, lane = tid & (kWave - 1);
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
@@ -518,11 +540,11 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void decode4_kernel(DecodeArgs a
 
   // ---- the share: units [u0, u1) of all requests' units
   const int64_t cap = int64_t(a.bt_cols) * a.block_size;
-  const auto length = [&](int r) {
-    const int64_t len = a.lens[r];
+  const auto length = [&](int r) __attribute__((always_inline)) {
+    const int64_t len = a.num_blocks > 0 ? a.lens[r] : 0;
     return len < 0 ? int64_t(0) : len < cap ? len : cap;
   };
-  const auto units_of = [&](int64_t len) {
+  const auto units_of = [&](int64_t len) __attribute__((always_inline)) {
     return len <= unit_keys ? 1u : uint32_t(len + unit_keys - 1) / uint32_t(unit_keys);
   };
   const int per = (a.num_reqs + kDecodeThreads - 1) / kDecodeThreads;
@@ -531,7 +553,8 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void decode4_kernel(DecodeArgs a
   uint64_t mine = 0;
   for (int r = ra; r < rb; ++r) {
     const int len = a.lens[r];
-    if (len < 0 || len > cap) err = LUMEN_ERR_RANGE;
+    if (len < 0 || len > cap) err = err < LUMEN_ERR_RANGE ? err : LUMEN_ERR_RANGE;
+    if (len > 0 && a.num_blocks == 0) err = LUMEN_ERR_BLOCK_ID;
     mine += units_of(length(r));
   }
   uint64_t upto = mine;
@@ -569,341 +592,465 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void decode4_kernel(DecodeArgs a
   // then of V, each (token, head, part) in the order of a token-major page
   const uint64_t page_bytes = uint64_t(a.block_size) * a.heads * kRow;
   const uint32_t slot_bytes = (a.hnd ? 1 : a.heads) * kRow;
-  int tok[kIssues];
-  int64_t offset[kIssues];
+  // A token's pieces are turned by a number of places that makes the same piece
+  // of 16 tokens lie in 16 different sixteenths of the banks' 256 bytes.
+  const int pieces = a.wg_heads * kParts;
+  const int even = pieces & 15 ? pieces & -pieces : 16;  // gcd(pieces, 16)
+  const auto turn = [&](int t) __attribute__((always_inline)) { return (t & 15) * even / 16; };
+  // keys of a tile: the largest power of two up to 16 that divides a page
+  const int low = a.block_size & -a.block_size;
+  const int tile_shift = low >= 16 ? 4 : __builtin_ctz(low);
+  int tile[kIssues];             // of the step, that the piece is in
+  const uint8_t *piece[kIssues]; // its place in a tile at byte 0
 #pragma unroll
   for (int i = 0; i < kIssues; ++i) {
-    const int half = step_keys * a.wg_heads * kParts;
+    const int half = step_keys * pieces;
     int c = i * kDecodeThreads + tid;
     const bool is_v = c >= half;
     c = is_v ? c - half : c;
     c = c < half ? c : half - 1;  // lanes past the step's end repeat a piece
-    const int row = c / kParts, t = row / a.wg_heads;
-    tok[i] = t;
-    offset[i] = (is_v ? a.v - a.k : 0) +
-                int64_t(a.hnd ? h0 * a.block_size : h0 + row - t * a.wg_heads) * kRow +
-                c % kParts * 16;
+    const int t = c / pieces;
+    int x = c - t * pieces - turn(t);
+    x = x < 0 ? x + pieces : x;
+    tile[i] = t >> tile_shift;
+    piece[i] = (is_v ? a.v : a.k) + (t & ((1 << tile_shift) - 1)) * slot_bytes +
+               int64_t(a.hnd ? h0 * a.block_size : h0 + x / kParts) * kRow +
+               x % kParts * 16;
   }
-  const bool wide = a.page_shift >= 4;  // tiles of 16 keys share a block id
-  const auto page_of = [&](uint32_t key) {
-    return a.page_shift >= 0 ? key >> a.page_shift : key / uint32_t(a.block_size);
+  const int step_tiles = step_keys >> tile_shift;
+  int round = kTiles / step_tiles;  // steps
+  round = round < kLive / a.wg_blocks ? round : kLive / a.wg_blocks;
+  round = round < kRoundSteps ? round : kRoundSteps;
+  // where the lane finds part `part` of its head's row of token t in a step
+  const auto place = [&](int t, int part) __attribute__((always_inline)) {
+    int x = hi * kParts + part + turn(t);
+    x = x < pieces ? x : x - pieces;
+    return uint32_t(t * pieces + x) * 16;
   };
+  // offsets into a stage of what the lane reads: K of key n, the same for n + 16;
+  // V of keys 4 quad + 0, 1 and + 2, 3, the same for + 16
+  constexpr int kVBytes = kE / 2;  // of V's codes
+  const int t0 = (active ? kbi : 0) * kBlockKeys;
+  uint32_t at_k[D == 256 ? 2 : 1], at_v[2], at_kp, at_vp[2];
+  at_k[0] = place(t0 + n, quad * (D / 8) / 16) + quad * (D / 8) % 16;
+  if constexpr (D == 256) at_k[1] = place(t0 + n, quad * 2 + 1);
+  at_kp = place(t0 + n, kParts - 1) + quad * 4;
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    at_v[j] = place(t0 + 4 * quad + 2 * j, n * kVBytes / 16) + n * kVBytes % 16;
+    at_vp[j] = place(t0 + 4 * quad + 2 * j, kParts - 1) + n / 4 * 4;
+  }
+  // (turn() is the same for keys 2j and 2j + 1 wherever it is not 0: `even` is
+  // at most 8 for any number of pieces of up to 8 heads)
+  const uint32_t key_bytes = pieces * 16, v_at = step_keys * key_bytes;
 
-  uint64_t u = u0;
-  while (u < u1) {
-    const int64_t len = length(r);
-    const uint64_t units = units_of(len);
-    const uint64_t stop = first + units < u1 ? first + units : u1;
-    const int64_t end = int64_t(stop - first) * unit_keys;
-    const uint32_t key_end = uint32_t(end < len ? end : len);
-    const uint32_t key_begin = uint32_t(u - first) * uint32_t(unit_keys);
-
-    // ---- Q: 16-bit floats under a power of two of the row's own, so that
-    // bf16 and fp16 keep all their bits whatever their range
-    half8v q[kSteps];
-    float cq;
-    {
-      const int row = (h0 + hi) * a.group + g0 + (n < rows ? n : 0);
-      const uint16_t *p =
-          a.q.base + int64_t(r) * a.q.token + row * a.q.head + quad * (D / 4);
-      uint4 raw[kSteps];
-      float big = 0.0f, x[8];
+  // ---- Q: 16-bit floats under a power of two of the row's own, so that bf16
+  // and fp16 keep all their bits whatever their range
+  half8v q[kSteps];
+  float cq = 0.0f;
+  uint4 raw[kSteps];
+  const auto fetch_q = [&](int req) __attribute__((always_inline)) {
+    const int row = (h0 + hi) * a.group + g0 + (n < rows ? n : 0);
+    const uint16_t *p =
+        a.q.base + int64_t(req) * a.q.token + row * a.q.head + quad * (D / 4);
 #pragma unroll
-      for (int i = 0; i < kSteps; ++i) {
-        raw[i] = *reinterpret_cast<const uint4 *>(p + 8 * i);
-        unpack8<kBf16>(raw[i], x);
+    for (int i = 0; i < kSteps; ++i)
+      raw[i] = *reinterpret_cast<const uint4 *>(p + 8 * i);
+  };
+  const auto take_q = [&]() __attribute__((always_inline)) {
+    float big = 0.0f, x[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) big = fmaxf(big, fabsf(x[j]));
-      }
-      big = quad_max(big);
-      uint32_t e = __builtin_bit_cast(uint32_t, big) >> 23;  // NaN: not the maximum
-      e = e == 255 ? 140 : e < 14 ? 14 : e;
-      const float up = __builtin_bit_cast(float, (267 - e) << 23);  // to 2^13..2^14
-      cq = a.scale_log2 * __builtin_bit_cast(float, (e - 13) << 23);
+    for (int i = 0; i < kSteps; ++i) {
+      a.bf16 ? unpack8<true>(raw[i], x) : unpack8<false>(raw[i], x);
 #pragma unroll
-      for (int i = 0; i < kSteps; ++i) {
-        unpack8<kBf16>(raw[i], x);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          q[i][2 * j] = _Float16(x[j] * up);
-          q[i][2 * j + 1] = _Float16(x[j + 4] * up);
-        }
-      }
+      for (int j = 0; j < 8; ++j) big = fmaxf(big, fabsf(x[j]));
     }
-
-    float4v o[kE];
+    big = quad_max(big);
+    uint32_t e = __builtin_bit_cast(uint32_t, big) >> 23;  // NaN: not the maximum
+    e = e == 255 ? 140 : e < 14 ? 14 : e;
+    const float up = __builtin_bit_cast(float, (267 - e) << 23);  // to 2^13..2^14
+    cq = a.scale_log2 * __builtin_bit_cast(float, (e - 13) << 23);
 #pragma unroll
-    for (int j = 0; j < kE; ++j) o[j] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
-    float m = -INFINITY, l = 0.0f;
-
-    const int32_t *table = a.bt + int64_t(r) * a.bt_cols;
-    const auto key_of = [&](int i) { return key_begin + uint32_t(i) * step_keys; };
-    // ids of a step's tiles (or keys); past the end those of its last key
-    const auto load_ids = [&](int i) {
-      uint32_t key = key_of(i) + (tid % (kDecodeWaves * kBlockKeys) << (wide ? 4 : 0));
-      key = key < key_end ? key : key_end - 1;
-      load_to_lds<4, false>(table + page_of(key),
-                            &id_ring[i % kSlots][wave % 4 * kWave]);
-    };
-    const auto load_rows = [&](int i, int stage) {
-      uint8_t *to = ring + stage * kStage + wave * kWave * 16;
-#pragma unroll
-      for (int c = 0; c < kIssues; ++c) {
-        int32_t id = id_ring[i % kSlots][tok[c] >> (wide ? 4 : 0)];
-        if (id < 0 || id >= a.num_blocks) id = 0;  // some block: the key is left out
-        const uint32_t key = key_of(i) + tok[c];
-        const uint32_t pos = a.page_shift >= 0 ? key & (uint32_t(a.block_size) - 1)
-                                               : key % uint32_t(a.block_size);
-        const uint8_t *from =
-            a.k + uint32_t(id) * page_bytes + uint64_t(pos) * slot_bytes + offset[c];
-        if (a.stream)
-          load_to_lds<16, true>(from, to + c * kDecodeThreads * 16);
-        else
-          load_to_lds<16, false>(from, to + c * kDecodeThreads * 16);
-      }
-    };
-    // The wavefront's keys of a step that count, a bit each.
-    const auto live_of = [&](int i) {
-      const int mykey = kbi * kBlockKeys + (lane & 31);
-      const int32_t id = active ? id_ring[i % kSlots][mykey >> (wide ? 4 : 0)] : 0;
-      const bool in = active && key_of(i) + mykey < key_end;
-      const bool ok = id >= 0 && id < a.num_blocks;
-      if (in && !ok) err = LUMEN_ERR_BLOCK_ID;
-      return uint32_t(__ballot(in && ok));
-    };
-    const auto use = [&](const uint8_t *stage, uint32_t live) {
-      if (live == 0) return;
-      // rows of the wavefront's block: (key, head)
-      const uint32_t key_bytes = a.wg_heads * kRow;
-      const uint8_t *kr = stage + (kbi * kBlockKeys * a.wg_heads + hi) * kRow;
-      const uint8_t *vr = kr + step_keys * key_bytes;
-      float4v s[2];
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        s[t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
-        const uint8_t *row = kr + (16 * t + n) * key_bytes;
-        const half2v pair =
-            as_half2(*reinterpret_cast<const uint32_t *>(row + D / 2 + 4 * quad));
-        uint32_t codes[kSteps];
-        row += quad * (D / 8);
-        if constexpr (D == 64) {
-          const uint2 x = *reinterpret_cast<const uint2 *>(row);
-          codes[0] = x.x, codes[1] = x.y;
-        } else {
-#pragma unroll
-          for (int i = 0; i < kSteps; i += 4) {
-            const uint4 x = *reinterpret_cast<const uint4 *>(row + 4 * i);
-            codes[i] = x.x, codes[i + 1] = x.y, codes[i + 2] = x.z, codes[i + 3] = x.w;
-          }
-        }
-        const half2v A = {pair[0], pair[0]}, B = {pair[1], pair[1]};
-#pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
-          half2v x[4];
-          codes4(codes[i], mask, one, x);
-          half8v f;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const half2v y = __builtin_elementwise_fma(x[j], A, B);
-            f[2 * j] = y[0];
-            f[2 * j + 1] = y[1];
-          }
-          s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f, q[i], s[t], 0, 0, 0);
-        }
-      }
-      // V: the lane's elements of 8 keys
-      uint32_t vc[8][kE >= 8 ? kE / 8 : 1], vp[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const uint8_t *row = vr + (4 * quad + (j < 4 ? j : 12 + j)) * key_bytes;
-        vp[j] = *reinterpret_cast<const uint32_t *>(row + D / 2 + n / 4 * 4);
-        row += n * (kE / 2);
-        if constexpr (D == 64) {
-          vc[j][0] = *reinterpret_cast<const uint16_t *>(row);
-        } else if constexpr (D == 128) {
-          vc[j][0] = *reinterpret_cast<const uint32_t *>(row);
-        } else {
-          const uint2 x = *reinterpret_cast<const uint2 *>(row);
-          vc[j][0] = x.x, vc[j][kE / 8 - 1] = x.y;
-        }
-      }
-      if (live != 0xffffffffu) {
-        // a key left out has no score, and no value either: its pair may be NaN
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const bool in = (live >> (4 * quad + (j < 4 ? j : 12 + j))) & 1;
-          if (!in) s[j / 4][j % 4] = -INFINITY;
-          if (!in) vp[j] = 0;
-        }
-      }
-      float top = -INFINITY;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) top = fmaxf(top, s[j / 4][j % 4]);
-      top = quad_max(top) * cq;
-      if (__any(top > m + kRise)) {
-        const float mn = fmaxf(m, top);
-        const float c = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
-        m = mn;
-        l *= c;
-#pragma unroll
-        for (int j = 0; j < kE; ++j) o[j] *= c;
-      }
-      const float shift = kBias - (m == -INFINITY ? 0.0f : m);
-      half8v p;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float x = __builtin_amdgcn_exp2f(
-            __builtin_fmaf(s[j / 4][j % 4], cq, shift));
-        l += x;
-        p[j] = _Float16(x);
-      }
-      half2v A[4], B[4];  // of keys 2j and 2j + 1 of the lane
+    for (int i = 0; i < kSteps; ++i) {
+      a.bf16 ? unpack8<true>(raw[i], x) : unpack8<false>(raw[i], x);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        A[j] = as_half2(__builtin_amdgcn_perm(vp[2 * j + 1], vp[2 * j], 0x05040100));
-        B[j] = as_half2(__builtin_amdgcn_perm(vp[2 * j + 1], vp[2 * j], 0x07060302));
+        q[i][2 * j] = _Float16(x[j] * up);
+        q[i][2 * j + 1] = _Float16(x[j + 4] * up);
       }
+    }
+  };
+  float4v o[kE];
+  float m = -INFINITY, l = 0.0f;
+  const auto clear = [&]() __attribute__((always_inline)) {
 #pragma unroll
-      for (int w = 0; w < kE / 4; ++w) {  // four elements at a time
-        half8v f[4];
+    for (int j = 0; j < kE; ++j) o[j] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+    m = -INFINITY, l = 0.0f;
+  };
+
+  const auto use = [&](const uint8_t *stage, uint32_t live) __attribute__((always_inline)) {
+    float4v s[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      s[t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+      const uint8_t *row = stage + 16 * t * key_bytes;
+      const half2v pair = as_half2(*reinterpret_cast<const uint32_t *>(row + at_kp));
+      uint32_t codes[kSteps];
+      if constexpr (D == 64) {
+        const uint2 x = *reinterpret_cast<const uint2 *>(row + at_k[0]);
+        codes[0] = x.x, codes[1] = x.y;
+      } else {
+#pragma unroll
+        for (int i = 0; i < kSteps; i += 4) {
+          const uint4 x = *reinterpret_cast<const uint4 *>(row + at_k[i / 4]);
+          codes[i] = x.x, codes[i + 1] = x.y, codes[i + 2] = x.z, codes[i + 3] = x.w;
+        }
+      }
+      const half2v A = {pair[0], pair[0]}, B = {pair[1], pair[1]};
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i) {
+        half2v x[4];
+        codes4(codes[i], mask, one, x);
+        half8v f;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          half2v x[4];
-          codes4(__builtin_amdgcn_perm(vc[2 * j + 1][w / 2], vc[2 * j][w / 2],
-                                       w % 2 ? 0x07060302 : 0x05040100),
-                 mask, one, x);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const half2v y = __builtin_elementwise_fma(x[e], A[j], B[j]);
-            f[e][2 * j] = y[0];
-            f[e][2 * j + 1] = y[1];
-          }
+          const half2v y = __builtin_elementwise_fma(x[j], A, B);
+          f[2 * j] = y[0];
+          f[2 * j + 1] = y[1];
         }
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          o[4 * w + e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[e], p, o[4 * w + e],
-                                                                0, 0, 0);
-      }
-    };
-
-    // ---- the steps: kStages - 1 under way while one is used
-    const int steps = a.num_blocks > 0 && key_begin < key_end
-                          ? int((key_end - key_begin + step_keys - 1) / step_keys)
-                          : 0;
-    if (a.num_blocks == 0 && key_begin < key_end) err = LUMEN_ERR_BLOCK_ID;
-    constexpr int kLoads = kIssues + 1;  // of one start
-    const auto start = [&](int i, int stage) {
-      if (i < steps) {
-        load_rows(i, stage);
-        load_ids(i + kStages);
-      }
-    };
-    if (steps > 0) {
-#pragma unroll
-      for (int i = 0; i < kStages; ++i) load_ids(i);
-      wait_loads<0>();
-      __syncthreads();
-#pragma unroll
-      for (int i = 0; i < kStages - 1; ++i) start(i, i);
-    }
-    for (int i = 0; i < steps; i += kStages) {
-#pragma unroll
-      for (int t = 0; t < kStages; ++t) {
-        const int at = i + t;
-        if (at < steps) {
-          const int behind = steps - 1 - at;  // started after this one
-          if (kStages > 2 && behind >= kStages - 2)
-            wait_loads<(kStages - 2) * kLoads>();
-          else if (kStages > 3 && behind == 1)
-            wait_loads<kLoads>();
-          else
-            wait_loads<0>();
-          // everyone's loads of this step have come, and everyone is done with
-          // the stage that the next start fills
-          lds_barrier();
-          start(at + kStages - 1, (t + kStages - 1) % kStages);
-          use(ring + t * kStage, live_of(at));
-        }
+        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f, q[i], s[t], 0, 0, 0);
       }
     }
-    wait_loads<0>();
-    l = quad_sum(l);
-    __syncthreads();  // the ring takes the sums
-
-    // ---- the wavefronts of one head together, in the first of them
-    if (a.wg_blocks > 1) {
-      if (quad == 0) lds_m[wave][n] = m;
-      __syncthreads();
-      float mm = m;
-      if (active)
-        for (int w = hi; w < a.wg_heads * a.wg_blocks; w += a.wg_heads)
-          mm = fmaxf(mm, lds_m[w][n]);
-      const float c = mm == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - mm);
-      m = mm;
-      l *= c;
-      if (quad == 0) lds_l[wave][n] = l;
+    // V: the lane's elements of 8 keys
+    uint32_t vc[8][kE >= 8 ? kE / 8 : 1], vp[8];
 #pragma unroll
-      for (int j = 0; j < kE; ++j) {
-        o[j] *= c;
-        if (kbi > 0) *reinterpret_cast<float4v *>(&lds_o[wave][j][4 * lane]) = o[j];
-      }
-      __syncthreads();
-      if (kbi == 0)
-        for (int w = wave + a.wg_heads; w < a.wg_heads * a.wg_blocks; w += a.wg_heads) {
-          l += lds_l[w][n];
-#pragma unroll
-          for (int j = 0; j < kE; ++j)
-            o[j] += *reinterpret_cast<const float4v *>(&lds_o[w][j][4 * lane]);
-        }
-    }
-    if (kbi == 0 && n < rows) {
-      if (u == first && stop == first + units) {  // the whole request
-        const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
-        uint16_t *out =
-            a.out +
-            ((int64_t(r) * a.heads + h0 + hi) * a.group + g0 + n) * D + 4 * quad * kE;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float x[kE < 8 ? 8 : kE];
-#pragma unroll
-          for (int j = 0; j < kE; ++j) x[j] = o[j][i] * inv;
-          uint16_t *to = out + i * kE;
-          if constexpr (kE == 4) {
-            *reinterpret_cast<uint2 *>(to) = uint2{
-                uint32_t(rounded<kBf16>(x[0])) | uint32_t(rounded<kBf16>(x[1])) << 16,
-                uint32_t(rounded<kBf16>(x[2])) | uint32_t(rounded<kBf16>(x[3])) << 16};
-          } else {
-#pragma unroll
-            for (int j = 0; j < kE; j += 8)
-              *reinterpret_cast<uint4 *>(to + j) = pack8<kBf16>(x + j);
-          }
-        }
+    for (int j = 0; j < 8; ++j) {
+      const uint8_t *row = stage + v_at + ((j & 1) + (j & 4) * 4) * key_bytes;
+      vp[j] = *reinterpret_cast<const uint32_t *>(row + at_vp[j / 2 % 2]);
+      row += at_v[j / 2 % 2];
+      if constexpr (D == 64) {
+        vc[j][0] = *reinterpret_cast<const uint16_t *>(row);
+      } else if constexpr (D == 128) {
+        vc[j][0] = *reinterpret_cast<const uint32_t *>(row);
       } else {
-        // a share may end one request and start another: two places
-        float *part =
-            a.parts + (((int64_t(set) * a.workers + worker) * 2 + (u == first)) *
-                           a.wg_heads + hi) * part_floats(D);
-        float *to = part + n * D + 4 * quad * kE;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int j = 0; j < kE; j += 4)
-            *reinterpret_cast<float4v *>(to + i * kE + j) =
-                float4v{o[j][i], o[j + 1][i], o[j + 2][i], o[j + 3][i]};
-        if (quad == 0) {
-          part[D * kQueries + n] = m;
-          part[D * kQueries + kQueries + n] = l;
-        }
+        const uint2 x = *reinterpret_cast<const uint2 *>(row);
+        vc[j][0] = x.x, vc[j][kE / 8 - 1] = x.y;
       }
     }
-    if (a.spans && set == 0 && tid == 0 && u == first) {
-      const uint64_t last = (first + units) * shares + total - 1;
-      a.spans[r] = int2{worker, int(last / total) - 1};
+    if (live != 0xffffffffu) {
+      // a key left out has no score, and no value either: its pair may be NaN
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const bool in = (live >> (4 * quad + (j < 4 ? j : 12 + j))) & 1;
+        if (!in) s[j / 4][j % 4] = -INFINITY;
+        if (!in) vp[j] = 0;
+      }
     }
-    u = stop;
-    first += units;
-    ++r;
-    __syncthreads();  // the LDS is used again
+    float top = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) top = fmaxf(top, s[j / 4][j % 4]);
+    top = quad_max(top) * cq;
+    if (__any(top > m + kRise)) {
+      const float mn = fmaxf(m, top);
+      const float c = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
+      m = mn;
+      l *= c;
+#pragma unroll
+      for (int j = 0; j < kE; ++j) o[j] *= c;
+    }
+    const float shift = kBias - (m == -INFINITY ? 0.0f : m);
+    half8v p;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float x = __builtin_amdgcn_exp2f(
+          __builtin_fmaf(s[j / 4][j % 4], cq, shift));
+      l += x;
+      p[j] = _Float16(x);
+    }
+    half2v A[4], B[4];  // of keys 2j and 2j + 1 of the lane
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      A[j] = as_half2(__builtin_amdgcn_perm(vp[2 * j + 1], vp[2 * j], 0x05040100));
+      B[j] = as_half2(__builtin_amdgcn_perm(vp[2 * j + 1], vp[2 * j], 0x07060302));
+    }
+#pragma unroll
+    for (int w = 0; w < kE / 4; ++w) {  // four elements at a time
+      half8v f[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        half2v x[4];
+        codes4(__builtin_amdgcn_perm(vc[2 * j + 1][w / 2], vc[2 * j][w / 2],
+                                     w % 2 ? 0x07060302 : 0x05040100),
+               mask, one, x);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const half2v y = __builtin_elementwise_fma(x[e], A[j], B[j]);
+          f[e][2 * j] = y[0];
+          f[e][2 * j + 1] = y[1];
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        o[4 * w + e] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[e], p, o[4 * w + e],
+                                                              0, 0, 0);
+    }
+  };
+
+  const uint32_t ring_at = uint32_t(__builtin_amdgcn_readfirstlane(
+      int(reinterpret_cast<uintptr_t>(LDS_PTR(uint8_t, ring))) + wave * kWave * 16));
+
+  // ---- up to kSegments parts of requests at a time
+  uint64_t u = u0;
+  while (u < u1) {
+    __syncthreads();  // the tables are used again
+    if (wave == 0) {
+      const int mine_r = r + lane;
+      const int64_t len = mine_r < a.num_reqs ? length(mine_r) : 0;
+      const uint64_t units = mine_r < a.num_reqs ? units_of(len) : 0;
+      uint64_t at = units;  // inclusive over the lanes
+      for (int d = 1; d < kWave; d <<= 1) {
+        const uint64_t x = __shfl_up(at, d);
+        if (lane >= d) at += x;
+      }
+      const uint64_t f = first + at - units;  // its first unit
+      const uint64_t ua = f > u ? f : u, ub = f + units < u1 ? f + units : u1;
+      uint32_t k0 = 0, k1 = 0;
+      int steps = 0;
+      if (ua < ub) {
+        const int64_t end = int64_t(ub - f) * unit_keys;
+        k0 = uint32_t(ua - f) * uint32_t(unit_keys);
+        k1 = uint32_t(end < len ? end : len);
+        if (k0 < k1) steps = int((k1 - k0 + step_keys - 1) / step_keys);
+        if (a.spans && set == 0 && ua == f) {
+          const uint64_t last = (f + units) * shares + total - 1;
+          a.spans[mine_r] = int2{worker, int(last / total) - 1};
+        }
+      }
+      int upto_step = steps;
+      for (int d = 1; d < kWave; d <<= 1) {
+        const int x = __shfl_up(upto_step, d);
+        if (lane >= d) upto_step += x;
+      }
+      seg_key0[lane] = k0;
+      seg_key1[lane] = k1;
+      seg_end[lane] = upto_step;
+      seg_flags[lane] = ua < ub ? (ua == f) | (ub == f + units) << 1 : -1;
+      if (lane == kWave - 1) {
+        seg_end[kSegments] = upto_step;
+        lds_first = f + units;
+      }
+    }
+    __syncthreads();
+    const auto read = [](const int &x) __attribute__((always_inline)) { return __builtin_amdgcn_readfirstlane(x); };
+    const int steps = read(seg_end[kSegments]);
+
+    // The result of one part; `room` is a stage of the ring that is free.
+    const auto finish = [&](int part, uint8_t *room) __attribute__((always_inline)) {
+      l = quad_sum(l);
+      // the wavefronts of one head together, in the first of them
+      if (a.wg_blocks > 1) {
+        auto &lds_o = *reinterpret_cast<float(*)[kDecodeWaves / 2][kE][4 * kWave]>(room);
+        if (quad == 0) lds_m[wave][n] = m, lds_l[wave][n] = l;
+        lds_barrier();
+        float mm = m, ll = 0.0f;
+        if (active) {
+          for (int w = hi; w < a.wg_heads * a.wg_blocks; w += a.wg_heads)
+            mm = fmaxf(mm, lds_m[w][n]);
+          for (int w = hi; w < a.wg_heads * a.wg_blocks; w += a.wg_heads)
+            ll += mm == -INFINITY ? 0.0f
+                                  : lds_l[w][n] * __builtin_amdgcn_exp2f(lds_m[w][n] - mm);
+        }
+        const float c = mm == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - mm);
+        m = mm;
+        l = ll;
+#pragma unroll
+        for (int j = 0; j < kE; ++j) o[j] *= c;
+        for (int left = a.wg_blocks; left > 1;) {
+          const int keep = (left + 1) / 2;
+          if (kbi >= keep && kbi < left) {
+#pragma unroll
+            for (int j = 0; j < kE; ++j)
+              *reinterpret_cast<float4v *>(
+                  &lds_o[(kbi - keep) * a.wg_heads + hi][j][4 * lane]) = o[j];
+          }
+          lds_barrier();
+          if (kbi < left - keep) {
+#pragma unroll
+            for (int j = 0; j < kE; ++j)
+              o[j] += *reinterpret_cast<const float4v *>(
+                  &lds_o[kbi * a.wg_heads + hi][j][4 * lane]);
+          }
+          lds_barrier();
+          left = keep;
+        }
+      }
+      const int flags = read(seg_flags[part]), req = r + part;
+      if (kbi == 0 && n < rows) {
+        if (flags == 3) {  // the whole request
+          const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+          uint16_t *out = a.out +
+                          ((int64_t(req) * a.heads + h0 + hi) * a.group + g0 + n) * D +
+                          4 * quad * kE;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float x[kE < 8 ? 8 : kE];
+#pragma unroll
+            for (int j = 0; j < kE; ++j) x[j] = o[j][i] * inv;
+            uint16_t *to = out + i * kE;
+            a.bf16 ? store_out<kE, true>(to, x) : store_out<kE, false>(to, x);
+          }
+        } else {
+          // a share may end one request and start another: two places
+          float *into = a.parts + (((int64_t(set) * a.workers + worker) * 2 + (flags & 1)) *
+                                       a.wg_heads + hi) * part_floats(D);
+          float *to = into + n * D + 4 * quad * kE;
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < kE; j += 4)
+              *reinterpret_cast<float4v *>(to + i * kE + j) =
+                  float4v{o[j][i], o[j + 1][i], o[j + 2][i], o[j + 3][i]};
+          if (quad == 0) {
+            into[D * kQueries + n] = m;
+            into[D * kQueries + kQueries + n] = l;
+          }
+        }
+      }
+      clear();
+    };
+    // zeros for requests without keys, which have no steps
+    for (int p = 0; p < kSegments && read(seg_flags[p]) >= 0; ++p)
+      if (read(seg_end[p]) == (p ? read(seg_end[p - 1]) : 0))
+        for (int i = tid; i < a.wg_heads * rows * (D / 8); i += kDecodeThreads) {
+          const int head = i / (rows * (D / 8)), at = i - head * (rows * (D / 8));
+          uint16_t *out =
+              a.out + ((int64_t(r + p) * a.heads + h0 + head) * a.group + g0) * D;
+          reinterpret_cast<uint4 *>(out)[at] = uint4{0, 0, 0, 0};
+        }
+
+    bool fresh = true;  // the next step starts a part
+    clear();
+    for (int base = 0; base < steps; base += round) {
+      const int count = steps - base < round ? steps - base : round;
+      // ---- the tables of the round's steps
+      __syncthreads();  // those before are done with
+      const auto part_of = [&](int step) __attribute__((always_inline)) {
+        int lo = 0, hi = kSegments - 1;  // the first part that ends after `step`
+        while (lo < hi) {
+          const int mid = (lo + hi) / 2;
+          if (seg_end[mid] > step)
+            hi = mid;
+          else
+            lo = mid + 1;
+        }
+        return lo;
+      };
+      const auto key_of = [&](int part, int step) __attribute__((always_inline)) {
+        const int before = part ? seg_end[part - 1] : 0;
+        return seg_key0[part] + uint32_t(step - before) * uint32_t(step_keys);
+      };
+      for (int i = tid; i < count * step_tiles; i += kDecodeThreads) {
+        const int step = i / step_tiles, part = part_of(base + step);
+        uint32_t key = key_of(part, base + step) +
+                       (uint32_t(i - step * step_tiles) << tile_shift);
+        const uint32_t end = seg_key1[part];
+        key = key < end ? key : (end - 1) >> tile_shift << tile_shift;
+        const uint32_t page = key / uint32_t(a.block_size);
+        int32_t id = a.bt[int64_t(r + part) * a.bt_cols + page];
+        if (id < 0 || id >= a.num_blocks) id = 0;  // some block: its keys are left out
+        tile_at[i] = uint32_t(id) * page_bytes +
+                     uint64_t(key - page * uint32_t(a.block_size)) * slot_bytes;
+      }
+      for (int i = tid; i < count * a.wg_blocks * kBlockKeys; i += kDecodeThreads) {
+        // two blocks a wavefront
+        const int block = i / kBlockKeys, step = block / a.wg_blocks;
+        const int part = part_of(base + step);
+        const uint32_t key = key_of(part, base + step) +
+                             uint32_t(i - step * a.wg_blocks * kBlockKeys);
+        bool in = key < seg_key1[part];
+        if (in) {
+          const int32_t id =
+              a.bt[int64_t(r + part) * a.bt_cols + key / uint32_t(a.block_size)];
+          in = id >= 0 && id < a.num_blocks;
+          if (!in) err = err < LUMEN_ERR_BLOCK_ID ? err : LUMEN_ERR_BLOCK_ID;
+        }
+        const uint64_t bits = __ballot(in);
+        if ((lane & 31) == 0) live_keys[block] = uint32_t(bits >> (lane & 32));
+      }
+      for (int i = tid; i < count; i += kDecodeThreads) {
+        const int part = part_of(base + i);
+        step_part[i] = part | (seg_end[part] == base + i + 1 ? kLast : 0);
+      }
+      __syncthreads();
+
+      // ---- the steps: kStages - 1 under way while one is used, over the ends
+      // of requests too
+      const uint8_t *from[kIssues];  // of the next start, a step ahead
+      const auto prepare = [&](int i) __attribute__((always_inline)) {
+        i = i < count ? i : count - 1;
+#pragma unroll
+        for (int c = 0; c < kIssues; ++c)
+          from[c] = piece[c] + tile_at[i * step_tiles + tile[c]];
+      };
+      const auto start = [&](int i, int stage) __attribute__((always_inline)) {
+        if (i >= count) return;
+        const uint32_t to = ring_at + stage * kStage;
+#pragma unroll
+        for (int c = 0; c < kIssues; ++c)
+          load_to_lds<kStream>(from[c], to + c * kDecodeThreads * 16);
+      };
+      const auto live_of = [&](int i) __attribute__((always_inline)) {
+        return active ? uint32_t(read(int(live_keys[i * a.wg_blocks + kbi]))) : 0u;
+      };
+      int part = read(step_part[0]);
+      uint32_t live = live_of(0);
+      if (fresh) {
+        fetch_q(r + (part & (kLast - 1)));
+        take_q();
+        wait_loads<0>();
+      }
+#pragma unroll
+      for (int i = 0; i < kStages - 1; ++i) {
+        prepare(i);
+        start(i, i);
+      }
+      prepare(kStages - 1);
+      int stage = 0;
+      for (int at = 0; at < count; ++at) {
+        const int behind = count - 1 - at;  // started after this one
+        if (kStages > 2 && behind >= kStages - 2)
+          wait_loads<(kStages - 2) * kIssues>();
+        else if (kStages > 3 && behind == 1)
+          wait_loads<kIssues>();
+        else
+          wait_loads<0>();
+        // everyone's loads of this step have come, and everyone is done with the
+        // stage that the next start fills
+        lds_barrier();
+        start(at + kStages - 1, stage == 0 ? kStages - 1 : stage - 1);
+        prepare(at + kStages);
+        const int next = at + 1 < count ? at + 1 : at;
+        const int next_part = step_part[next];
+        const int next_live = live_keys[next * a.wg_blocks + (active ? kbi : 0)];
+        if (live) use(ring + stage * kStage, live);
+        fresh = part & kLast;
+        if (fresh) {
+          lds_barrier();  // this stage takes the sums
+          finish(part & (kLast - 1), ring + stage * kStage);
+        }
+        part = read(next_part);
+        live = active ? uint32_t(read(next_live)) : 0u;
+        if (fresh && behind > 0) {
+          fetch_q(r + (part & (kLast - 1)));
+          take_q();
+        }
+        stage = stage + 1 < kStages ? stage + 1 : 0;
+      }
+      wait_loads<0>();
+    }
+    u = uniform(lds_first);
+    first = u;
+    r += kSegments;
   }
   record_wave(a.status, err);
 }
@@ -1028,9 +1175,9 @@ struct DecodeKernels {
 };
 
 template <int D>
-DecodeKernels decode_kernels(bool bf16) {
-  return bf16 ? DecodeKernels{decode4_kernel<D, true>, decode4_join_kernel<D, true>}
-              : DecodeKernels{decode4_kernel<D, false>, decode4_join_kernel<D, false>};
+DecodeKernels decode_kernels(bool bf16, bool alone) {
+  return {alone ? decode4_kernel<D, true> : decode4_kernel<D, false>,
+          bf16 ? decode4_join_kernel<D, true> : decode4_join_kernel<D, false>};
 }
 
 template <bool kAppend>
@@ -1217,7 +1364,6 @@ int lumen_attn_decode4(const lumen_kv_layout *layout, int32_t layer,
   a.bt = d_block_tables;
   a.bt_cols = bt_cols;
   a.block_size = bs;
-  a.page_shift = (bs & (bs - 1)) == 0 ? __builtin_ctz(unsigned(bs)) : -1;
   a.num_blocks = layout->num_blocks;
   a.lens = d_lens;
   a.num_reqs = num_reqs;
@@ -1231,14 +1377,14 @@ int lumen_attn_decode4(const lumen_kv_layout *layout, int32_t layer,
   a.wg_heads = plan.wg_heads;
   a.wg_blocks = plan.wg_blocks;
   a.workers = plan.workers;
-  // lines that no other workgroup reads pass the caches by
-  a.stream = a.hnd || plan.wg_heads == a.heads;
+  a.bf16 = dtype == LUMEN_ATTN_BF16;
   a.spans = shared ? static_cast<int2 *>(d_workspace) : nullptr;
   a.parts = reinterpret_cast<float *>(static_cast<char *>(d_workspace) + plan.parts_at);
-  const bool bf = dtype == LUMEN_ATTN_BF16;
-  const DecodeKernels k = at.head_dim == 64    ? decode_kernels<64>(bf)
-                          : at.head_dim == 128 ? decode_kernels<128>(bf)
-                                               : decode_kernels<256>(bf);
+  // lines that no other workgroup reads pass the caches by
+  const bool alone = a.hnd || plan.wg_heads == a.heads;
+  const DecodeKernels k = at.head_dim == 64    ? decode_kernels<64>(a.bf16, alone)
+                          : at.head_dim == 128 ? decode_kernels<128>(a.bf16, alone)
+                                               : decode_kernels<256>(a.bf16, alone);
   hipStream_t s = static_cast<hipStream_t>(stream);
   hipLaunchKernelGGL(k.main, dim3(unsigned(plan.workers * plan.sets)),
                      dim3(kDecodeThreads), 0, s, a);

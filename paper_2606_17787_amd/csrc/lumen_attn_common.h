@@ -58,20 +58,17 @@ __device__ __forceinline__ uint4 pack8(const float *x) {
 
 // ------------------------------------------------------------ other parts
 
-// x of lane l ^ kLanes (16 or 32).  Two results that the compiler is told to
-// be of the same operand are taken by it for one, hence the empty asm.
+// x of lane l and of lane l ^ kLanes (16 or 32), in the same order for both.
+// (The elements are copied out before they are cast: a cast of a vector's
+// element in place reads its first.)
 template <int kLanes>
-__device__ __forceinline__ float swapped(float x) {
+__device__ __forceinline__ void both(float x, float *a, float *b) {
   const uint32_t u = __builtin_bit_cast(uint32_t, x);
-  uint32_t w = u;
-  asm("" : "+v"(w));
-  if constexpr (kLanes == 16) {
-    const auto r = __builtin_amdgcn_permlane16_swap(u, w, false, false);
-    return __builtin_bit_cast(float, (threadIdx.x & 16) ? r[0] : r[1]);
-  } else {
-    const auto r = __builtin_amdgcn_permlane32_swap(u, w, false, false);
-    return __builtin_bit_cast(float, (threadIdx.x & 32) ? r[0] : r[1]);
-  }
+  const auto r = kLanes == 16 ? __builtin_amdgcn_permlane16_swap(u, u, false, false)
+                              : __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  const uint32_t r0 = r[0], r1 = r[1];
+  *a = __builtin_bit_cast(float, r0);
+  *b = __builtin_bit_cast(float, r1);
 }
 
 // lumen_attn_rows, typed.

@@ -295,7 +295,9 @@ __global__ __launch_bounds__(kThreads) void prompt_kernel(PromptArgs a) {
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[t][i]);
-    top = fmaxf(top, swapped<32>(top)) * a.scale_log2;
+    float ta, tb;
+    both<32>(top, &ta, &tb);
+    top = fmaxf(ta, tb) * a.scale_log2;
     if (__any(top > m + kSlack)) {
       const float mn = fmaxf(m, top);
       const float c = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
@@ -337,7 +339,9 @@ __global__ __launch_bounds__(kThreads) void prompt_kernel(PromptArgs a) {
       }
   }
   if (!here) return;
-  l += swapped<32>(l);
+  float la, lb;
+  both<32>(l, &la, &lb);
+  l = la + lb;
   const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
   uint16_t *out = a.out + ((q0 + tok) * a.q_heads + hq) * D;
 #pragma unroll
