@@ -455,6 +455,9 @@ template <int kLeft>
 __device__ __forceinline__ void wait_loads() {
   asm volatile("s_waitcnt vmcnt(%0)" :: "i"(kLeft) : "memory");
 }
+__device__ __forceinline__ void wait_lds() {
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+}
 // A barrier after the wavefront's own LDS reads, with loads under way.
 __device__ __forceinline__ void lds_barrier() {
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -467,6 +470,10 @@ __device__ __forceinline__ uint64_t uniform(uint64_t x) {
   return uint64_t(__builtin_amdgcn_readfirstlane(uint32_t(x))) |
          uint64_t(__builtin_amdgcn_readfirstlane(uint32_t(x >> 32))) << 32;
 }
+
+// What a wavefront's rows share: the workgroup's other heads' places and cache
+// lines that other workgroups read too; only the places; nothing.
+enum class Sharing { kLines, kStep, kNone };
 
 // Decode attention, bound by the cache's bytes: D/2 + 16 a row, read once.
 //
@@ -494,8 +501,10 @@ __device__ __forceinline__ uint64_t uniform(uint64_t x) {
 // lane holds D/16 consecutive elements of 8 keys, all of one quarter.  Values
 // are exact: code and pair give the stored value by one fused multiply-add that
 // rounds as the format says.
-template <int D, bool kStream>
+template <int D, Sharing kSharing>
 __global__ __launch_bounds__(kDecodeThreads, 2) void decode4_kernel(DecodeArgs a) {
+  constexpr bool kPrivate = kSharing == Sharing::kNone;
+  constexpr bool kStream = kSharing != Sharing::kLines;
   constexpr int kRow = D / 2 + 16;
   constexpr int kSteps = D / 32;  // products over head_dim
   constexpr int kE = D / 16;      // elements of V a lane holds of a key
@@ -604,13 +613,15 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void decode4_kernel(DecodeArgs a
   const uint8_t *piece[kIssues]; // its place in a tile at byte 0
 #pragma unroll
   for (int i = 0; i < kIssues; ++i) {
-    const int half = step_keys * pieces;
-    int c = i * kDecodeThreads + tid;
+    // kNone: a wavefront loads its own block's rows
+    const int half = kPrivate ? kBlockKeys * kParts : step_keys * pieces;
+    int c = kPrivate ? i * kWave + lane : i * kDecodeThreads + tid;
     const bool is_v = c >= half;
     c = is_v ? c - half : c;
     c = c < half ? c : half - 1;  // lanes past the step's end repeat a piece
-    const int t = c / pieces;
+    int t = c / pieces;
     int x = c - t * pieces - turn(t);
+    if (kPrivate) t += kbi * kBlockKeys;
     x = x < 0 ? x + pieces : x;
     tile[i] = t >> tile_shift;
     piece[i] = (is_v ? a.v : a.k) + (t & ((1 << tile_shift) - 1)) * slot_bytes +
@@ -630,7 +641,7 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void decode4_kernel(DecodeArgs a
   // offsets into a stage of what the lane reads: K of key n, the same for n + 16;
   // V of keys 4 quad + 0, 1 and + 2, 3, the same for + 16
   constexpr int kVBytes = kE / 2;  // of V's codes
-  const int t0 = (active ? kbi : 0) * kBlockKeys;
+  const int t0 = kPrivate ? 0 : (active ? kbi : 0) * kBlockKeys;
   uint32_t at_k[D == 256 ? 2 : 1], at_v[2], at_kp, at_vp[2];
   at_k[0] = place(t0 + n, quad * (D / 8) / 16) + quad * (D / 8) % 16;
   if constexpr (D == 256) at_k[1] = place(t0 + n, quad * 2 + 1);
@@ -642,7 +653,9 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void decode4_kernel(DecodeArgs a
   }
   // (turn() is the same for keys 2j and 2j + 1 wherever it is not 0: `even` is
   // at most 8 for any number of pieces of up to 8 heads)
-  const uint32_t key_bytes = pieces * 16, v_at = step_keys * key_bytes;
+  const uint32_t key_bytes = pieces * 16;
+  const uint32_t v_at = (kPrivate ? kBlockKeys : step_keys) * key_bytes;
+  constexpr int kOwn = 2 * kBlockKeys * kRow;  // bytes of a wavefront's block
 
   // ---- Q: 16-bit floats under a power of two of the row's own, so that bf16
   // and fp16 keep all their bits whatever their range
@@ -689,40 +702,24 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void decode4_kernel(DecodeArgs a
   };
 
   const auto use = [&](const uint8_t *stage, uint32_t live) __attribute__((always_inline)) {
-    float4v s[2];
+    // everything the block reads, at once: one wait instead of one for each
+    uint32_t kc[2][kSteps], kp[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      s[t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
       const uint8_t *row = stage + 16 * t * key_bytes;
-      const half2v pair = as_half2(*reinterpret_cast<const uint32_t *>(row + at_kp));
-      uint32_t codes[kSteps];
+      kp[t] = *reinterpret_cast<const uint32_t *>(row + at_kp);
       if constexpr (D == 64) {
         const uint2 x = *reinterpret_cast<const uint2 *>(row + at_k[0]);
-        codes[0] = x.x, codes[1] = x.y;
+        kc[t][0] = x.x, kc[t][1] = x.y;
       } else {
 #pragma unroll
         for (int i = 0; i < kSteps; i += 4) {
           const uint4 x = *reinterpret_cast<const uint4 *>(row + at_k[i / 4]);
-          codes[i] = x.x, codes[i + 1] = x.y, codes[i + 2] = x.z, codes[i + 3] = x.w;
+          kc[t][i] = x.x, kc[t][i + 1] = x.y, kc[t][i + 2] = x.z, kc[t][i + 3] = x.w;
         }
-      }
-      const half2v A = {pair[0], pair[0]}, B = {pair[1], pair[1]};
-#pragma unroll
-      for (int i = 0; i < kSteps; ++i) {
-        half2v x[4];
-        codes4(codes[i], mask, one, x);
-        half8v f;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const half2v y = __builtin_elementwise_fma(x[j], A, B);
-          f[2 * j] = y[0];
-          f[2 * j + 1] = y[1];
-        }
-        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f, q[i], s[t], 0, 0, 0);
       }
     }
-    // V: the lane's elements of 8 keys
-    uint32_t vc[8][kE >= 8 ? kE / 8 : 1], vp[8];
+    uint32_t vc[8][kE >= 8 ? kE / 8 : 1], vp[8];  // V: the lane's elements of 8 keys
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const uint8_t *row = stage + v_at + ((j & 1) + (j & 4) * 4) * key_bytes;
@@ -735,6 +732,27 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void decode4_kernel(DecodeArgs a
       } else {
         const uint2 x = *reinterpret_cast<const uint2 *>(row);
         vc[j][0] = x.x, vc[j][kE / 8 - 1] = x.y;
+      }
+    }
+    if constexpr (D != 256) __builtin_amdgcn_sched_barrier(0);
+    float4v s[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      s[t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+      const half2v pair = as_half2(kp[t]);
+      const half2v A = {pair[0], pair[0]}, B = {pair[1], pair[1]};
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i) {
+        half2v x[4];
+        codes4(kc[t][i], mask, one, x);
+        half8v f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const half2v y = __builtin_elementwise_fma(x[j], A, B);
+          f[2 * j] = y[0];
+          f[2 * j + 1] = y[1];
+        }
+        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f, q[i], s[t], 0, 0, 0);
       }
     }
     if (live != 0xffffffffu) {
@@ -797,7 +815,8 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void decode4_kernel(DecodeArgs a
   };
 
   const uint32_t ring_at = uint32_t(__builtin_amdgcn_readfirstlane(
-      int(reinterpret_cast<uintptr_t>(LDS_PTR(uint8_t, ring))) + wave * kWave * 16));
+      int(reinterpret_cast<uintptr_t>(LDS_PTR(uint8_t, ring))) +
+      wave * (kPrivate ? kOwn : kWave * 16)));
 
   // ---- up to kSegments parts of requests at a time
   uint64_t u = u0;
@@ -997,7 +1016,7 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void decode4_kernel(DecodeArgs a
         const uint32_t to = ring_at + stage * kStage;
 #pragma unroll
         for (int c = 0; c < kIssues; ++c)
-          load_to_lds<kStream>(from[c], to + c * kDecodeThreads * 16);
+          load_to_lds<kStream>(from[c], to + c * (kPrivate ? kWave : kDecodeThreads) * 16);
       };
       const auto live_of = [&](int i) __attribute__((always_inline)) {
         return active ? uint32_t(read(int(live_keys[i * a.wg_blocks + kbi]))) : 0u;
@@ -1025,14 +1044,18 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void decode4_kernel(DecodeArgs a
         else
           wait_loads<0>();
         // everyone's loads of this step have come, and everyone is done with the
-        // stage that the next start fills
-        lds_barrier();
+        // stage that the next start fills; a wavefront that reads only what it
+        // loaded waits for itself alone, and runs ahead while others wait
+        if constexpr (kPrivate)
+          wait_lds();
+        else
+          lds_barrier();
         start(at + kStages - 1, stage == 0 ? kStages - 1 : stage - 1);
         prepare(at + kStages);
         const int next = at + 1 < count ? at + 1 : at;
         const int next_part = step_part[next];
         const int next_live = live_keys[next * a.wg_blocks + (active ? kbi : 0)];
-        if (live) use(ring + stage * kStage, live);
+        if (live) use(ring + stage * kStage + (kPrivate ? wave * kOwn : 0), live);
         fresh = part & kLast;
         if (fresh) {
           lds_barrier();  // this stage takes the sums
@@ -1175,8 +1198,10 @@ struct DecodeKernels {
 };
 
 template <int D>
-DecodeKernels decode_kernels(bool bf16, bool alone) {
-  return {alone ? decode4_kernel<D, true> : decode4_kernel<D, false>,
+DecodeKernels decode_kernels(bool bf16, Sharing sharing) {
+  return {sharing == Sharing::kNone   ? decode4_kernel<D, Sharing::kNone>
+          : sharing == Sharing::kStep ? decode4_kernel<D, Sharing::kStep>
+                                      : decode4_kernel<D, Sharing::kLines>,
           bf16 ? decode4_join_kernel<D, true> : decode4_join_kernel<D, false>};
 }
 
@@ -1380,11 +1405,12 @@ int lumen_attn_decode4(const lumen_kv_layout *layout, int32_t layer,
   a.bf16 = dtype == LUMEN_ATTN_BF16;
   a.spans = shared ? static_cast<int2 *>(d_workspace) : nullptr;
   a.parts = reinterpret_cast<float *>(static_cast<char *>(d_workspace) + plan.parts_at);
-  // lines that no other workgroup reads pass the caches by
-  const bool alone = a.hnd || plan.wg_heads == a.heads;
-  const DecodeKernels k = at.head_dim == 64    ? decode_kernels<64>(a.bf16, alone)
-                          : at.head_dim == 128 ? decode_kernels<128>(a.bf16, alone)
-                                               : decode_kernels<256>(a.bf16, alone);
+  const Sharing sharing = plan.wg_heads == 1         ? Sharing::kNone
+                          : plan.wg_heads == a.heads ? Sharing::kStep
+                                                     : Sharing::kLines;
+  const DecodeKernels k = at.head_dim == 64    ? decode_kernels<64>(a.bf16, sharing)
+                          : at.head_dim == 128 ? decode_kernels<128>(a.bf16, sharing)
+                                               : decode_kernels<256>(a.bf16, sharing);
   hipStream_t s = static_cast<hipStream_t>(stream);
   hipLaunchKernelGGL(k.main, dim3(unsigned(plan.workers * plan.sets)),
                      dim3(kDecodeThreads), 0, s, a);
