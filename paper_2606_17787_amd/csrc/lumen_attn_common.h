@@ -71,6 +71,40 @@ __device__ __forceinline__ void both(float x, float *a, float *b) {
   *b = __builtin_bit_cast(float, r1);
 }
 
+// Starts a load of 16 bytes a lane from the lane's address into LDS, at byte
+// `to` + 16 * lane (`to` the wavefront's; kStream: not to be kept in caches).  It is counted like any load, but the
+// compiler does not know of it: wait_loads<n> waits until at most the last n
+// are still under way, and keeps reads of the LDS behind it.  That, unlike the
+// builtin, lets a read wait for its own block alone.
+template <bool kStream>
+__device__ __forceinline__ void load_to_lds(const void *from, uint32_t to) {
+  if constexpr (kStream)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt"
+                 :: "s"(to), "v"(from) : "memory");
+  else
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+                 :: "s"(to), "v"(from) : "memory");
+}
+template <int kLeft>
+__device__ __forceinline__ void wait_loads() {
+  asm volatile("s_waitcnt vmcnt(%0)" :: "i"(kLeft) : "memory");
+}
+__device__ __forceinline__ void wait_lds() {
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+}
+// A barrier after the wavefront's own LDS reads, with loads under way.
+__device__ __forceinline__ void lds_barrier() {
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+#define LDS_PTR(T, p) ((__attribute__((address_space(3))) T *)(p))
+
+// A value that is the same in all lanes, in scalar registers.
+__device__ __forceinline__ uint64_t uniform(uint64_t x) {
+  return uint64_t(__builtin_amdgcn_readfirstlane(uint32_t(x))) |
+         uint64_t(__builtin_amdgcn_readfirstlane(uint32_t(x >> 32))) << 32;
+}
+
 // lumen_attn_rows, typed.
 struct Rows {
   uint16_t *base;

@@ -42,13 +42,11 @@ __device__ __forceinline__ f32x16 mfma(frag8 a, frag8 b, f32x16 c) {
         __builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 
-#define LDS_PTR(T, p) ((__attribute__((address_space(3))) T *)(p))
-#define GLOBAL_PTR(T, p) ((const __attribute__((address_space(1))) T *)(p))
-
 constexpr int kWaves = 8;
 constexpr int kThreads = kWaves * kWave;
 constexpr int kKeys = 64;  // keys of a tile
 constexpr float kSlack = 8.0f;
+constexpr int kMfma = 0x8, kDsRead = 0x100;  // of sched_group_barrier
 
 template <int D>
 __device__ __forceinline__ int swizzle_k(int row) {
@@ -232,23 +230,26 @@ __global__ __launch_bounds__(kThreads) void prompt_kernel(PromptArgs a) {
       q[i] = *reinterpret_cast<const frag8 *>(p + 16 * i);
   }
 
+  // the queries are here before the first tile's loads, which the compiler does
+  // not count, so that no wait for them is left in the loop
+  __builtin_amdgcn_s_waitcnt(0x0f70);
+
   const uint16_t *kb = a.k.base + k0 * a.k.token + hk * a.k.head;
   const uint16_t *vb = a.v.base + k0 * a.v.token + hk * a.v.head;
-  const auto load = [&](int step, int buf) {
+  const uint32_t lds_at = uint32_t(__builtin_amdgcn_readfirstlane(
+      int(reinterpret_cast<uintptr_t>(LDS_PTR(uint16_t, lds))) + wave * kWave * 16));
+  const auto load = [&](int step, int buf) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < kIssues; ++i) {
       const int at = i * kThreads + wave * 64;
       const int row = (at + lane) / kChunks, pos = (at + lane) % kChunks;
       int key = step * kKeys + row;
       key = key < nk ? key : nk - 1;  // rows past the end repeat the last key
-      __builtin_amdgcn_global_load_lds(
-          GLOBAL_PTR(uint32_t, kb + int64_t(key) * a.k.token +
-                                   8 * (pos ^ swizzle_k<D>(row))),
-          LDS_PTR(uint32_t, &lds[buf][0][at * 8]), 16, 0, 0);
-      __builtin_amdgcn_global_load_lds(
-          GLOBAL_PTR(uint32_t, vb + int64_t(key) * a.v.token +
-                                   8 * (pos ^ swizzle_v<D>(row))),
-          LDS_PTR(uint32_t, &lds[buf][1][at * 8]), 16, 0, 0);
+      const uint32_t to = lds_at + (buf * 2 * kTile + i * kThreads * 8) * 2;
+      load_to_lds<false>(kb + int64_t(key) * a.k.token + 8 * (pos ^ swizzle_k<D>(row)),
+                         to);
+      load_to_lds<false>(vb + int64_t(key) * a.v.token + 8 * (pos ^ swizzle_v<D>(row)),
+                         to + kTile * 2);
     }
   };
 
@@ -262,24 +263,39 @@ __global__ __launch_bounds__(kThreads) void prompt_kernel(PromptArgs a) {
   if (steps > 0) load(0, 0);
   for (int step = 0; step < steps; ++step) {
     const int buf = step & 1;
-    __builtin_amdgcn_s_waitcnt(0);
-    __syncthreads();
+    wait_loads<0>();
+    lds_barrier();
     if (step + 1 < steps) load(step + 1, buf ^ 1);
     if (step >= wave_steps) continue;
     // ---- scores, keys down and queries across
     f32x16 sc[2];
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
+    for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int i = 0; i < 16; ++i) sc[t][i] = 0.0f;
+    // the second half's keys are read while the first half's products run
+    frag8 k[D / 16];
+    const auto key_row = [&](int t, int i) __attribute__((always_inline)) {
       const int row = t * 32 + col;
+      return *reinterpret_cast<const frag8 *>(
+          &lds[buf][0][row * D + 8 * ((2 * i + half) ^ swizzle_k<D>(row))]);
+    };
 #pragma unroll
-      for (int i = 0; i < D / 16; ++i) {
-        const frag8 k = *reinterpret_cast<const frag8 *>(
-            &lds[buf][0][row * D + 8 * ((2 * i + half) ^ swizzle_k<D>(row))]);
-        sc[t] = mfma<kBf16>(k, q[i], sc[t]);
-      }
+    for (int i = 0; i < D / 16; ++i) k[i] = key_row(0, i);
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) {
+      sc[0] = mfma<kBf16>(k[i], q[i], sc[0]);
+      k[i] = key_row(1, i);
     }
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) sc[1] = mfma<kBf16>(k[i], q[i], sc[1]);
+    __builtin_amdgcn_sched_group_barrier(kDsRead, D / 16, 0);
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) {
+      __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(kDsRead, 1, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(kMfma, D / 16, 0);
     if (step * kKeys + kKeys - 1 > w0 + behind) {
 #pragma unroll
       for (int t = 0; t < 2; ++t)
