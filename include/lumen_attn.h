@@ -63,6 +63,9 @@ extern "C" {
  * lengths into LDS. */
 #define LUMEN_ATTN_MAX_REQS 4096
 
+/* Most query tokens, and most key tokens, of one prompt call. */
+#define LUMEN_ATTN_MAX_TOKENS 134217728
+
 /* Magnitude to which append4 holds an element. */
 #define LUMEN_ATTN_KV4_MAX 6848
 
@@ -154,6 +157,14 @@ int lumen_attn_decode4(const lumen_kv_layout *layout, int32_t layer,
                        void *d_out, void *d_workspace, size_t workspace_bytes,
                        int32_t *d_status, lumen_stream_t stream);
 
+/* Bytes of workspace with which a prompt call may cut long sequences' keys into
+ * parts (0 where it would not, and for sizes it refuses). */
+size_t lumen_attn_prompt_workspace_bytes(int32_t num_seqs, int64_t num_q_tokens,
+                                         int64_t num_k_tokens,
+                                         int32_t num_q_heads,
+                                         int32_t num_kv_heads,
+                                         int32_t head_dim);
+
 /* Causal attention over packed sequences.  Sequence s has queries [d_cu_q[s],
  * d_cu_q[s+1]) and keys [d_cu_k[s], d_cu_k[s+1]) (d_cu_k NULL: d_cu_q), aligned
  * at their ends: with n queries and m keys, query i sees keys j <= i + m - n.
@@ -164,14 +175,20 @@ int lumen_attn_decode4(const lumen_kv_layout *layout, int32_t layer,
  * tokens in no sequence are not written.  head_dim 64 or 128.  scale finite
  * and above 0.  A sequence whose bounds fall outside [0, num_q_tokens] or [0,
  * num_k_tokens], or end before they begin, is skipped (RANGE).  Sequences must
- * not share queries. */
+ * not share queries.  Token counts at most LUMEN_ATTN_MAX_TOKENS.  d_workspace:
+ * lumen_attn_prompt_workspace_bytes bytes, 16-byte aligned, not shared by calls in
+ * flight at the same time; what it holds does not matter.  With it, the keys of
+ * long sequences with few queries are shared by several workgroups; NULL: they
+ * are not, and the rounding of their sums differs.  The result does not depend on
+ * timing. */
 int lumen_attn_prompt(const lumen_attn_rows *q, const lumen_attn_rows *k,
                       const lumen_attn_rows *v, int32_t dtype,
                       const int32_t *d_cu_q, const int32_t *d_cu_k,
                       int32_t num_seqs, int64_t num_q_tokens,
                       int64_t num_k_tokens, int32_t num_q_heads,
                       int32_t num_kv_heads, int32_t head_dim, float scale,
-                      void *d_out, int32_t *d_status, lumen_stream_t stream);
+                      void *d_out, void *d_workspace, size_t workspace_bytes,
+                      int32_t *d_status, lumen_stream_t stream);
 
 #ifdef __cplusplus
 }

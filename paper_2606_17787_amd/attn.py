@@ -23,6 +23,7 @@ HEADER = os.path.join(os.path.dirname(_kv.HEADER), "lumen_attn.h")
 LUMEN_ATTN_BF16 = 0
 LUMEN_ATTN_FP16 = 1
 LUMEN_ATTN_MAX_REQS = 4096  # include/lumen_attn.h
+LUMEN_ATTN_MAX_TOKENS = 134217728  # include/lumen_attn.h
 LUMEN_ATTN_KV4_MAX = 6848  # include/lumen_attn.h
 
 _DTYPES = {torch.bfloat16: LUMEN_ATTN_BF16, torch.float16: LUMEN_ATTN_FP16}
@@ -67,7 +68,9 @@ def _lib():
                                 f32, p, p, sz, p, p]),
         "lumen_attn_prompt": (ctypes.c_int,
                               [rows, rows, rows, i32, p, p, i32, i64, i64,
-                               i32, i32, i32, f32, p, p, p]),
+                               i32, i32, i32, f32, p, p, sz, p, p]),
+        "lumen_attn_prompt_workspace_bytes": (sz, [i32, i64, i64, i32, i32,
+                                                   i32]),
     }
     for name, (res, args) in sigs.items():
         f = getattr(lib, name)
@@ -319,7 +322,25 @@ def prepare_decode4(shape, num_blocks, layer, cache, block_tables, lens, q,
                      (cache, block_tables, lens, q, out, workspace, status))
 
 
-def _prompt_args(q, k, v, out, cu_q, status, cu_k, scale):
+def lumen_attn_prompt_workspace_bytes(num_seqs: int, num_q_tokens: int,
+                                      num_k_tokens: int, num_q_heads: int,
+                                      num_kv_heads: int,
+                                      head_dim: int) -> int:
+    return int(_lib().lumen_attn_prompt_workspace_bytes(
+        num_seqs, num_q_tokens, num_k_tokens, num_q_heads, num_kv_heads,
+        head_dim))
+
+
+def new_prompt_workspace(q: torch.Tensor, k: torch.Tensor,
+                         num_seqs: int) -> Optional[torch.Tensor]:
+    """Workspace for prompt calls of these sizes; None where they take
+    none."""
+    n = lumen_attn_prompt_workspace_bytes(num_seqs, q.shape[0], k.shape[0],
+                                          q.shape[1], k.shape[1], q.shape[2])
+    return torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
+
+
+def _prompt_args(q, k, v, out, cu_q, status, cu_k, scale, workspace):
     if q.dim() != 3 or k.dim() != 3:
         raise ValueError("q, k and v are [tokens, heads, head_dim]")
     D, H = q.shape[2], k.shape[1]
@@ -336,7 +357,17 @@ def _prompt_args(q, k, v, out, cu_q, status, cu_k, scale):
             _kv._dev(cu_q, "cu_q", torch.int32),
             None if cu_k is None else _kv._dev(cu_k, "cu_k", torch.int32),
             cu_q.numel() - 1, q.shape[0], k.shape[0], q.shape[1], H, D,
-            _scale(scale, D), _out(out, q.shape, q.dtype), _status(status))
+            _scale(scale, D), _out(out, q.shape, q.dtype),
+            None if workspace is None else _kv._dev(workspace, "workspace"),
+            0 if workspace is None else _kv._nbytes(workspace),
+            _status(status))
+
+
+def _own_workspace(q, k, cu_q, workspace):
+    """The caller's workspace, or one of the call's own."""
+    if workspace is None and q.is_cuda and k.dim() == q.dim() == 3:
+        return new_prompt_workspace(q, k, cu_q.numel() - 1)
+    return workspace
 
 
 def lumen_attn_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
@@ -344,17 +375,28 @@ def lumen_attn_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
                       status: torch.Tensor,
                       cu_k: Optional[torch.Tensor] = None,
                       scale: Optional[float] = None,
+                      workspace: Optional[torch.Tensor] = None,
                       stream: Optional[torch.cuda.Stream] = None) -> None:
     """Causal attention over packed sequences, q [Tq, Hq, D], k and v
     [Tk, H, D], into out [Tq, Hq, D] (cu_k None: the keys are the queries'
-    own tokens)."""
+    own tokens).  workspace None: one is allocated for the call, on the
+    stream it runs on."""
+    if stream is not None and workspace is None:
+        with torch.cuda.stream(stream):
+            workspace = _own_workspace(q, k, cu_q, None)
+    workspace = _own_workspace(q, k, cu_q, workspace)
     _call("lumen_attn_prompt",
-          _prompt_args(q, k, v, out, cu_q, status, cu_k, scale), stream)
+          _prompt_args(q, k, v, out, cu_q, status, cu_k, scale, workspace),
+          stream)
 
 
-def prepare_prompt(q, k, v, out, cu_q, status, cu_k=None,
-                   scale=None) -> "_kv.PreparedCall":
-    """lumen_attn_prompt with its arguments checked once."""
+def prepare_prompt(q, k, v, out, cu_q, status, cu_k=None, scale=None,
+                   workspace=None) -> "_kv.PreparedCall":
+    """lumen_attn_prompt with its arguments checked once; workspace None: one
+    is allocated and kept, so the object must not be in flight twice at a
+    time."""
+    workspace = _own_workspace(q, k, cu_q, workspace)
     return _prepared("lumen_attn_prompt",
-                     _prompt_args(q, k, v, out, cu_q, status, cu_k, scale),
-                     (q, k, v, out, cu_q, status, cu_k))
+                     _prompt_args(q, k, v, out, cu_q, status, cu_k, scale,
+                                  workspace),
+                     (q, k, v, out, cu_q, status, cu_k, workspace))

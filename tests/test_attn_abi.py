@@ -38,7 +38,8 @@ def test_exports_every_declared_entry_point(lib):
     assert set(names) == {"lumen_attn_slots", "lumen_attn_append4",
                           "lumen_attn_read4", "lumen_attn_decode4",
                           "lumen_attn_decode4_workspace_bytes",
-                          "lumen_attn_prompt"}
+                          "lumen_attn_prompt",
+                          "lumen_attn_prompt_workspace_bytes"}
     for n in names:
         assert hasattr(lib, n), n
 
@@ -154,10 +155,11 @@ def test_decode_workspace_bytes(lib):
 def test_prompt_refusals(lib):
     def call(q=None, k=None, v=None, dtype=0, cu_q=FAKE, cu_k=FAKE, S=2,
              tq=10, tk=10, hq=8, h=2, d=128, scale=0.1, out=FAKE,
-             status=FAKE):
+             status=FAKE, ws=None, wsb=0):
         q, k, v = (rows() if x is None else x for x in (q, k, v))
         return lib.lumen_attn_prompt(q, k, v, dtype, cu_q, cu_k, S, tq, tk,
-                                     hq, h, d, scale, out, status, None)
+                                     hq, h, d, scale, out, ws, wsb, status,
+                                     None)
     for kw in (dict(S=-1), dict(tq=-1), dict(tk=-1), dict(hq=0), dict(h=0),
                dict(h=3), dict(scale=0.0), dict(scale=float("nan")),
                dict(scale=float("inf")), dict(cu_q=None), dict(out=None),
@@ -175,6 +177,17 @@ def test_prompt_refusals(lib):
         assert call(**kw) == kv.LUMEN_ERR_MISALIGNED, kw
     assert call(S=0, cu_q=None, tq=0, tk=0, out=None, q=rows(None),
                 k=rows(None), v=rows(None)) == kv.LUMEN_OK
+
+
+def test_prompt_workspace(lib):
+    f = lib.lumen_attn_prompt_workspace_bytes
+    assert f(2, 10, 10, 8, 2, 128) == 0 and f(2, 10, 9000, 8, 2, 96) == 0
+    assert f(2, 10, 9000, 8, 3, 128) == 0 and f(-1, 10, 9000, 8, 2, 128) == 0
+    most = 0
+    for s, tq, tk in ((1, 1, 5000), (3, 100, 100000), (9, 1 << 27, 1 << 27)):
+        n = f(s, tq, tk, 8, 2, 128)
+        assert 0 < n < 1 << 28 and n >= most
+        most = n
 
 
 def test_binding_refuses_host_tensors_and_shapes():
