@@ -157,8 +157,9 @@ int lumen_attn_decode4(const lumen_kv_layout *layout, int32_t layer,
                        void *d_out, void *d_workspace, size_t workspace_bytes,
                        int32_t *d_status, lumen_stream_t stream);
 
-/* Bytes of workspace with which a prompt call may cut long sequences' keys into
- * parts (0 where it would not, and for sizes it refuses). */
+/* Bytes of workspace that a prompt call needs: for its plan, and for partial
+ * results where it may cut long sequences' keys into parts (0 for small calls,
+ * which need none, and for sizes it refuses). */
 size_t lumen_attn_prompt_workspace_bytes(int32_t num_seqs, int64_t num_q_tokens,
                                          int64_t num_k_tokens,
                                          int32_t num_q_heads,
@@ -176,11 +177,9 @@ size_t lumen_attn_prompt_workspace_bytes(int32_t num_seqs, int64_t num_q_tokens,
  * and above 0.  A sequence whose bounds fall outside [0, num_q_tokens] or [0,
  * num_k_tokens], or end before they begin, is skipped (RANGE).  Sequences must
  * not share queries.  Token counts at most LUMEN_ATTN_MAX_TOKENS.  d_workspace:
- * lumen_attn_prompt_workspace_bytes bytes, 16-byte aligned, not shared by calls in
- * flight at the same time; what it holds does not matter.  With it, the keys of
- * long sequences with few queries are shared by several workgroups; NULL: they
- * are not, and the rounding of their sums differs.  The result does not depend on
- * timing. */
+ * lumen_attn_prompt_workspace_bytes bytes (NULL where that is 0), 16-byte aligned,
+ * not shared by calls in flight at the same time; what it holds does not matter.
+ * The result does not depend on timing. */
 int lumen_attn_prompt(const lumen_attn_rows *q, const lumen_attn_rows *k,
                       const lumen_attn_rows *v, int32_t dtype,
                       const int32_t *d_cu_q, const int32_t *d_cu_k,

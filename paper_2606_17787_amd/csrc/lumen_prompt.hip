@@ -13,19 +13,37 @@ namespace {
 
 using namespace lumen_attn_detail;
 
+// A workgroup's work: queries [t0, t0 + tile) of a sequence against its keys'
+// steps [first, last).
+struct Unit {
+  int32_t q0, nq, k0, nk;  // the sequence; nq 0: no work
+  int32_t t0, first, last;
+  int32_t place;  // of its result among the parts, or -1: it is the whole
+};
+
+// A tile that was cut: its first unit, and how many there are.
+struct Cut {
+  int32_t unit, parts;
+};
+
 struct PromptArgs {
   Rows q, k, v;
   const int32_t *cu_q, *cu_k;
   int32_t num_seqs;
   int64_t num_q, num_k;
   int32_t q_heads, kv_heads;
-  int32_t heads_per_tile;
-  uint32_t slots;  // workgroups that run at once, a set of heads; 0: no tile is cut
+  int32_t heads_per_tile, tile_tokens;
   float scale_log2;  // scale * log2(e)
   uint16_t *out;
   int32_t *status;
-  float *parts;  // [max_parts][part_floats]
-  uint32_t max_parts;  // parts of cut tiles, times sets of heads
+  // the plan; units is NULL where the kernel finds its unit itself
+  Unit *units;
+  int32_t num_units;  // room, for one set of heads
+  int32_t slots;      // workgroups that run at once, for one set of heads
+  int32_t *num_cuts;
+  Cut *cuts;
+  int32_t max_parts;  // room, for one set of heads; 0: no tile is cut
+  float *parts;       // [max_parts][sets of heads][part_floats]
 };
 
 // 16-bit fragments of the matrix instructions, and their products.
@@ -46,6 +64,8 @@ __device__ __forceinline__ f32x16 mfma(frag8 a, frag8 b, f32x16 c) {
 }
 
 constexpr int kKeys = 64;  // keys of a tile
+#define CONSTANT_PTR(T, p) ((const __attribute__((address_space(4))) T *)(p))
+
 constexpr float kSlack = 8.0f;
 constexpr int kMfma = 0x8, kDsRead = 0x100;  // of sched_group_barrier
 
@@ -59,210 +79,222 @@ __device__ __forceinline__ int swizzle_v(int row) {
   return D == 128 ? (row & 3) * 4 + ((row & 2) ? 2 : 0) : (row & 3) * 2;
 }
 
-// Sum over the wavefront's lanes, the same in all of them.
-__device__ __forceinline__ uint32_t wave_sum(uint32_t x) {
-  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);  // row_shr 1
-  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, true);  // row_bcast 15
-  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, true);  // row_bcast 31
-  return __builtin_amdgcn_readlane(x, 63);
-}
-
-// Tiles of at least this many keys may be cut: shorter parts would cost more to
-// start and to join than they save.
+// Tiles are cut into parts of at least this many keys: shorter ones would cost
+// more to start and to join than they save.
 constexpr int kMinPartKeys = 512;
-// Keys of a call from which on tiles may be cut: below, the second launch that
-// joins them costs what it saves.
+// Keys of a call from which on tiles may be cut.
 constexpr int kCutKeys = 2048;
 
-// A part of a query tile's keys: tile `tile` of sequence `seq`, part `part` of
-// `parts`, each of `levels` levels; `first` is its tile's first part's place in
-// the order of all parts.
-struct Part {
-  int seq, tile, part, parts, levels;
-  uint32_t first;
+__device__ __forceinline__ int steps_to(int keys) {
+  return keys > 0 ? (keys + kKeys - 1) / kKeys : 0;
+}
+
+// One sequence of a call.
+struct Sequence {
+  int64_t q0, k0;
+  int nq, nk;
+  int tiles;  // of queries
 };
 
-// The order of work.  Tile t of a sequence with `behind` keys before its first
-// query sees about (t + 1) tiles of keys more than behind: its level.  Tiles go
-// by falling level, those of one level in the order of their sequences' threads,
-// so that the long ones start first and the short ones fill the end.  A tile of
-// more than `cut` levels, what a workgroup's slot has to do on average, goes as
-// ceil(level / size) equal parts, where `size` is half of that (and at least
-// kMinPartKeys): few long rows then fill the chip as many short ones do.  The
-// level of a rank is found by bisection over the number of parts at or above it,
-// a sum over the sequences: on one wavefront's lanes (every wavefront for itself)
-// up to 64 sequences, on the workgroup's threads above.
-template <int kThreads>
-struct Finder {
-  static constexpr int kPer = (LUMEN_ATTN_MAX_REQS + kThreads - 1) / kThreads;
-  uint32_t n[kPer], off[kPer], top, cut, size;
-  float inv_size;
-  bool narrow;
-  int me, step, lane, wave;
-  uint32_t *lds;
+__device__ __forceinline__ bool sequence(const PromptArgs &a, int s, Sequence *out) {
+  const int64_t q0 = a.cu_q[s], q1 = a.cu_q[s + 1];
+  const int64_t k0 = a.cu_k[s], k1 = a.cu_k[s + 1];
+  *out = Sequence{q0, k0, 0, 0, 0};
+  if (q0 < 0 || q1 < q0 || q1 > a.num_q || k0 < 0 || k1 < k0 || k1 > a.num_k)
+    return false;
+  out->nq = int(q1 - q0);
+  out->nk = int(k1 - k0);
+  out->tiles = (out->nq + a.tile_tokens - 1) / a.tile_tokens;
+  return true;
+}
 
-  __device__ __forceinline__ uint32_t total(uint32_t x) const {
-    x = wave_sum(x);
-    if (narrow) return x;
-    __syncthreads();
-    if (lane == 0) lds[wave] = x;
-    __syncthreads();
-    x = 0;
-    for (int w = 0; w < kThreads / kWave; ++w) x += lds[w];
-    return x;
-  }
-  // x / size, exact for x below 2^23 (levels are at most 2^22)
-  __device__ __forceinline__ uint32_t over_size(uint32_t x) const {
-    uint32_t a = uint32_t(float(x) * inv_size);
-    a -= a * size > x;
-    return a + ((a + 1) * size <= x);
-  }
-  __device__ __forceinline__ uint32_t parts_at(uint32_t level) const {
-    return level <= cut ? 1u : over_size(level + size - 1);
-  }
-  // parts of the tiles of levels 1 to m, all of them cut into parts of `size`
-  __device__ __forceinline__ uint32_t parts_to(uint32_t m) const {
-    const uint32_t a = over_size(m), b = m - a * size;
-    return size * (a * (a + 1) / 2) + b * (a + 1);
-  }
-  // parts at level j or above
-  __device__ __forceinline__ uint32_t above(uint32_t j) const {
-    uint32_t c = 0;
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      if (narrow && i) break;
-      const uint32_t last = n[i] + off[i], from = j - 1 > off[i] ? j - 1 : off[i];
-      if (last <= from) continue;
-      if (top <= cut) {  // nothing is cut
-        c += last - from;
-        continue;
-      }
-      const uint32_t whole = last < cut ? last : cut;  // levels up to here
-      if (from < whole) c += whole - from;
-      if (last > cut) c += parts_to(last) - parts_to(from > cut ? from : cut);
-    }
-    return total(c);
-  }
+// The whole tile `t` of a sequence.
+__device__ __forceinline__ Unit whole_tile(const PromptArgs &a, const Sequence &s, int t) {
+  const int t0 = t * a.tile_tokens;
+  const int end = t0 + a.tile_tokens < s.nq ? t0 + a.tile_tokens : s.nq;
+  return Unit{int(s.q0), s.nq, int(s.k0), s.nk, t0, 0, steps_to(end + s.nk - s.nq), -1};
+}
 
-  // `slots`: workgroups that run at once, for one set of heads; 0: no cuts
-  __device__ void look(const PromptArgs &a, int tile_tokens, uint32_t slots,
-                       uint32_t *scratch) {
-    const int tid = threadIdx.x;
-    narrow = a.num_seqs <= kWave;
-    lane = tid & (kWave - 1), wave = tid / kWave;
-    me = narrow ? lane : tid, step = narrow ? kWave : kThreads;
-    lds = scratch;
-    top = 0, cut = 0x7fffffffu, size = 1;
-    int err = LUMEN_OK;
-    uint64_t work = 0;
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      n[i] = off[i] = 0;
-      const int s = me + i * step;
-      if (s >= a.num_seqs || (narrow && i)) continue;
-      const int64_t q0 = a.cu_q[s], q1 = a.cu_q[s + 1];
-      const int64_t k0 = a.cu_k[s], k1 = a.cu_k[s + 1];
-      if (q0 < 0 || q1 < q0 || q1 > a.num_q || k0 < 0 || k1 < k0 || k1 > a.num_k) {
-        err = LUMEN_ERR_RANGE;
-        continue;
-      }
-      n[i] = uint32_t(q1 - q0 + tile_tokens - 1) / uint32_t(tile_tokens);
-      const int64_t behind = (k1 - k0) - (q1 - q0);
-      off[i] = behind > 0 ? uint32_t(behind) / uint32_t(tile_tokens) : 0u;
-      top = n[i] && n[i] + off[i] > top ? n[i] + off[i] : top;
-      work += uint64_t(n[i]) * off[i] + uint64_t(n[i]) * (n[i] + 1) / 2;
-    }
+// The `rank`-th tile, sequence by sequence: for calls whose tiles all run at
+// once, so that their order does not matter.
+__device__ __forceinline__ Unit find_tile(const PromptArgs &a, int rank) {
+  const int lane = threadIdx.x & (kWave - 1);
+  int err = LUMEN_OK;
+  for (int base = 0; base < a.num_seqs; base += kWave) {
+    Sequence s{0, 0, 0, 0, 0};
+    if (base + lane < a.num_seqs && !sequence(a, base + lane, &s)) err = LUMEN_ERR_RANGE;
     if (blockIdx.x == 0) record_wave(a.status, err);
-    if (slots) {
-      // in two pieces, so that sums over the threads stay in 32 bits
-      const uint64_t low = total(uint32_t(work) & 0x3fffffu);
-      const uint64_t all = low + (uint64_t(total(uint32_t(work >> 22))) << 22);
-      // held to 2^22, which no level passes
-      const float share = fminf(float(all) / float(slots), 4194304.0f);
-      const uint32_t least = uint32_t((kMinPartKeys + tile_tokens - 1) / tile_tokens);
-      cut = uint32_t(share) + 1;
-      size = cut / 2 + 1;
-      size = size > least ? size : least;
-      cut = cut > size ? cut : size;
-    }
-    inv_size = 1.0f / float(size);
+    int upto = s.tiles;  // inclusive over the lanes
+#pragma unroll
     for (int o = 1; o < kWave; o <<= 1) {
-      const uint32_t t = __shfl_xor(top, o);
-      top = t > top ? t : top;
+      const int x = __shfl_up(upto, o);
+      if (lane >= o) upto += x;
     }
-    if (!narrow) {
-      __syncthreads();
-      if (lane == 0) lds[wave] = top;
-      __syncthreads();
-      for (int w = 0; w < kThreads / kWave; ++w) top = lds[w] > top ? lds[w] : top;
+    const uint64_t past = __ballot(rank < upto);
+    if (past && blockIdx.x) {  // the first workgroup looks at every sequence
+      const int at = __ffsll(static_cast<unsigned long long>(past)) - 1;
+      const Sequence found{__builtin_amdgcn_readlane(int(s.q0), at),
+                           __builtin_amdgcn_readlane(int(s.k0), at),
+                           __builtin_amdgcn_readlane(s.nq, at),
+                           __builtin_amdgcn_readlane(s.nk, at), 0};
+      const int before = __builtin_amdgcn_readlane(upto - s.tiles, at);
+      return whole_tile(a, found, rank - before);
     }
-    top = __builtin_amdgcn_readfirstlane(top);
-  }
-
-  // The part of place `rank`; false where there are fewer.
-  __device__ bool find(uint32_t rank, Part *out) {
-    if (top == 0 || rank >= above(1)) return false;
-    uint32_t lo = 1, hi = top, before = 0;  // above(lo) > rank >= above(hi + 1)
-    while (lo < hi) {
-      const uint32_t mid = lo + (hi - lo + 1) / 2;
-      const uint32_t c = above(mid);
-      if (c > rank) {
-        lo = mid;
-      } else {
-        hi = mid - 1;
-        before = c;
+    if (past) {
+      const int at = __ffsll(static_cast<unsigned long long>(past)) - 1;
+      const int seq = base + at, tile = rank - __builtin_amdgcn_readlane(upto - s.tiles, at);
+      for (int i = base + kWave + lane; i < a.num_seqs; i += kWave) {
+        Sequence rest;
+        if (!sequence(a, i, &rest)) err = LUMEN_ERR_RANGE;
       }
+      record_wave(a.status, err);
+      Sequence found;
+      sequence(a, seq, &found);
+      return whole_tile(a, found, tile);
     }
-    rank -= before;  // among the parts at level lo, in thread order
-    const uint32_t parts = parts_at(lo);
-    const uint32_t index = parts == 1 ? rank : rank / parts;  // the tile among those
-    uint32_t mine = 0;
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) mine += off[i] < lo && lo <= off[i] + n[i];
-    uint32_t upto = mine;  // inclusive over the lanes
-    for (int o = 1; o < kWave; o <<= 1) {
-      const uint32_t u = __shfl_up(upto, o);
-      if (lane >= o) upto += u;
-    }
-    if (!narrow) {
-      __syncthreads();
-      if (lane == kWave - 1) lds[wave] = upto;
-      __syncthreads();
-      for (int w = 0; w < wave; ++w) upto += lds[w];
-    }
-    uint32_t left = index - (upto - mine);
-    const bool found = index < upto && index >= upto - mine;
-    int s = 0, t = 0;
-    if (found) {
-#pragma unroll
-      for (int i = 0; i < kPer; ++i)
-        if (off[i] < lo && lo <= off[i] + n[i] && left-- == 0) {
-          s = me + i * step;
-          t = int(lo - 1 - off[i]);
-        }
-    }
-    if (narrow) {
-      const int at = __ffsll(static_cast<unsigned long long>(__ballot(found))) - 1;
-      out->seq = __builtin_amdgcn_readlane(s, at);
-      out->tile = __builtin_amdgcn_readlane(t, at);
-    } else {
-      __syncthreads();
-      if (found) lds[0] = uint32_t(s), lds[1] = uint32_t(t);
-      __syncthreads();
-      out->seq = __builtin_amdgcn_readfirstlane(int(lds[0]));
-      out->tile = __builtin_amdgcn_readfirstlane(int(lds[1]));
-      __syncthreads();
-    }
-    out->part = int(rank - index * parts);
-    out->parts = int(parts);
-    out->levels = parts == 1 ? int(lo) : int((lo + parts - 1) / parts);
-    out->first = before + index * parts;
-    return true;
+    rank -= __builtin_amdgcn_readlane(upto, kWave - 1);
   }
-};
+  return Unit{0, 0, 0, 0, 0, 0, 0, -1};
+}
+
+// The plan: every tile by falling work, so that the long ones start first and
+// the short ones fill the end; those with more steps than a workgroup's slot
+// has to do on average go in equal parts of about half of that (at least
+// kMinPartKeys), so that few long rows fill the chip as many short ones do.  One
+// workgroup: tiles are counted by work into kPlanThreads bins, the bins are
+// summed from the top, and each tile takes the next place of its bin.  Which of
+// two tiles of a bin comes first changes nothing but that order.
+constexpr int kPlanThreads = 1024;
+__global__ __launch_bounds__(kPlanThreads) void prompt_plan_kernel(PromptArgs a) {
+  __shared__ int tiles_to[LUMEN_ATTN_MAX_REQS];  // inclusive, over the sequences
+  __shared__ uint32_t bins[kPlanThreads];
+  __shared__ uint64_t wave_work[kPlanThreads / kWave];
+  __shared__ int64_t wave_tiles[kPlanThreads / kWave];
+  __shared__ int top, cuts, parts_used;
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
+  const int per = (a.num_seqs + kPlanThreads - 1) / kPlanThreads;
+  int err = LUMEN_OK, longest = 0;
+  int64_t mine = 0;
+  uint64_t work = 0;
+  Sequence s;
+  if (tid == 0) top = cuts = parts_used = 0;
+  bins[tid] = 0;
+  for (int i = tid * per; i < (tid + 1) * per && i < a.num_seqs; ++i) {
+    if (!sequence(a, i, &s)) err = LUMEN_ERR_RANGE;
+    mine += s.tiles;
+    tiles_to[i] = int(mine < a.num_units ? mine : a.num_units);
+    // steps of the sequence's tiles, and of its last one
+    const int seen = s.nk < s.nq ? s.nk : s.nq;  // queries that see a key
+    const int64_t n = (seen + a.tile_tokens - 1) / a.tile_tokens + (s.nk < s.nq);
+    work += uint64_t(n * (s.nk - seen) + a.tile_tokens * n * (n + 1) / 2) / kKeys + n;
+    const int last = s.tiles ? steps_to(s.nk) : 0;
+    longest = last > longest ? last : longest;
+  }
+  int64_t upto = mine;
+  uint64_t sum = work;
+  for (int o = 1; o < kWave; o <<= 1) {
+    const int64_t x = __shfl_up(upto, o);
+    if (lane >= o) upto += x;
+    sum += __shfl_xor(sum, o);
+    const int y = __shfl_xor(longest, o);
+    longest = y > longest ? y : longest;
+  }
+  if (lane == kWave - 1) wave_tiles[wave] = upto;
+  if (lane == 0) wave_work[wave] = sum;
+  __syncthreads();
+  if (lane == 0) atomicMax(&top, longest);
+  int64_t before = upto - mine, all = 0;
+  sum = 0;
+  for (int w = 0; w < kPlanThreads / kWave; ++w) {
+    if (w < wave) before += wave_tiles[w];
+    all += wave_tiles[w];
+    sum += wave_work[w];
+  }
+  // held to the room there is: more tiles are possible only where sequences
+  // share queries
+  const int tiles = int(all < a.num_units ? all : a.num_units);
+  for (int i = tid * per; i < (tid + 1) * per && i < a.num_seqs; ++i) {
+    const int64_t to = tiles_to[i] + before;
+    tiles_to[i] = int(to < a.num_units ? to : a.num_units);
+  }
+  __syncthreads();
+  // more steps than this: a cut into parts of `part` steps or a little less
+  const uint64_t share = sum / uint32_t(a.slots);
+  const int half = share < 0x3fffffff ? int(share / 2) + 1 : 0x3fffffff;
+  const int part = half > kMinPartKeys / kKeys ? half : kMinPartKeys / kKeys;
+  const int whole = a.max_parts ? 2 * part : 0x7fffffff;
+  // a bin of work, the most in bin 0
+  const float scale = float(kPlanThreads - 1) / float(top + 1);
+  const auto bin_of = [&](int steps) {
+    return kPlanThreads - 1 - int(float(steps) * scale);
+  };
+  const auto tile_at = [&](int i, int *parts) {
+    int lo = 0, hi = a.num_seqs - 1;  // the first sequence with tiles_to > i
+    while (lo < hi) {
+      const int mid = (lo + hi) / 2;
+      if (tiles_to[mid] > i)
+        hi = mid;
+      else
+        lo = mid + 1;
+    }
+    Sequence q;
+    sequence(a, lo, &q);
+    const Unit u = whole_tile(a, q, i - (lo ? tiles_to[lo - 1] : 0));
+    *parts = u.last > whole ? (u.last + part - 1) / part : 1;
+    return u;
+  };
+  for (int i = tid; i < tiles; i += kPlanThreads) {
+    int parts;
+    const Unit u = tile_at(i, &parts);
+    atomicAdd(&bins[bin_of(u.last / parts)], uint32_t(parts));
+  }
+  __syncthreads();
+  // exclusive sums of the bins
+  uint32_t bin = bins[tid], run = bin;
+  for (int o = 1; o < kWave; o <<= 1) {
+    const uint32_t x = __shfl_up(run, o);
+    if (lane >= o) run += x;
+  }
+  if (lane == kWave - 1) wave_tiles[wave] = run;
+  __syncthreads();
+  for (int w = 0; w < wave; ++w) run += uint32_t(wave_tiles[w]);
+  bins[tid] = run - bin;
+  uint32_t total = 0;
+  for (int w = 0; w < kPlanThreads / kWave; ++w) total += uint32_t(wave_tiles[w]);
+  __syncthreads();
+  for (int i = tid; i < tiles; i += kPlanThreads) {
+    int parts;
+    Unit u = tile_at(i, &parts);
+    const uint32_t at = atomicAdd(&bins[bin_of(u.last / parts)], uint32_t(parts));
+    // more units, or parts, than there is room for are possible only where
+    // sequences share queries
+    if (at + uint32_t(parts) > uint32_t(a.num_units)) continue;
+    if (parts == 1) {
+      a.units[at] = u;
+      continue;
+    }
+    const int place = atomicAdd(&parts_used, parts);
+    const bool room = place + parts <= a.max_parts;
+    if (room) a.cuts[atomicAdd(&cuts, 1)] = Cut{int(at), parts};
+    const int steps = u.last;
+    for (int c = 0; c < parts; ++c) {
+      Unit x = u;
+      if (room) {
+        x.first = int(int64_t(steps) * c / parts);
+        x.last = int(int64_t(steps) * (c + 1) / parts);
+        x.place = place + c;
+      } else if (c) {
+        x.nq = 0;
+      }
+      a.units[at + c] = x;
+    }
+  }
+  for (uint32_t i = total + tid; i < uint32_t(a.num_units); i += kPlanThreads)
+    a.units[i].nq = 0;
+  __syncthreads();
+  if (tid == 0) *a.num_cuts = cuts;
+  record_wave(a.status, err);
+}
 
 // Floats of a part's result: the lanes' sums, then their maxima and sums.
 constexpr int part_floats(int D, int waves) { return waves * kWave * (D / 2 + 2); }
@@ -317,35 +349,25 @@ __global__ __launch_bounds__(kWaves *kWave, 2) void prompt_kernel(PromptArgs a) 
   // ---- the unit: sequence, tokens, heads
   const int gp = a.heads_per_tile;
   const int groups = a.q_heads / gp;
-  const int tile_tokens = 32 * kWaves / gp;
   const int hg = int(blockIdx.x % unsigned(groups));
-  Part p;
-  {
-    Finder<kThreads> finder;
-    finder.look(a, tile_tokens, a.slots, reinterpret_cast<uint32_t *>(lds));
-    if (!finder.find(blockIdx.x / unsigned(groups), &p)) return;
+  const int rank = int(blockIdx.x / unsigned(groups));
+  Unit u;
+  if (a.units) {  // by scalar loads
+    const auto *from = CONSTANT_PTR(int32_t, a.units + rank);
+    u = Unit{from[0], from[1], from[2], from[3], from[4], from[5], from[6], from[7]};
+  } else {
+    u = find_tile(a, rank);
   }
-  const int s = p.seq, tile = p.tile;
-  const int64_t q0 = a.cu_q[s], q1 = a.cu_q[s + 1];
-  const int64_t k0 = a.cu_k[s], k1 = a.cu_k[s + 1];
-  const int nq = int(q1 - q0), nk = int(k1 - k0), behind = nk - nq;
-  const int t0 = tile * tile_tokens;
+  if (u.nq == 0) return;
+  const int64_t q0 = u.q0, k0 = u.k0;
+  const int nq = u.nq, nk = u.nk, t0 = u.t0, behind = nk - nq;
   const int hq = hg * gp + wave % gp;
   const int hk = hg * gp / (a.q_heads / a.kv_heads);
   const int w0 = t0 + wave / gp * 32;  // the wavefront's first token
   const int tok = w0 + col;
   const bool here = w0 < nq;
   const int limit = tok + behind;  // last key that the lane's query sees
-  const int tile_end = t0 + tile_tokens < nq ? t0 + tile_tokens : nq;
-  // the part's keys, in steps of kKeys: [first_step, steps)
-  const auto steps_to = [](int keys) { return keys > 0 ? (keys + kKeys - 1) / kKeys : 0; };
-  int steps = steps_to(tile_end + behind), first_step = 0;
-  if (p.parts > 1) {
-    const int part_keys = p.levels * tile_tokens;
-    first_step = steps_to(p.part * part_keys);
-    const int stop = steps_to((p.part + 1) * part_keys);
-    if (p.part + 1 < p.parts && stop < steps) steps = stop;
-  }
+  const int first_step = u.first, steps = u.last;
   const int wave_end = (w0 + 32 < nq ? w0 + 32 : nq) + behind;
   int wave_steps = here ? steps_to(wave_end) : 0;
   wave_steps = wave_steps < steps ? wave_steps : steps;
@@ -498,9 +520,8 @@ __global__ __launch_bounds__(kWaves *kWave, 2) void prompt_kernel(PromptArgs a) 
   float la, lb;
   both<32>(l, &la, &lb);
   l = la + lb;
-  if (p.parts > 1) {
-    if (blockIdx.x >= a.max_parts) return;  // only where sequences share queries
-    float *part = a.parts + int64_t(blockIdx.x) * part_floats(D, kWaves);
+  if (u.place >= 0) {
+    float *part = a.parts + (int64_t(u.place) * groups + hg) * part_floats(D, kWaves);
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)
 #pragma unroll
@@ -520,33 +541,24 @@ __global__ __launch_bounds__(kWaves *kWave, 2) void prompt_kernel(PromptArgs a) 
 template <int D, bool kBf16, int kWaves>
 __global__ __launch_bounds__(kWaves *kWave, 2) void prompt_join_kernel(PromptArgs a) {
   constexpr int kThreads = kWaves * kWave;
-  __shared__ uint32_t lds[kWaves + 2];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int gp = a.heads_per_tile, groups = a.q_heads / gp;
-  const int tile_tokens = 32 * kWaves / gp;
-  const int hg = int(blockIdx.x % unsigned(groups));
-  Finder<kThreads> finder;
-  Part p;
-  finder.look(a, tile_tokens, a.slots, lds);
-  // parts of cut tiles come first, and each has at least two: the workgroup
-  // takes the tiles that start at its two places
-  for (uint32_t rank = blockIdx.x / unsigned(groups) * 2, end = rank + 2; rank < end;
-       ++rank) {
-    if (finder.top <= finder.cut || rank >= finder.above(finder.cut + 1)) return;
-    if (!finder.find(rank, &p) || p.first != rank) continue;
-    if ((uint64_t(rank) + p.parts) * groups > a.max_parts) return;
-    const int64_t q0 = a.cu_q[p.seq];
-    const Row r{p.tile * tile_tokens + wave / gp * 32 + (lane & 31),
-                int(a.cu_q[p.seq + 1] - q0), q0, hg * gp + wave % gp, lane >> 5};
+  const int items = *a.num_cuts * groups;
+  for (int item = blockIdx.x; item < items; item += gridDim.x) {
+    const Cut cut = a.cuts[item / groups];
+    const int hg = item % groups;
+    const Unit u = a.units[cut.unit];
+    const Row r{u.t0 + wave / gp * 32 + (lane & 31), u.nq, u.q0, hg * gp + wave % gp,
+                lane >> 5};
     f32x16 o[D / 32];
     float m = -INFINITY, l = 0.0f;
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)
 #pragma unroll
       for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
-    for (int c = 0; c < p.parts; ++c) {
+    for (int c = 0; c < cut.parts; ++c) {
       const float *part =
-          a.parts + (int64_t(rank + c) * groups + hg) * part_floats(D, kWaves);
+          a.parts + (int64_t(u.place + c) * groups + hg) * part_floats(D, kWaves);
       const float pm = part[kThreads * (D / 2) + tid];
       const float pl = part[kThreads * (D / 2 + 1) + tid];
       const float mn = fmaxf(m, pm);
@@ -575,10 +587,11 @@ __global__ __launch_bounds__(kWaves *kWave, 2) void prompt_join_kernel(PromptArg
 // Grid and workspace of a call.
 struct PromptPlan {
   int waves, heads_per_tile, tile_tokens, groups;
-  int slots;      // workgroups that run at once, for one set of heads
-  int64_t tiles;  // at most, for one set of heads
-  int64_t parts;  // of cut tiles at most, for one set of heads; 0: none is cut
-  size_t bytes;
+  int slots;        // workgroups that run at once, for one set of heads
+  int64_t tiles;    // at most, for one set of heads
+  int64_t parts;    // of cut tiles at most, for one set of heads; 0: none is cut
+  bool planned;     // by a kernel before
+  size_t units_at, cuts_at, parts_at, bytes;
 };
 
 // The workspace is sized for the largest device of this architecture, so that
@@ -588,7 +601,6 @@ constexpr int kMaxUnits = 256;
 PromptPlan prompt_plan(int32_t num_seqs, int64_t num_q, int64_t num_k,
                        int32_t q_heads, int32_t kv_heads, int32_t head_dim, int cus) {
   PromptPlan p;
-  // Waves of a workgroup.
   p.waves = 8;
   const int group = q_heads / kv_heads;
   p.heads_per_tile = p.waves;
@@ -596,18 +608,25 @@ PromptPlan prompt_plan(int32_t num_seqs, int64_t num_q, int64_t num_k,
   p.tile_tokens = 32 * p.waves / p.heads_per_tile;
   p.groups = q_heads / p.heads_per_tile;
   p.slots = (cus < kMaxUnits ? cus : kMaxUnits) * 8 / p.waves / p.groups;
+  if (p.slots < 1) p.slots = 1;
   // at most a part-filled tile for each sequence beside the full ones
   p.tiles = num_q / p.tile_tokens + num_seqs;
   p.parts = 0;
   if (num_k >= kCutKeys) {
-    // a cut tile of `level` levels has less than 2 * level / size parts, and size
-    // is more than half a slot's share of all levels (its float's rounding is
-    // far less than the 1 added to each half)
+    // a cut tile has less than twice its steps over `part`'s parts, and `part`
+    // is at least half a slot's share of all steps
     p.parts = int64_t(p.slots) * 4;
     const int64_t most = p.tiles * (num_k / kMinPartKeys + 2);
     if (p.parts > most) p.parts = most;
   }
-  p.bytes = size_t(p.parts) * p.groups * part_floats(head_dim, p.waves) * sizeof(float);
+  p.planned = p.parts > 0 || p.tiles > p.slots;
+  const auto up = [](size_t n) { return (n + 255) & ~size_t(255); };
+  p.units_at = 256;  // the number of cuts stands first
+  p.cuts_at = p.units_at + up(size_t(p.tiles + p.parts) * sizeof(Unit));
+  p.parts_at = p.cuts_at + up(size_t(p.parts / 2 + 1) * sizeof(Cut));
+  p.bytes = !p.planned ? 0
+                       : p.parts_at + size_t(p.parts) * p.groups *
+                                          part_floats(head_dim, p.waves) * sizeof(float);
   return p;
 }
 
@@ -675,10 +694,10 @@ int lumen_attn_prompt(const lumen_attn_rows *q, const lumen_attn_rows *k,
   if (num_seqs == 0) return LUMEN_OK;
   int cus = 0;
   if ((st = compute_units(&cus)) != LUMEN_OK) return st;
-  PromptPlan p = prompt_plan(num_seqs, num_q_tokens, num_k_tokens, num_q_heads,
-                             num_kv_heads, head_dim, cus);
-  if (!d_workspace) p.parts = 0;
-  if (p.parts && workspace_bytes < p.bytes) return LUMEN_ERR_INVALID_ARG;
+  const PromptPlan p = prompt_plan(num_seqs, num_q_tokens, num_k_tokens, num_q_heads,
+                                   num_kv_heads, head_dim, cus);
+  if (p.planned && (!d_workspace || workspace_bytes < p.bytes))
+    return LUMEN_ERR_INVALID_ARG;
   if ((p.tiles + p.parts) * p.groups > INT32_MAX) return LUMEN_ERR_UNSUPPORTED;
   (void)hipGetLastError();
   PromptArgs a;
@@ -693,23 +712,33 @@ int lumen_attn_prompt(const lumen_attn_rows *q, const lumen_attn_rows *k,
   a.q_heads = num_q_heads;
   a.kv_heads = num_kv_heads;
   a.heads_per_tile = p.heads_per_tile;
-  a.slots = p.parts ? uint32_t(p.slots) : 0u;
+  a.tile_tokens = p.tile_tokens;
   a.scale_log2 = scale * 1.44269504088896341f;
   a.out = static_cast<uint16_t *>(d_out);
   a.status = d_status;
-  a.parts = static_cast<float *>(d_workspace);
-  a.max_parts = uint32_t(p.parts * p.groups);
+  char *ws = static_cast<char *>(d_workspace);
+  a.units = p.planned ? reinterpret_cast<Unit *>(ws + p.units_at) : nullptr;
+  a.num_units = int32_t(p.tiles + p.parts);
+  a.slots = p.slots;
+  a.num_cuts = reinterpret_cast<int32_t *>(ws);
+  a.cuts = reinterpret_cast<Cut *>(ws + p.cuts_at);
+  a.max_parts = int32_t(p.parts);
+  a.parts = reinterpret_cast<float *>(ws + p.parts_at);
   const bool bf = dtype == LUMEN_ATTN_BF16;
   const PromptKernels kernels =
       p.waves == 4 ? (head_dim == 64 ? prompt_kernels<64, 4>(bf) : prompt_kernels<128, 4>(bf))
                    : (head_dim == 64 ? prompt_kernels<64, 8>(bf) : prompt_kernels<128, 8>(bf));
   const dim3 threads(unsigned(p.waves * kWave));
   hipStream_t s = static_cast<hipStream_t>(stream);
+  if (p.planned)
+    hipLaunchKernelGGL(prompt_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, a);
   hipLaunchKernelGGL(kernels.main, dim3(unsigned((p.tiles + p.parts) * p.groups)),
                      threads, 0, s, a);
-  if (p.parts)
-    hipLaunchKernelGGL(kernels.join, dim3(unsigned((p.parts + 1) / 2 * p.groups)),
-                       threads, 0, s, a);
+  if (p.parts) {
+    int64_t items = p.parts / 2 * p.groups;
+    if (items > cus) items = cus;
+    hipLaunchKernelGGL(kernels.join, dim3(unsigned(items < 1 ? 1 : items)), threads, 0, s, a);
+  }
   return hipGetLastError() == hipSuccess ? LUMEN_OK : LUMEN_ERR_HIP;
 }
 
