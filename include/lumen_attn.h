@@ -66,6 +66,8 @@ extern "C" {
 /* Most query tokens, and most key tokens, of one prompt call. */
 #define LUMEN_ATTN_MAX_TOKENS 134217728
 
+/* Largest token stride of a prompt call's keys and values, in elements. */
+#define LUMEN_ATTN_MAX_STRIDE 16777216
 /* Magnitude to which append4 holds an element. */
 #define LUMEN_ATTN_KV4_MAX 6848
 
@@ -139,16 +141,16 @@ size_t lumen_attn_decode4_workspace_bytes(const lumen_kv_layout *layout,
 
 /* Attention of one token per request over layer `layer` of the 4-bit cache:
  *     out[r][h] = sum_t softmax_t(scale * q[r][h] . K[t][h/G]) V[t][h/G],
- * t < d_lens[r], G = num_q_heads / H (H must divide num_q_heads).  q: rows
+ * t < d_lens[r], G = num_q_heads / H (H must divide num_q_heads, at most
+ * 65535).  q: rows
  * (r, h) of dtype; d_out [num_reqs][num_q_heads][D] of dtype, contiguous,
  * 16-byte aligned.  scale must be finite and above 0.  A request of length 0
  * gets zeros; a negative one too (RANGE).  Tokens in pages past bt_cols
  * (RANGE) or with a block id outside [0, num_blocks) (BLOCK_ID) are left out
  * of the sum.  What the cache holds past a request's length does not matter,
  * NaN included.  The result does not depend on timing.  d_workspace:
- * lumen_attn_decode4_workspace_bytes bytes, 16-byte aligned, zeroed once
- * before its first call; a call leaves it ready for the next.  Calls in flight
- * at the same time must not share one. */
+ * lumen_attn_decode4_workspace_bytes bytes, 16-byte aligned, not shared by
+ * calls in flight at the same time; what it holds does not matter. */
 int lumen_attn_decode4(const lumen_kv_layout *layout, int32_t layer,
                        const void *d_cache, const int32_t *d_block_tables,
                        int32_t bt_cols, const int32_t *d_lens,
@@ -176,7 +178,10 @@ size_t lumen_attn_prompt_workspace_bytes(int32_t num_seqs, int64_t num_q_tokens,
  * tokens in no sequence are not written.  head_dim 64 or 128.  scale finite
  * and above 0.  A sequence whose bounds fall outside [0, num_q_tokens] or [0,
  * num_k_tokens], or end before they begin, is skipped (RANGE).  Sequences must
- * not share queries.  Token counts at most LUMEN_ATTN_MAX_TOKENS.  d_workspace:
+ * not share queries.  Token counts at most LUMEN_ATTN_MAX_TOKENS; token strides
+ * of k and v at most LUMEN_ATTN_MAX_STRIDE where they have more than one token.
+ * What a query does not see does not reach its row, NaN and infinities
+ * included; a NaN or infinity among the values it sees does.  d_workspace:
  * lumen_attn_prompt_workspace_bytes bytes (NULL where that is 0), 16-byte aligned,
  * not shared by calls in flight at the same time; what it holds does not matter.
  * The result does not depend on timing. */

@@ -24,6 +24,7 @@ LUMEN_ATTN_BF16 = 0
 LUMEN_ATTN_FP16 = 1
 LUMEN_ATTN_MAX_REQS = 4096  # include/lumen_attn.h
 LUMEN_ATTN_MAX_TOKENS = 134217728  # include/lumen_attn.h
+LUMEN_ATTN_MAX_STRIDE = 16777216  # include/lumen_attn.h
 LUMEN_ATTN_KV4_MAX = 6848  # include/lumen_attn.h
 
 _DTYPES = {torch.bfloat16: LUMEN_ATTN_BF16, torch.float16: LUMEN_ATTN_FP16}
@@ -275,9 +276,9 @@ def lumen_attn_decode4_workspace_bytes(shape, num_reqs: int,
 
 def new_decode4_workspace(shape, num_reqs: int, num_q_heads: int,
                           device=None) -> torch.Tensor:
-    """Zeroed workspace for decode4 calls of up to num_reqs requests."""
+    """Workspace for decode4 calls of up to num_reqs requests."""
     n = lumen_attn_decode4_workspace_bytes(shape, num_reqs, num_q_heads)
-    return torch.zeros(max(n, 16), dtype=torch.uint8, device=device or "cuda")
+    return torch.empty(max(n, 16), dtype=torch.uint8, device=device or "cuda")
 
 
 def _decode4_args(shape, num_blocks, layer, cache, block_tables, lens, q, out,

@@ -1337,9 +1337,6 @@ int lumen_attn_decode4(const lumen_kv_layout *layout, int32_t layer,
       !aligned(d_workspace, 16) || !aligned(d_lens, 4) ||
       !aligned(d_block_tables, 4))
     return LUMEN_ERR_MISALIGNED;
-  if (int64_t(layout->num_blocks) * layout->block_size >
-      int64_t(UINT32_MAX) / layout->num_kv_heads)
-    return LUMEN_ERR_UNSUPPORTED;  // rows are counted in 32 bits
   int cus = 0;
   if ((st = compute_units(&cus)) != LUMEN_OK) return st;
   (void)hipGetLastError();
