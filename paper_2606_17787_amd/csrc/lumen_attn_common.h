@@ -85,6 +85,11 @@ __device__ __forceinline__ void load_to_lds(const void *from, uint32_t to) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
                  :: "s"(to), "v"(from) : "memory");
 }
+// The same from byte `at` of the lane on, of memory at `from`.
+__device__ __forceinline__ void load_to_lds(const void *from, uint32_t at, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+               :: "s"(to), "v"(at), "s"(from) : "memory");
+}
 template <int kLeft>
 __device__ __forceinline__ void wait_loads() {
   asm volatile("s_waitcnt vmcnt(%0)" :: "i"(kLeft) : "memory");

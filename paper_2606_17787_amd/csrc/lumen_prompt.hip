@@ -67,6 +67,9 @@ constexpr int kKeys = 64;  // keys of a tile
 #define CONSTANT_PTR(T, p) ((const __attribute__((address_space(4))) T *)(p))
 
 constexpr float kSlack = 8.0f;
+// fp16 weights are taken times 2^kLift: up to 2^15 then, and a weight only
+// rounds to a subnormal or 0 when it is under 2^-21 or 2^-32 of the largest.
+constexpr float kLift = 7.0f;
 constexpr int kMfma = 0x8, kDsRead = 0x100;  // of sched_group_barrier
 
 template <int D>
@@ -331,19 +334,68 @@ __device__ __forceinline__ void write_row(const PromptArgs &a, const Row &r,
     }
 }
 
-// A workgroup takes 32 * kWaves query rows of one KV head: a wavefront 32
-// consecutive tokens of one query head, heads_per_tile of them different heads
-// of the group.
-template <int D, bool kBf16, int kWaves>
-__global__ __launch_bounds__(kWaves *kWave, 2) void prompt_kernel(PromptArgs a) {
-  constexpr int kThreads = kWaves * kWave;
-  constexpr int kChunks = D / 8;              // 16-byte chunks of a row
-  constexpr int kTile = kKeys * D;            // elements of a K or V tile
+template <bool kBf16>
+__device__ __forceinline__ bool not_finite16(uint32_t x) {
+  constexpr uint32_t kExp = kBf16 ? 0x7f80 : 0x7c00;
+  return (x & kExp) == kExp;
+}
+
+template <int D, int kWaves>
+struct PromptShape {
+  static constexpr int kThreads = kWaves * kWave;
+  static constexpr int kChunks = D / 8;    // 16-byte chunks of a row
+  static constexpr int kTile = kKeys * D;  // elements of a K or V tile
+  // tiles in LDS: kStages - 1 under way while one is used; two workgroups of
+  // four wavefronts share a compute unit's 160 KB
+  static constexpr int kStages = kWaves == 8 ? 4 : 2;
+};
+
+// Infinities and NaN of a tile in LDS become 0.
+template <bool kBf16, int kElems, int kThreads>
+__device__ __forceinline__ void clear_nonfinite(uint16_t *tile, int tid) {
+  uint32_t *w = reinterpret_cast<uint32_t *>(tile);
+#pragma unroll 1
+  for (int i = tid; i < kElems / 2; i += kThreads) {
+    const uint32_t x = w[i];
+    const uint32_t keep = (not_finite16<kBf16>(x) ? 0u : 0xffffu) |
+                          (not_finite16<kBf16>(x >> 16) ? 0u : 0xffff0000u);
+    if (keep != 0xffffffffu) w[i] = x & keep;
+  }
+}
+
+// Adds a row's infinities and NaN, whatever the weight, where it is seen.
+template <int D, bool kBf16>
+__device__ __forceinline__ void add_nonfinite(const uint16_t *row, bool seen, f32x16 *o) {
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const frag4 x = *reinterpret_cast<const frag4 *>(row + d * 32 + 8 * i);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint16_t bits = uint16_t(x[j]);
+        if (seen && not_finite16<kBf16>(bits)) o[d][4 * i + j] += value<kBf16>(bits);
+      }
+    }
+}
+
+// One workgroup's tile, or part of one: 32 * kWaves query rows of one KV head,
+// a wavefront 32 consecutive tokens of one query head, heads_per_tile of them
+// different heads of the group.
+//
+// A value that is masked for some of a wavefront's queries has the weight 0 for
+// them in the products, which keeps it out unless it is an infinity or NaN.
+// Where a sum comes out as one, nothing is written and the call returns true:
+// the tile is then done again with kApart, where such values are taken out of
+// the products and added to the queries that see them.
+template <int D, bool kBf16, int kWaves, bool kApart>
+__device__ __forceinline__ bool prompt_tile(const PromptArgs &a, const int tid,
+                                            uint16_t *lds, bool *not_finite) {
+  using S = PromptShape<D, kWaves>;
+  constexpr int kThreads = S::kThreads, kChunks = S::kChunks, kTile = S::kTile;
+  constexpr int kStages = S::kStages, kStageBytes = 2 * kTile * 2;
   constexpr int kIssues = kKeys * kChunks / kThreads;
-  // tiles in LDS: kStages - 1 under way while one is used
-  constexpr int kStages = kWaves == 8 ? 4 : 2;
-  __shared__ __attribute__((aligned(1024))) uint16_t lds[kStages][2][kTile];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 31, half = lane >> 5;
 
   // ---- the unit: sequence, tokens, heads
@@ -357,8 +409,10 @@ __global__ __launch_bounds__(kWaves *kWave, 2) void prompt_kernel(PromptArgs a) 
     u = Unit{from[0], from[1], from[2], from[3], from[4], from[5], from[6], from[7]};
   } else {
     u = find_tile(a, rank);
+    for (int32_t *x : {&u.q0, &u.nq, &u.k0, &u.nk, &u.t0, &u.first, &u.last, &u.place})
+      *x = __builtin_amdgcn_readfirstlane(*x);
   }
-  if (u.nq == 0) return;
+  if (u.nq == 0) return false;
   const int64_t q0 = u.q0, k0 = u.k0;
   const int nq = u.nq, nk = u.nk, t0 = u.t0, behind = nk - nq;
   const int hq = hg * gp + wave % gp;
@@ -390,20 +444,47 @@ __global__ __launch_bounds__(kWaves *kWave, 2) void prompt_kernel(PromptArgs a) 
   const uint16_t *vb = a.v.base + k0 * a.v.token + hk * a.v.head;
   const uint32_t lds_at = uint32_t(__builtin_amdgcn_readfirstlane(
       int(reinterpret_cast<uintptr_t>(LDS_PTR(uint16_t, lds))) + wave * kWave * 16));
-  const auto load = [&](int step, int buf) __attribute__((always_inline)) {
+  // the lane's piece of each load: its key in the tile, its chunk, and both as
+  // an offset from the tile's first key
+  const auto row_of = [&](int i) { return (i * kThreads + tid) / kChunks; };
+  const auto chunk_k = [&](int i) { return 16 * ((tid % kChunks) ^ swizzle_k<D>(row_of(i))); };
+  const auto chunk_v = [&](int i) { return 16 * ((tid % kChunks) ^ swizzle_v<D>(row_of(i))); };
+  const uint32_t token_k = uint32_t(a.k.token) * 2, token_v = uint32_t(a.v.token) * 2;
+  uint32_t from_k[kIssues], from_v[kIssues];
 #pragma unroll
-    for (int i = 0; i < kIssues; ++i) {
-      const int at = i * kThreads + wave * 64;
-      const int row = (at + lane) / kChunks, pos = (at + lane) % kChunks;
-      int key = step * kKeys + row;
-      key = key < nk ? key : nk - 1;  // rows past the end repeat the last key
-      const uint32_t to = lds_at + (buf * 2 * kTile + i * kThreads * 8) * 2;
-      load_to_lds<false>(kb + int64_t(key) * a.k.token + 8 * (pos ^ swizzle_k<D>(row)),
-                         to);
-      load_to_lds<false>(vb + int64_t(key) * a.v.token + 8 * (pos ^ swizzle_v<D>(row)),
-                         to + kTile * 2);
+  for (int i = 0; i < kIssues; ++i) {
+    from_k[i] = row_of(i) * token_k + chunk_k(i);
+    from_v[i] = row_of(i) * token_v + chunk_v(i);
+  }
+  const auto load = [&](int step, int buf) __attribute__((always_inline)) {
+    const uint16_t *kt = kb + int64_t(step) * kKeys * a.k.token;
+    const uint16_t *vt = vb + int64_t(step) * kKeys * a.v.token;
+    const uint32_t to = lds_at + buf * kStageBytes;
+    const int last = nk - 1 - step * kKeys;
+    if (last >= kKeys - 1) {
+#pragma unroll
+      for (int i = 0; i < kIssues; ++i) {
+        load_to_lds(kt, from_k[i], to + i * kThreads * 16);
+        load_to_lds(vt, from_v[i], to + i * kThreads * 16 + kTile * 2);
+      }
+    } else {  // rows past the end repeat the last key
+#pragma unroll
+      for (int i = 0; i < kIssues; ++i) {
+        const uint32_t row = row_of(i) < last ? row_of(i) : last;
+        load_to_lds(kt, row * token_k + chunk_k(i), to + i * kThreads * 16);
+        load_to_lds(vt, row * token_v + chunk_v(i), to + i * kThreads * 16 + kTile * 2);
+      }
     }
   };
+
+  // where the lane reads in a tile; the other chunks' places differ in those
+  // bits of the address that count chunks
+  const auto *lds_bytes = LDS_PTR(const char, lds);
+  const uint32_t read_k = col * D * 2 + 16 * (half ^ swizzle_k<D>(col));
+  const int tr_row = 4 * half + ((lane & 15) >> 2);
+  const uint32_t read_v = kTile * 2 + tr_row * D * 2 +
+                          16 * ((((lane & 16) >> 3) | ((lane & 2) >> 1)) ^ swizzle_v<D>(tr_row)) +
+                          8 * (lane & 1);
 
   f32x16 o[D / 32];
 #pragma unroll
@@ -426,6 +507,10 @@ __global__ __launch_bounds__(kWaves *kWave, 2) void prompt_kernel(PromptArgs a) 
       wait_loads<0>();
     lds_barrier();
     const int now = buf;
+    if constexpr (kApart) {
+      clear_nonfinite<kBf16, kTile, kThreads>(lds + now * 2 * kTile + kTile, tid);
+      lds_barrier();
+    }
     buf = buf + 1 < kStages ? buf + 1 : 0;
     if (step + kStages - 1 < steps)
       load(step + kStages - 1, now ? now - 1 : kStages - 1);
@@ -438,10 +523,10 @@ __global__ __launch_bounds__(kWaves *kWave, 2) void prompt_kernel(PromptArgs a) 
       for (int i = 0; i < 16; ++i) sc[t][i] = 0.0f;
     // the second half's keys are read while the first half's products run
     frag8 k[D / 16];
+    const uint32_t stage = now * kStageBytes;
     const auto key_row = [&](int t, int i) __attribute__((always_inline)) {
-      const int row = t * 32 + col;
-      return *reinterpret_cast<const frag8 *>(
-          &lds[now][0][row * D + 8 * ((2 * i + half) ^ swizzle_k<D>(row))]);
+      return *reinterpret_cast<const __attribute__((address_space(3))) frag8 *>(
+          lds_bytes + ((read_k ^ (32 * i)) + stage) + t * 32 * D * 2);
     };
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) k[i] = key_row(0, i);
@@ -487,7 +572,7 @@ __global__ __launch_bounds__(kWaves *kWave, 2) void prompt_kernel(PromptArgs a) 
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[d][i] *= c;
     }
-    const float ms = m == -INFINITY ? 0.0f : m;
+    const float ms = m == -INFINITY ? 0.0f : m - (kBf16 ? 0.0f : kLift);
     frag8 pr[4];
 #pragma unroll
     for (int t = 0; t < 2; ++t)
@@ -506,16 +591,35 @@ __global__ __launch_bounds__(kWaves *kWave, 2) void prompt_kernel(PromptArgs a) 
         frag8 v;
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
-          const int row = ks * 16 + 8 * b + 4 * half + ((lane & 15) >> 2);
-          const int at = d * 32 + (lane & 16) + 4 * (lane & 3);
-          const frag4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(
-              frag4, &lds[now][1][row * D + 8 * ((at >> 3) ^ swizzle_v<D>(row)) +
-                                  (at & 7)]));
+          const frag4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+              (__attribute__((address_space(3))) frag4 *)(
+                  lds_bytes + ((read_v ^ (64 * d)) + stage) + (ks * 16 + 8 * b) * D * 2));
 #pragma unroll
           for (int i = 0; i < 4; ++i) v[4 * b + i] = x[i];
         }
         o[d] = mfma<kBf16>(v, pr[ks], o[d]);
       }
+    if constexpr (kApart) {
+      const int end = step * kKeys + kKeys < nk ? step * kKeys + kKeys : nk;
+#pragma unroll 1
+      for (int key = step * kKeys; key < end; ++key)
+        add_nonfinite<D, kBf16>(vb + int64_t(key) * a.v.token + 4 * half,
+                                key <= limit, o);
+    }
+  }
+  if constexpr (!kApart) {
+    float z = 0.0f;  // NaN if any sum is not finite
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) z = __builtin_fmaf(o[d][i], 0.0f, z);
+    const bool any = __any(z != z);
+    if (lane == 0) not_finite[wave] = any;
+    lds_barrier();
+    bool again = false;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) again |= not_finite[w];
+    if (__builtin_amdgcn_readfirstlane(again)) return true;
   }
   float la, lb;
   both<32>(l, &la, &lb);
@@ -530,10 +634,31 @@ __global__ __launch_bounds__(kWaves *kWave, 2) void prompt_kernel(PromptArgs a) 
             float4{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
     part[kThreads * (D / 2) + tid] = m;
     part[kThreads * (D / 2 + 1) + tid] = l;
-    return;
+  } else if (here) {
+    write_row<D, kBf16>(a, Row{tok, nq, q0, hq, half}, o, l);
   }
-  if (!here) return;
-  write_row<D, kBf16>(a, Row{tok, nq, q0, hq, half}, o, l);
+  return false;
+}
+
+template <int D, bool kBf16, int kWaves>
+__global__ __launch_bounds__(kWaves *kWave, 2) void prompt_kernel(PromptArgs a) {
+  using S = PromptShape<D, kWaves>;
+  __shared__ __attribute__((aligned(1024))) uint16_t lds[S::kStages * 2 * S::kTile];
+  __shared__ bool not_finite[kWaves];
+  if (!prompt_tile<D, kBf16, kWaves, false>(a, threadIdx.x, lds, not_finite)) return;
+  // from the arguments on, so that nothing is kept for this in the first loop
+  auto *args = __builtin_amdgcn_kernarg_segment_ptr();
+  int tid = threadIdx.x;
+  asm volatile("" : "+s"(args));
+  asm volatile("" : "+v"(tid));
+  uint64_t words[sizeof(PromptArgs) / 8];
+#pragma unroll
+  for (unsigned i = 0; i < sizeof(PromptArgs) / 8; ++i)
+    words[i] = CONSTANT_PTR(uint64_t, args)[i];
+  PromptArgs again;
+  static_assert(sizeof(words) == sizeof(again));
+  __builtin_memcpy(&again, words, sizeof(again));
+  prompt_tile<D, kBf16, kWaves, true>(again, tid, lds, not_finite);
 }
 
 // Puts the parts of cut tiles together, in their order: a workgroup for a tile
@@ -598,10 +723,24 @@ struct PromptPlan {
 // its size needs no device.
 constexpr int kMaxUnits = 256;
 
+// Wavefronts of a workgroup. Eight share a tile of keys among twice the queries
+// and keep two more tiles under way: 2.03 ms against 2.17 for one prompt of
+// 16,384 tokens (32 query heads over 8, D 128), 144 us against 153 for 4,096,
+// 83 against 86 for 8 x 2,048 tokens of 8 heads over one. Four, of which two
+// workgroups run on a compute unit, leave fewer lanes idle at the ends of
+// sequences and spread few tiles better: 106 us against 122 for 64 prompts of
+// 256 tokens, 98 against 103 for 8 of 1,024, 67 against 70 for one of 2,048,
+// 76 against 87 for 4,096 tokens of 8 heads over one behind 16,384.
+int prompt_waves(int32_t num_seqs, int64_t num_q, int32_t q_heads) {
+  const bool long_ones = num_q >= int64_t(num_seqs) * 2048;
+  const bool many = num_q * q_heads / (8 * 32) >= 2 * kMaxUnits;
+  return long_ones && many ? 8 : 4;
+}
+
 PromptPlan prompt_plan(int32_t num_seqs, int64_t num_q, int64_t num_k,
                        int32_t q_heads, int32_t kv_heads, int32_t head_dim, int cus) {
   PromptPlan p;
-  p.waves = 8;
+  p.waves = prompt_waves(num_seqs, num_q, q_heads);
   const int group = q_heads / kv_heads;
   p.heads_per_tile = p.waves;
   while (group % p.heads_per_tile) p.heads_per_tile /= 2;
@@ -686,6 +825,10 @@ int lumen_attn_prompt(const lumen_attn_rows *q, const lumen_attn_rows *k,
   if ((st = check_rows(q, num_q_tokens)) != LUMEN_OK) return st;
   if ((st = check_rows(k, num_k_tokens)) != LUMEN_OK) return st;
   if ((st = check_rows(v, num_k_tokens)) != LUMEN_OK) return st;
+  // a tile's rows are within 32 bits of its first
+  if (num_k_tokens > 1 && (k->token_stride > LUMEN_ATTN_MAX_STRIDE ||
+                           v->token_stride > LUMEN_ATTN_MAX_STRIDE))
+    return LUMEN_ERR_UNSUPPORTED;
   if (num_seqs > 0 && !d_cu_q) return LUMEN_ERR_INVALID_ARG;
   if (num_q_tokens > 0 && !d_out) return LUMEN_ERR_INVALID_ARG;
   if (!aligned(d_out, 16) || !aligned(d_workspace, 16) || !aligned(d_cu_q, 4) ||

@@ -170,6 +170,10 @@ def test_prompt_refusals(lib):
     for kw in (dict(dtype=2), dict(d=256), dict(d=96), dict(tq=1 << 31),
                dict(tk=1 << 31)):
         assert call(**kw) == kv.LUMEN_ERR_UNSUPPORTED, kw
+    far = rows(token=(1 << 24) + 8)
+    assert call(k=far) == kv.LUMEN_ERR_UNSUPPORTED
+    assert call(v=far) == kv.LUMEN_ERR_UNSUPPORTED
+    assert call(S=0, tq=1, tk=1, k=far, v=far) == kv.LUMEN_OK
     assert call(S=attn.LUMEN_ATTN_MAX_REQS + 1) == kv.LUMEN_ERR_TOO_MANY
     for kw in (dict(cu_q=ODD), dict(cu_k=ODD), dict(out=FAKE + 8),
                dict(status=ODD), dict(q=rows(FAKE + 8)),

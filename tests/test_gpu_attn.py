@@ -1,5 +1,7 @@
 """The serving operators on the GPU against plain references: slot maps, the
 4-bit cache's append and read, decode and prompt attention."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -629,6 +631,79 @@ def test_prompt_scale_and_sharp_scores():
 def test_prompt_many_sequences():
     rng = np.random.default_rng(4)
     check_prompt([int(x) for x in rng.integers(0, 9, 700)], None, 1, 2, 64, BF)
+
+
+def test_prompt_eight_wavefronts():
+    """Long sequences of many heads, which take the larger workgroups: a mean
+    of 2,048 queries and 131,072 rows."""
+    check_prompt([2048], None, 16, 4, 64, BF, seed=1)
+    check_prompt([2100, 0, 5500], [2200, 0, 5500], 2, 12, 128, FP, seed=2)
+
+
+@pytest.mark.parametrize("nq,nk,H,G,D", [
+    ([3], [9000], 1, 1, 128),          # one tile, many parts
+    ([40, 1, 90], [5000, 2100, 0], 2, 4, 128),
+    ([17, 64], [20011, 70], 1, 8, 64),
+    ([1] * 70 + [33], [64] * 70 + [8000], 2, 3, 64)])
+@pytest.mark.parametrize("dtype", [BF, FP])
+def test_prompt_few_rows_of_long_keys(nq, nk, H, G, D, dtype):
+    """Tiles whose keys are cut into parts, and joined."""
+    check_prompt(nq, nk, H, G, D, dtype, seed=len(nq))
+
+
+@pytest.mark.parametrize("H,G,D,dtype", [(2, 1, 64, BF), (1, 4, 128, FP),
+                                         (2, 8, 128, BF), (1, 2, 64, FP)])
+@pytest.mark.parametrize("nq,nk", [([70, 200], [70, 200]), ([33], [150]),
+                                   ([5, 130], [6000, 130])])
+def test_prompt_values_that_are_not_finite(H, G, D, dtype, nq, nk):
+    """NaN and infinities among a sequence's own values reach the queries that
+    see them, in their elements, and nothing else."""
+    g = torch.Generator(device=dev()).manual_seed(sum(nk))
+    q = torch.randn(sum(nq), H * G, D, generator=g, device=dev()).to(dtype)
+    k, v = (torch.randn(sum(nk), H, D, generator=g, device=dev()).to(dtype)
+            for _ in range(2))
+    cu_q, cu_k = np.cumsum([0] + nq), np.cumsum([0] + nk)
+    want, slack = prompt_want(q, k, v, cu_q, cu_k, D ** -0.5, ref.UNIT[dtype])
+    # (sequence, key from its end, head, element, value)
+    bad = [(s, back, h, e, x) for s in range(len(nq)) for h in range(H)
+           for back, e, x in ((1, 3, "nan"), (2, 40, "inf"), (30, 63, "-inf"),
+                              (31, 0, "nan"), (nk[s], D - 1, "inf"))
+           if back <= nk[s]]
+    for s, back, h, e, x in bad:
+        key = nk[s] - back
+        v[cu_k[s] + key, h, e] = float(x)
+        first = max(0, key - (nk[s] - nq[s]))  # query that sees it
+        rows = slice(int(cu_q[s]) + first, int(cu_q[s + 1]))
+        heads = slice(h * G, h * G + G)
+        want[rows, heads, e] += float(x)
+    out, status = torch.full_like(q, 7.0), word()
+    attn.lumen_attn_prompt(q, k, v, out, i32(cu_q), status, cu_k=i32(cu_k))
+    assert int(status) == 0
+    got, fine = out.double(), torch.isfinite(want)
+    assert torch.equal(torch.isnan(got), torch.isnan(want))
+    inf = torch.isinf(want)
+    assert torch.equal(torch.isinf(got), inf)
+    assert torch.equal(got[inf], want[inf])
+    zero = torch.zeros_like(want)
+    ref.assert_close(torch.where(fine, got, zero), torch.where(fine, want, zero),
+                     torch.where(fine, slack, zero), dtype)
+
+
+def test_prompt_many_small_weights():
+    """One key far above 70,000 others whose weights are 2^-25 of it each: in
+    fp16 they would round to 0."""
+    n, D = 70001, 64
+    q = torch.zeros(1, 1, D, dtype=FP, device=dev())
+    k = torch.zeros(n, 1, D, dtype=FP, device=dev())
+    v = torch.ones(n, 1, D, dtype=FP, device=dev())
+    q[..., 0], k[7, :, 0], v[7] = 1.0, 25 * math.log(2), -1.0
+    out, status = torch.empty_like(q), word()
+    cu_q, cu_k = [0, 1], [0, n]
+    attn.lumen_attn_prompt(q, k, v, out, i32(cu_q), status, cu_k=i32(cu_k),
+                           scale=1.0)
+    want, slack = prompt_want(q, k, v, cu_q, cu_k, 1.0, ref.UNIT[FP])
+    assert int(status) == 0
+    ref.assert_close(out, want, slack, FP)
 
 
 def test_prompt_bad_bounds():
