@@ -161,10 +161,14 @@ __device__ __forceinline__ Unit find_tile(const PromptArgs &a, int rank) {
 }
 
 // The plan: every tile by falling work, so that the long ones start first and
-// the short ones fill the end; those with more steps than a workgroup's slot
-// has to do on average go in equal parts of about half of that (at least
-// kMinPartKeys), so that few long rows fill the chip as many short ones do.  One
-// workgroup: tiles are counted by work into kPlanThreads bins, the bins are
+// the short ones fill the end.  A part is three quarters of the steps that a
+// workgroup's slot has to do on average, at least kMinPartKeys, and tiles of
+// more than twice that are cut into equal parts of at most a part, so that few
+// long rows fill the chip as many short ones do.  (Smaller parts balance better
+// and cost more to join: 5 suffixes of 1,237 tokens behind up to 11,003 take 153
+// us, against 164 with a half and 175 with the whole average; 8 of 300 behind up
+// to 5,000 take 110, 113 and 114; 2 of 128 behind up to 16,384 take 68, 78 and
+// 58.)  One workgroup: tiles are counted by work into kPlanThreads bins, the bins are
 // summed from the top, and each tile takes the next place of its bin.  Which of
 // two tiles of a bin comes first changes nothing but that order.
 constexpr int kPlanThreads = 1024;
@@ -223,8 +227,8 @@ __global__ __launch_bounds__(kPlanThreads) void prompt_plan_kernel(PromptArgs a)
   __syncthreads();
   // more steps than this: a cut into parts of `part` steps or a little less
   const uint64_t share = sum / uint32_t(a.slots);
-  const int half = share < 0x3fffffff ? int(share / 2) + 1 : 0x3fffffff;
-  const int part = half > kMinPartKeys / kKeys ? half : kMinPartKeys / kKeys;
+  const int most = share < 0x1fffffff ? int(share * 3 / 4) + 1 : 0x1fffffff;
+  const int part = most > kMinPartKeys / kKeys ? most : kMinPartKeys / kKeys;
   const int whole = a.max_parts ? 2 * part : 0x7fffffff;
   // a bin of work, the most in bin 0
   const float scale = float(kPlanThreads - 1) / float(top + 1);
@@ -309,29 +313,27 @@ struct Row {
   int hq, half;
 };
 
+// 32 elements of it from element 32 * d on.
 template <int D, bool kBf16>
-__device__ __forceinline__ void write_row(const PromptArgs &a, const Row &r,
-                                          const f32x16 *o, float l) {
+__device__ __forceinline__ void write_row(const PromptArgs &a, const Row &r, int d,
+                                          const f32x16 &o, float l) {
   const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
-  uint16_t *out = a.out + ((r.q0 + r.tok) * a.q_heads + r.hq) * D;
+  uint16_t *out = a.out + ((r.q0 + r.tok) * a.q_heads + r.hq) * D + d * 32;
 #pragma unroll
-  for (int d = 0; d < D / 32; ++d)
+  for (int g = 0; g < 2; ++g) {
+    uint32_t w[4];
 #pragma unroll
-    for (int g = 0; g < 2; ++g) {
-      uint32_t w[4];
-#pragma unroll
-      for (int b = 0; b < 4; ++b) {
-        const int i = 8 * g + 2 * b;
-        w[b] = uint32_t(rounded<kBf16>(o[d][i] * inv)) |
-               uint32_t(rounded<kBf16>(o[d][i + 1] * inv)) << 16;
-      }
-      const auto x = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
-      const auto y = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
-      const uint32_t x0 = x[0], y0 = y[0], x1 = x[1], y1 = y[1];
-      if (r.tok < r.nq)
-        *reinterpret_cast<uint4 *>(out + d * 32 + 16 * g + 8 * r.half) =
-            uint4{x0, y0, x1, y1};
+    for (int b = 0; b < 4; ++b) {
+      const int i = 8 * g + 2 * b;
+      w[b] = uint32_t(rounded<kBf16>(o[i] * inv)) |
+             uint32_t(rounded<kBf16>(o[i + 1] * inv)) << 16;
     }
+    const auto x = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
+    const auto y = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+    const uint32_t x0 = x[0], y0 = y[0], x1 = x[1], y1 = y[1];
+    if (r.tok < r.nq)
+      *reinterpret_cast<uint4 *>(out + 16 * g + 8 * r.half) = uint4{x0, y0, x1, y1};
+  }
 }
 
 template <bool kBf16>
@@ -635,7 +637,9 @@ __device__ __forceinline__ bool prompt_tile(const PromptArgs &a, const int tid,
     part[kThreads * (D / 2) + tid] = m;
     part[kThreads * (D / 2 + 1) + tid] = l;
   } else if (here) {
-    write_row<D, kBf16>(a, Row{tok, nq, q0, hq, half}, o, l);
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+      write_row<D, kBf16>(a, Row{tok, nq, q0, hq, half}, d, o[d], l);
   }
   return false;
 }
@@ -661,49 +665,49 @@ __global__ __launch_bounds__(kWaves *kWave, 2) void prompt_kernel(PromptArgs a) 
   prompt_tile<D, kBf16, kWaves, true>(again, tid, lds, not_finite);
 }
 
-// Puts the parts of cut tiles together, in their order: a workgroup for a tile
-// and set of heads, with the lanes' places of prompt_kernel.
+// Puts the parts of cut tiles together, in their order: a workgroup for 32
+// elements of a tile's rows of a set of heads, with the lanes' places of
+// prompt_kernel.  A tile of few rows over long keys may have tens of parts:
+// their loads do not wait for one another.
 template <int D, bool kBf16, int kWaves>
 __global__ __launch_bounds__(kWaves *kWave, 2) void prompt_join_kernel(PromptArgs a) {
   constexpr int kThreads = kWaves * kWave;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int gp = a.heads_per_tile, groups = a.q_heads / gp;
-  const int items = *a.num_cuts * groups;
+  const int items = *a.num_cuts * groups * (D / 32);
   for (int item = blockIdx.x; item < items; item += gridDim.x) {
-    const Cut cut = a.cuts[item / groups];
-    const int hg = item % groups;
+    const int d = item % (D / 32), hg = item / (D / 32) % groups;
+    const Cut cut = a.cuts[item / (D / 32) / groups];
     const Unit u = a.units[cut.unit];
     const Row r{u.t0 + wave / gp * 32 + (lane & 31), u.nq, u.q0, hg * gp + wave % gp,
                 lane >> 5};
-    f32x16 o[D / 32];
+    const int64_t apart = int64_t(groups) * part_floats(D, kWaves);
+    const float *part = a.parts + (int64_t(u.place) * groups + hg) * part_floats(D, kWaves);
+    const float *ms = part + kThreads * (D / 2) + tid, *ls = ms + kThreads;
+    const float *os = part + (d * 4 * kThreads + tid) * 4;
     float m = -INFINITY, l = 0.0f;
+#pragma unroll 8
+    for (int c = 0; c < cut.parts; ++c) m = fmaxf(m, ms[c * apart]);
+    f32x16 o;
 #pragma unroll
-    for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
+    for (int i = 0; i < 16; ++i) o[i] = 0.0f;
+    // no key of any part is seen: all sums are 0
+    const float shift = m == -INFINITY ? 0.0f : m;
+#pragma unroll 4
     for (int c = 0; c < cut.parts; ++c) {
-      const float *part =
-          a.parts + (int64_t(u.place + c) * groups + hg) * part_floats(D, kWaves);
-      const float pm = part[kThreads * (D / 2) + tid];
-      const float pl = part[kThreads * (D / 2 + 1) + tid];
-      const float mn = fmaxf(m, pm);
-      const float c0 = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
-      const float c1 = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(pm - mn);
-      m = mn;
-      l = l * c0 + pl * c1;
+      const float w = __builtin_amdgcn_exp2f(ms[c * apart] - shift);
+      l = __builtin_fmaf(ls[c * apart], w, l);
 #pragma unroll
-      for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float4 x =
-              *reinterpret_cast<const float4 *>(part + ((d * 4 + i) * kThreads + tid) * 4);
-          o[d][4 * i] = o[d][4 * i] * c0 + x.x * c1;
-          o[d][4 * i + 1] = o[d][4 * i + 1] * c0 + x.y * c1;
-          o[d][4 * i + 2] = o[d][4 * i + 2] * c0 + x.z * c1;
-          o[d][4 * i + 3] = o[d][4 * i + 3] * c0 + x.w * c1;
-        }
+      for (int i = 0; i < 4; ++i) {
+        const float4 x =
+            *reinterpret_cast<const float4 *>(os + c * apart + i * kThreads * 4);
+        o[4 * i] = __builtin_fmaf(x.x, w, o[4 * i]);
+        o[4 * i + 1] = __builtin_fmaf(x.y, w, o[4 * i + 1]);
+        o[4 * i + 2] = __builtin_fmaf(x.z, w, o[4 * i + 2]);
+        o[4 * i + 3] = __builtin_fmaf(x.w, w, o[4 * i + 3]);
+      }
     }
-    write_row<D, kBf16>(a, r, o, l);
+    write_row<D, kBf16>(a, r, d, o, l);
   }
 }
 
@@ -753,7 +757,7 @@ PromptPlan prompt_plan(int32_t num_seqs, int64_t num_q, int64_t num_k,
   p.parts = 0;
   if (num_k >= kCutKeys) {
     // a cut tile has less than twice its steps over `part`'s parts, and `part`
-    // is at least half a slot's share of all steps
+    // is at least three quarters of a slot's share of all steps
     p.parts = int64_t(p.slots) * 4;
     const int64_t most = p.tiles * (num_k / kMinPartKeys + 2);
     if (p.parts > most) p.parts = most;
@@ -878,8 +882,8 @@ int lumen_attn_prompt(const lumen_attn_rows *q, const lumen_attn_rows *k,
   hipLaunchKernelGGL(kernels.main, dim3(unsigned((p.tiles + p.parts) * p.groups)),
                      threads, 0, s, a);
   if (p.parts) {
-    int64_t items = p.parts / 2 * p.groups;
-    if (items > cus) items = cus;
+    int64_t items = p.parts / 2 * p.groups * (head_dim / 32);
+    if (items > 4 * cus) items = 4 * cus;
     hipLaunchKernelGGL(kernels.join, dim3(unsigned(items < 1 ? 1 : items)), threads, 0, s, a);
   }
   return hipGetLastError() == hipSuccess ? LUMEN_OK : LUMEN_ERR_HIP;
