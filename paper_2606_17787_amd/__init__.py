@@ -4,6 +4,7 @@ Modules:
   kvckpt     Python binding of the HIP library (include/lumen_kv_ckpt.h)
   attn       slot maps, 4-bit paged cache, decode and prompt attention
              (include/lumen_attn.h)
+  recover4   example: serving from a 4-bit cache, a failure and the recovery
   build      in-tree hipcc build of the library for gfx950
   workloads  seeded synthetic inputs (cache shapes, ranges, block tables)
 
