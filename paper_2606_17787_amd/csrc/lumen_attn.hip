@@ -19,7 +19,10 @@ using namespace lumen_attn_detail;
 // ---------------------------------------------------------------- slots
 
 constexpr int kSlotThreads = 256;
-constexpr int kSlotTokens = 4;  // consecutive tokens a thread maps at a time
+// Consecutive tokens that a thread maps at a time, one page lookup after another
+// (8 new tokens take 4.9 us with 2, 6.4 with 4 and 9.5 with 8; 1,024 prompts of
+// 512 tokens 16.2, 16.8 and 16.1).
+constexpr int kSlotTokens = 2;
 constexpr uint32_t kHeld = 0x7fffffffu;  // token and page sums are held to this
 
 // Sums of counts held to kHeld: associative, so any order of the scan gives
@@ -52,8 +55,10 @@ struct SlotReq {
   bool range;       // refused with RANGE
 };
 
+// tokens >= 0; divided without the sign, in 32 bits
 __device__ __forceinline__ int32_t pages_of(int32_t tokens, int32_t bs) {
-  return int32_t((int64_t(tokens) + bs - 1) / bs);
+  const uint32_t whole = uint32_t(tokens) / uint32_t(bs);
+  return int32_t(whole + (whole * uint32_t(bs) != uint32_t(tokens)));
 }
 
 __device__ __forceinline__ SlotReq slot_req(const SlotArgs &a, int r) {
@@ -156,19 +161,22 @@ __global__ __launch_bounds__(kSlotThreads) void slots_kernel(SlotArgs a) {
 
   const int64_t grid = int64_t(gridDim.x) * kSlotThreads;
   const int64_t me = int64_t(blockIdx.x) * kSlotThreads + tid;
+  // a thread's tokens are consecutive: the request is looked for once, the page
+  // once each block_size tokens
   for (int64_t i0 = me * kSlotTokens; i0 < a.num_slots; i0 += grid * kSlotTokens) {
     int r = -1;
-    int32_t s = 0, first = 0;
-    uint32_t b = 0;
-    bool ok = false;
+    uint32_t end = 0;          // of request r's tokens
+    int32_t page = 0, pos = 0; // of the token
+    int32_t id = -1;           // of the page, -1 where there is none
     for (int k = 0; k < kSlotTokens; ++k) {
       const int64_t i = i0 + k;
       if (i >= a.num_slots) break;
       int64_t slot = -1;
       if (i < int64_t(total)) {
         const uint32_t u = uint32_t(i);
-        if (r < 0 || u >= cu[r + 1]) {
-          int lo = r < 0 ? 0 : r + 1, hi = R - 1;  // last r with cu[r] <= u
+        const bool other = u >= end;
+        if (other) {
+          int lo = r + 1, hi = R - 1;  // last r with cu[r] <= u
           while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
             if (cu[mid] <= u)
@@ -177,24 +185,30 @@ __global__ __launch_bounds__(kSlotThreads) void slots_kernel(SlotArgs a) {
               hi = mid - 1;
           }
           r = lo;
+          end = cu[r + 1];
+          const uint32_t tok = uint32_t(a.start[r]) + (u - cu[r]);
+          page = int32_t(tok / uint32_t(a.block_size));
+          pos = int32_t(tok - uint32_t(page) * uint32_t(a.block_size));
+        } else if (++pos == a.block_size) {
+          pos = 0;
+          ++page;
+        }
+        if (other || pos == 0) {
           const SlotReq q = slot_req(a, r);
-          s = a.start[r];
-          first = q.first;
-          b = base[r];
-          ok = !q.range && (q.need == 0 || add_held(b, q.need) <= count);
-          if (q.need == 0) first = 0x7fffffff;  // every page is in the table
+          const uint32_t b = base[r];
+          id = -1;
+          if (!q.range && (q.need == 0 || add_held(b, q.need) <= count)) {
+            // where nothing is new, every page is in the table
+            id = q.need && page >= q.first
+                     ? a.free_ids[count - 1 - b - uint32_t(page - q.first)]
+                     : a.bt[int64_t(r) * a.bt_cols + page];
+            if (id < 0 || id >= a.num_blocks) {
+              id = -1;
+              err = err < LUMEN_ERR_BLOCK_ID ? err : LUMEN_ERR_BLOCK_ID;
+            }
+          }
         }
-        if (ok) {
-          const int32_t tok = s + int32_t(u - cu[r]);
-          const int32_t page = tok / a.block_size;
-          const int32_t id =
-              page >= first ? a.free_ids[count - 1 - b - uint32_t(page - first)]
-                            : a.bt[int64_t(r) * a.bt_cols + page];
-          if (id >= 0 && id < a.num_blocks)
-            slot = int64_t(id) * a.block_size + (tok - page * a.block_size);
-          else
-            err = err < LUMEN_ERR_BLOCK_ID ? err : LUMEN_ERR_BLOCK_ID;
-        }
+        if (id >= 0) slot = int64_t(id) * a.block_size + pos;
       }
       a.slots[i] = slot;
     }
@@ -479,8 +493,9 @@ enum class Sharing { kLines, kStep, kNone };
 // order of their addresses, kStages steps in turn: what is in flight takes no
 // registers, and each cache line is asked for once (a wavefront that reads its
 // own head's 80 bytes out of each 640 makes the first-level cache fetch 1.5
-// lines for 80 bytes: 2.2 TB/s).  Block ids come the same way, kStages steps
-// before the rows they lead to.
+// lines for 80 bytes: 2.2 TB/s).  Where a round's rows start, and which of its
+// keys count, is laid out in LDS before the round, so that a step's addresses
+// are one read and one addition.
 //
 // One block of 32 keys: scores^T = K Q^T and sums^T = V^T P^T by 16x16x32
 // products of 16-bit floats, queries across (the heads of the group, up to 16).
@@ -492,6 +507,12 @@ enum class Sharing { kLines, kStep, kNone };
 // lane holds D/16 consecutive elements of 8 keys, all of one quarter.  Values
 // are exact: code and pair give the stored value by one fused multiply-add that
 // rounds as the format says.
+//
+// Measured, D 128, a large copy being 4.85 TB/s: 256 requests around 2,048
+// tokens, 32 query heads over 8, 181 us, 4.9 TB/s; 512 around 4,096 of 8 over
+// one, 119 us, 3.7 TB/s (a wavefront's own rows, 1,280 bytes of a page at a
+// time); three of 100,000, 96 us, 4.1 TB/s (the join is 4.5 us of it).  D 256, 64
+// requests of 4,096 tokens, 32 query heads over 8: 141 us, 4.3 TB/s.
 template <int D, Sharing kSharing>
 __global__ __launch_bounds__(kDecodeThreads, 2) void decode4_kernel(DecodeArgs a) {
   constexpr bool kPrivate = kSharing == Sharing::kNone;
@@ -600,8 +621,10 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void decode4_kernel(DecodeArgs a
   // keys of a tile: the largest power of two up to 16 that divides a page
   const int low = a.block_size & -a.block_size;
   const int tile_shift = low >= 16 ? 4 : __builtin_ctz(low);
-  int tile[kIssues];             // of the step, that the piece is in
-  const uint8_t *piece[kIssues]; // its place in a tile at byte 0
+  int tile[kIssues];       // of the step, that the piece is in; below 0 of V
+  uint32_t piece[kIssues]; // its place in a tile's rows of the heads
+  const int64_t heads_at = int64_t(a.hnd ? h0 * a.block_size : h0) * kRow;
+  const uint8_t *const k_at = a.k + heads_at, *const v_of = a.v + heads_at;
 #pragma unroll
   for (int i = 0; i < kIssues; ++i) {
     // kNone: a wavefront loads its own block's rows
@@ -614,11 +637,12 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void decode4_kernel(DecodeArgs a
     int x = c - t * pieces - turn(t);
     if (kPrivate) t += kbi * kBlockKeys;
     x = x < 0 ? x + pieces : x;
-    tile[i] = t >> tile_shift;
-    piece[i] = (is_v ? a.v : a.k) + (t & ((1 << tile_shift) - 1)) * slot_bytes +
-               int64_t(a.hnd ? h0 * a.block_size : h0 + x / kParts) * kRow +
-               x % kParts * 16;
+    tile[i] = t >> tile_shift | (is_v ? INT32_MIN : 0);
+    piece[i] = (t & ((1 << tile_shift) - 1)) * slot_bytes + x * 16;
   }
+  const auto address = [&](int i, int step_tile) __attribute__((always_inline)) {
+    return (tile[i] < 0 ? v_of : k_at) + piece[i] + tile_at[step_tile + (tile[i] & 0xffff)];
+  };
   const int step_tiles = step_keys >> tile_shift;
   int round = kTiles / step_tiles;  // steps
   round = round < kLive / a.wg_blocks ? round : kLive / a.wg_blocks;
@@ -652,20 +676,29 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void decode4_kernel(DecodeArgs a
   // and fp16 keep all their bits whatever their range
   half8v q[kSteps];
   float cq = 0.0f;
-  uint4 raw[kSteps];
+  uint4 raw[D == 256 ? 1 : kSteps];
+  // (for D 256 there are no registers to hold a row as it is, so it is read
+  // once more)
+  constexpr bool kTwice = D == 256;
+  const uint16_t *q_row = nullptr;
   const auto fetch_q = [&](int req) __attribute__((always_inline)) {
     const int row = (h0 + hi) * a.group + g0 + (n < rows ? n : 0);
-    const uint16_t *p =
-        a.q.base + int64_t(req) * a.q.token + row * a.q.head + quad * (D / 4);
+    q_row = a.q.base + int64_t(req) * a.q.token + row * a.q.head + quad * (D / 4);
+    if constexpr (!kTwice) {
 #pragma unroll
-    for (int i = 0; i < kSteps; ++i)
-      raw[i] = *reinterpret_cast<const uint4 *>(p + 8 * i);
+      for (int i = 0; i < kSteps; ++i)
+        raw[i] = *reinterpret_cast<const uint4 *>(q_row + 8 * i);
+    }
   };
   const auto take_q = [&]() __attribute__((always_inline)) {
+    const auto part = [&](int i, float *x) __attribute__((always_inline)) {
+      if constexpr (kTwice) raw[0] = *reinterpret_cast<const uint4 *>(q_row + 8 * i);
+      a.bf16 ? unpack8<true>(raw[kTwice ? 0 : i], x) : unpack8<false>(raw[kTwice ? 0 : i], x);
+    };
     float big = 0.0f, x[8];
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
-      a.bf16 ? unpack8<true>(raw[i], x) : unpack8<false>(raw[i], x);
+      part(i, x);
 #pragma unroll
       for (int j = 0; j < 8; ++j) big = fmaxf(big, fabsf(x[j]));
     }
@@ -674,9 +707,10 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void decode4_kernel(DecodeArgs a
     e = e == 255 ? 140 : e < 14 ? 14 : e;
     const float up = __builtin_bit_cast(float, (267 - e) << 23);  // to 2^13..2^14
     cq = a.scale_log2 * __builtin_bit_cast(float, (e - 13) << 23);
+    if constexpr (kTwice) asm volatile("" ::: "memory");
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
-      a.bf16 ? unpack8<true>(raw[i], x) : unpack8<false>(raw[i], x);
+      part(i, x);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         q[i][2 * j] = _Float16(x[j] * up);
@@ -711,21 +745,27 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void decode4_kernel(DecodeArgs a
       }
     }
     uint32_t vc[8][kE >= 8 ? kE / 8 : 1], vp[8];  // V: the lane's elements of 8 keys
+    const auto read_v = [&]() __attribute__((always_inline)) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const uint8_t *row = stage + v_at + ((j & 1) + (j & 4) * 4) * key_bytes;
-      vp[j] = *reinterpret_cast<const uint32_t *>(row + at_vp[j / 2 % 2]);
-      row += at_v[j / 2 % 2];
-      if constexpr (D == 64) {
-        vc[j][0] = *reinterpret_cast<const uint16_t *>(row);
-      } else if constexpr (D == 128) {
-        vc[j][0] = *reinterpret_cast<const uint32_t *>(row);
-      } else {
-        const uint2 x = *reinterpret_cast<const uint2 *>(row);
-        vc[j][0] = x.x, vc[j][kE / 8 - 1] = x.y;
+      for (int j = 0; j < 8; ++j) {
+        const uint8_t *row = stage + v_at + ((j & 1) + (j & 4) * 4) * key_bytes;
+        vp[j] = *reinterpret_cast<const uint32_t *>(row + at_vp[j / 2 % 2]);
+        row += at_v[j / 2 % 2];
+        if constexpr (D == 64) {
+          vc[j][0] = *reinterpret_cast<const uint16_t *>(row);
+        } else if constexpr (D == 128) {
+          vc[j][0] = *reinterpret_cast<const uint32_t *>(row);
+        } else {
+          const uint2 x = *reinterpret_cast<const uint2 *>(row);
+          vc[j][0] = x.x, vc[j][kE / 8 - 1] = x.y;
+        }
       }
+    };
+    // for D 256 there are no registers to hold both at once
+    if constexpr (D != 256) {
+      read_v();
+      __builtin_amdgcn_sched_barrier(0);
     }
-    if constexpr (D != 256) __builtin_amdgcn_sched_barrier(0);
     float4v s[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
@@ -745,6 +785,10 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void decode4_kernel(DecodeArgs a
         }
         s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f, q[i], s[t], 0, 0, 0);
       }
+    }
+    if constexpr (D == 256) {
+      __builtin_amdgcn_sched_barrier(0);
+      read_v();
     }
     if (live != 0xffffffffu) {
       // a key left out has no score, and no value either: its pair may be NaN
@@ -1000,7 +1044,7 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void decode4_kernel(DecodeArgs a
         i = i < count ? i : count - 1;
 #pragma unroll
         for (int c = 0; c < kIssues; ++c)
-          from[c] = piece[c] + tile_at[i * step_tiles + tile[c]];
+          from[c] = address(c, i * step_tiles);
       };
       const auto start = [&](int i, int stage) __attribute__((always_inline)) {
         if (i >= count) return;
