@@ -406,6 +406,17 @@ def test_decode_long_and_many(lens):
     check_decode(rng, lens, 2, 4, 128, 16, "NHD", BF)
 
 
+@pytest.mark.parametrize("order", ["NHD", "HND"])
+@pytest.mark.parametrize("H", [3, 5, 6, 7, 9, 11, 12, 16, 24])
+def test_decode_head_counts(H, order):
+    """Workgroups of every number of heads that lie together, and head counts
+    of which a workgroup takes a part."""
+    rng = np.random.default_rng(H)
+    check_decode(rng, [1, 700, 33, 1290, 0, 128], H, 2, 128, 16, order, BF)
+    check_decode(rng, [40, 515], H, 1, 64, 24, order, FP)
+    check_decode(rng, [300, 1, 77], H, 3, 256, 8, order, BF)
+
+
 def test_decode_one_long_request_of_one_head():
     rng = np.random.default_rng(77)
     check_decode(rng, [120001], 1, 8, 64, 32, "HND", FP)
