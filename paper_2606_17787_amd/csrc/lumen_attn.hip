@@ -20,8 +20,8 @@ using namespace lumen_attn_detail;
 
 constexpr int kSlotThreads = 256;
 // Consecutive tokens that a thread maps at a time, one page lookup after another
-// (8 new tokens take 4.9 us with 2, 6.4 with 4 and 9.5 with 8; 1,024 prompts of
-// 512 tokens 16.2, 16.8 and 16.1).
+// (8 new tokens take 4.7 us with 2, 6.4 with 4 and 9.5 with 8; 1,024 prompts of
+// 512 tokens 16.2, 16.8 and 16.1 with two workgroups a compute unit).
 constexpr int kSlotTokens = 2;
 constexpr uint32_t kHeld = 0x7fffffffu;  // token and page sums are held to this
 
@@ -1345,7 +1345,9 @@ int lumen_attn_slots(const int32_t *d_start, const int32_t *d_end,
   const int64_t page_wgs = pages < num_reqs / 16 + 1 ? pages : num_reqs / 16 + 1;
   if (blocks < page_wgs) blocks = page_wgs;
   if (blocks < 1) blocks = 1;
-  if (blocks > int64_t(cus) * 2) blocks = int64_t(cus) * 2;
+  // more of them would scan the requests for too few tokens each (1,024 prompts of
+  // 512 tokens: 16.2 us with 2 a compute unit, 14.6 with 4, 16.4 with 8)
+  if (blocks > int64_t(cus) * 4) blocks = int64_t(cus) * 4;
   hipLaunchKernelGGL(slots_kernel, dim3(unsigned(blocks)), dim3(kSlotThreads),
                      2 * (size_t(num_reqs) + 1) * sizeof(uint32_t),
                      static_cast<hipStream_t>(stream), a);
