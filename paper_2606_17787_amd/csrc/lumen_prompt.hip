@@ -275,7 +275,11 @@ __global__ __launch_bounds__(kPlanThreads) void prompt_plan_kernel(PromptArgs a)
     const uint32_t at = atomicAdd(&bins[bin_of(u.last / parts)], uint32_t(parts));
     // more units, or parts, than there is room for are possible only where
     // sequences share queries
-    if (at + uint32_t(parts) > uint32_t(a.num_units)) continue;
+    if (at + uint32_t(parts) > uint32_t(a.num_units)) {
+      // places of it that there are hold no unit
+      for (uint32_t x = at; x < uint32_t(a.num_units); ++x) a.units[x].nq = 0;
+      continue;
+    }
     if (parts == 1) {
       a.units[at] = u;
       continue;

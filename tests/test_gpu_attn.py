@@ -736,6 +736,26 @@ def test_prompt_bad_bounds():
     assert int(status) == ref.RANGE
 
 
+def test_prompt_sequences_that_share_queries():
+    """Bounds that go back and forth: more tiles than queries have room for.
+    Every row is a sequence's or not written."""
+    g = torch.Generator(device=dev()).manual_seed(3)
+    n, m, H, G, D = 200, 9000, 1, 8, 64
+    q = torch.randn(n, H * G, D, generator=g, device=dev()).to(BF)
+    k, v = (torch.randn(m, H, D, generator=g, device=dev()).to(BF)
+            for _ in range(2))
+    want, slack = prompt_want(q, k, v, [0, n], [0, m], D ** -0.5, ref.UNIT[BF])
+    out, status = torch.full_like(q, 7.0), word()
+    attn.lumen_attn_prompt(q, k, v, out, i32([0, n] * 600), status,
+                           cu_k=i32([0, m] * 600))
+    assert int(status) == ref.RANGE
+    written = (out != 7.0).any(-1, keepdim=True).expand_as(out)
+    assert bool(written.any())
+    seven, zero = torch.full_like(want, 7.0), torch.zeros_like(want)
+    ref.assert_close(out, torch.where(written, want, seven),
+                     torch.where(written, slack, zero), BF)
+
+
 # ------------------------------------------------- streams, graphs, together
 
 def test_calls_on_another_stream_and_in_a_graph():
