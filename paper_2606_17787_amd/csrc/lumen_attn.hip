@@ -1377,7 +1377,7 @@ size_t lumen_attn_decode4_workspace_bytes(const lumen_kv_layout *layout,
                                           int32_t num_q_heads) {
   Layer at;
   if (check_layout(layout, 0, &at) != LUMEN_OK || num_reqs < 0 ||
-      num_reqs > LUMEN_ATTN_MAX_REQS || num_q_heads < 1 ||
+      num_reqs > LUMEN_ATTN_MAX_REQS || num_q_heads < 1 || num_q_heads > 65535 ||
       num_q_heads % layout->num_kv_heads)
     return 0;
   return decode_plan(layout, at.head_dim, num_reqs, num_q_heads, kMaxUnits).bytes;

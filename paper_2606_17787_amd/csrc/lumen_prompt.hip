@@ -772,8 +772,11 @@ PromptPlan prompt_plan(int32_t num_seqs, int64_t num_q, int64_t num_k,
   while (group % p.heads_per_tile) p.heads_per_tile /= 2;
   p.tile_tokens = 32 * p.waves / p.heads_per_tile;
   p.groups = q_heads / p.heads_per_tile;
-  p.slots = (cus < kMaxUnits ? cus : kMaxUnits) * 8 / p.waves / p.groups;
-  if (p.slots < 1) p.slots = 1;
+  const auto slots = [&](int units) {
+    const int n = units * 8 / p.waves / p.groups;
+    return n < 1 ? 1 : n;
+  };
+  p.slots = slots(cus < kMaxUnits ? cus : kMaxUnits);
   // at most a part-filled tile for each sequence beside the full ones
   p.tiles = num_q / p.tile_tokens + num_seqs;
   p.parts = 0;
@@ -784,7 +787,9 @@ PromptPlan prompt_plan(int32_t num_seqs, int64_t num_q, int64_t num_k,
     const int64_t most = p.tiles * (num_k / kMinPartKeys + 2);
     if (p.parts > most) p.parts = most;
   }
-  p.planned = p.parts > 0 || p.tiles > p.slots;
+  // the same for every device, as the workspace's size is: a small device takes
+  // a call's few tiles without a plan too, in another order
+  p.planned = p.parts > 0 || p.tiles > slots(kMaxUnits);
   const auto up = [](size_t n) { return (n + 255) & ~size_t(255); };
   p.units_at = 256;  // the number of cuts stands first
   p.cuts_at = p.units_at + up(size_t(p.tiles + p.parts) * sizeof(Unit));
@@ -793,6 +798,11 @@ PromptPlan prompt_plan(int32_t num_seqs, int64_t num_q, int64_t num_k,
                        : p.parts_at + size_t(p.parts) * p.groups *
                                           part_floats(head_dim, p.waves) * sizeof(float);
   return p;
+}
+
+// A grid of more workgroups than a launch takes.
+bool too_many_groups(const PromptPlan &p) {
+  return (p.tiles + p.parts) * p.groups > INT32_MAX;
 }
 
 struct PromptKernels {
@@ -827,8 +837,9 @@ size_t lumen_attn_prompt_workspace_bytes(int32_t num_seqs, int64_t num_q_tokens,
   if (check_prompt(num_seqs, num_q_tokens, num_k_tokens, num_q_heads, num_kv_heads,
                    head_dim) != LUMEN_OK)
     return 0;
-  return prompt_plan(num_seqs, num_q_tokens, num_k_tokens, num_q_heads, num_kv_heads,
-                     head_dim, kMaxUnits).bytes;
+  const PromptPlan p = prompt_plan(num_seqs, num_q_tokens, num_k_tokens, num_q_heads,
+                                   num_kv_heads, head_dim, kMaxUnits);
+  return too_many_groups(p) ? 0 : p.bytes;
 }
 
 int lumen_attn_prompt(const lumen_attn_rows *q, const lumen_attn_rows *k,
@@ -865,9 +876,9 @@ int lumen_attn_prompt(const lumen_attn_rows *q, const lumen_attn_rows *k,
   if ((st = compute_units(&cus)) != LUMEN_OK) return st;
   const PromptPlan p = prompt_plan(num_seqs, num_q_tokens, num_k_tokens, num_q_heads,
                                    num_kv_heads, head_dim, cus);
+  if (too_many_groups(p)) return LUMEN_ERR_UNSUPPORTED;
   if (p.planned && (!d_workspace || workspace_bytes < p.bytes))
     return LUMEN_ERR_INVALID_ARG;
-  if ((p.tiles + p.parts) * p.groups > INT32_MAX) return LUMEN_ERR_UNSUPPORTED;
   (void)hipGetLastError();
   PromptArgs a;
   a.q = rows_of(q, 0);

@@ -194,6 +194,20 @@ def test_prompt_workspace(lib):
         most = n
 
 
+def test_workspace_of_refused_sizes(lib):
+    """0 for every size that the call itself refuses."""
+    f = lib.lumen_attn_decode4_workspace_bytes
+    assert f(layout(num_kv_heads=1), 2, 65535) > 0
+    assert f(layout(num_kv_heads=1), 2, 65536) == 0
+    g = lib.lumen_attn_prompt_workspace_bytes
+    assert g(1, 1 << 27, 1 << 27, 8, 8, 128) > 0
+    # 2^27 tokens of 4,096 heads: more workgroups than a launch takes
+    assert g(1, 1 << 27, 1 << 27, 4096, 4096, 128) == 0
+    assert lib.lumen_attn_prompt(
+        rows(), rows(), rows(), 0, FAKE, FAKE, 1, 1 << 27, 1 << 27, 4096,
+        4096, 128, 0.1, FAKE, FAKE, 1 << 40, FAKE, None) < 0
+
+
 def test_binding_refuses_host_tensors_and_shapes():
     sh = attn.cache_shape4(1, 2, 128, 16)
     with pytest.raises(ValueError, match="head_dim 96"):
