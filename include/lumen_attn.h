@@ -144,8 +144,8 @@ size_t lumen_attn_decode4_workspace_bytes(const lumen_kv_layout *layout,
  * t < d_lens[r], G = num_q_heads / H (H must divide num_q_heads, at most
  * 65535).  q: rows
  * (r, h) of dtype; d_out [num_reqs][num_q_heads][D] of dtype, contiguous,
- * 16-byte aligned.  scale must be finite and above 0.  A request of length 0
- * gets zeros; a negative one too (RANGE).  Tokens in pages past bt_cols
+ * 16-byte aligned.  scale must be above 0 and scale * log2(e) finite.  A request
+ * of length 0 gets zeros; a negative one too (RANGE).  Tokens in pages past bt_cols
  * (RANGE) or with a block id outside [0, num_blocks) (BLOCK_ID) are left out
  * of the sum.  What the cache holds past a request's length does not matter,
  * NaN included.  The result does not depend on timing.  d_workspace:
@@ -175,8 +175,8 @@ size_t lumen_attn_prompt_workspace_bytes(int32_t num_seqs, int64_t num_q_tokens,
  * rows (j, h), h < num_kv_heads, which must divide num_q_heads; query head h
  * uses KV head h / (num_q_heads / num_kv_heads).  d_out
  * [num_q_tokens][num_q_heads][head_dim], contiguous, 16-byte aligned; rows of
- * tokens in no sequence are not written.  head_dim 64 or 128.  scale finite
- * and above 0.  A sequence whose bounds fall outside [0, num_q_tokens] or [0,
+ * tokens in no sequence are not written.  head_dim 64 or 128.  scale above 0,
+ * scale * log2(e) finite.  A sequence whose bounds fall outside [0, num_q_tokens] or [0,
  * num_k_tokens], or end before they begin, is skipped (RANGE).  Sequences must
  * not share queries.  Token counts at most LUMEN_ATTN_MAX_TOKENS; token strides
  * of k and v at most LUMEN_ATTN_MAX_STRIDE where they have more than one token.

@@ -403,7 +403,7 @@ struct DecodeArgs {
   int32_t num_reqs, heads, group;
   bool hnd, bf16;
   Rows q;
-  float scale_log2;  // scale * log2(e)
+  float scale_log2;
   uint16_t *out;
   int32_t *status;
   int32_t wg_heads, wg_blocks;  // heads and key blocks of a workgroup
@@ -1395,8 +1395,7 @@ int lumen_attn_decode4(const lumen_kv_layout *layout, int32_t layer,
   if (st != LUMEN_OK) return st;
   if ((st = check_dtype(dtype)) != LUMEN_OK) return st;
   if (num_reqs < 0 || bt_cols < 0 || num_q_heads < 1 ||
-      num_q_heads % layout->num_kv_heads || !(scale > 0.0f) ||
-      !(scale < INFINITY))
+      num_q_heads % layout->num_kv_heads || check_scale(scale) != LUMEN_OK)
     return LUMEN_ERR_INVALID_ARG;
   if (num_q_heads > 65535) return LUMEN_ERR_UNSUPPORTED;
   if ((st = check_status(d_status)) != LUMEN_OK) return st;
@@ -1434,7 +1433,7 @@ int lumen_attn_decode4(const lumen_kv_layout *layout, int32_t layer,
   a.group = num_q_heads / layout->num_kv_heads;
   a.hnd = layout->cache_order == LUMEN_CACHE_HND;
   a.q = rows_of(q, 0);
-  a.scale_log2 = scale * 1.44269504088896341f;
+  a.scale_log2 = scale_log2(scale);
   a.out = static_cast<uint16_t *>(d_out);
   a.status = d_status;
   a.wg_heads = plan.wg_heads;

@@ -5,6 +5,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include <math.h>
 #include <stdint.h>
 
 #include <atomic>
@@ -149,6 +150,12 @@ inline int check_rows(const lumen_attn_rows *r, int64_t tokens) {
   if (!aligned(r->d_base, 16) || r->token_stride % 8 || r->head_stride % 8)
     return LUMEN_ERR_MISALIGNED;
   return LUMEN_OK;
+}
+
+inline float scale_log2(float scale) { return scale * 1.44269504088896341f; }
+
+inline int check_scale(float scale) {
+  return scale > 0.0f && scale_log2(scale) < INFINITY ? LUMEN_OK : LUMEN_ERR_INVALID_ARG;
 }
 
 // The rows from token `first` on.

@@ -33,7 +33,7 @@ struct PromptArgs {
   int64_t num_q, num_k;
   int32_t q_heads, kv_heads;
   int32_t heads_per_tile, tile_tokens;
-  float scale_log2;  // scale * log2(e)
+  float scale_log2;
   uint16_t *out;
   int32_t *status;
   // the plan; units is NULL where the kernel finds its unit itself
@@ -852,8 +852,7 @@ int lumen_attn_prompt(const lumen_attn_rows *q, const lumen_attn_rows *k,
                       int32_t *d_status, lumen_stream_t stream) {
   int st = check_dtype(dtype);
   if (st != LUMEN_OK) return st;
-  if (!(scale > 0.0f) || !(scale < INFINITY) ||
-      (!d_cu_k && num_q_tokens != num_k_tokens))
+  if (check_scale(scale) != LUMEN_OK || (!d_cu_k && num_q_tokens != num_k_tokens))
     return LUMEN_ERR_INVALID_ARG;
   if ((st = check_prompt(num_seqs, num_q_tokens, num_k_tokens, num_q_heads,
                          num_kv_heads, head_dim)) != LUMEN_OK)
@@ -893,7 +892,7 @@ int lumen_attn_prompt(const lumen_attn_rows *q, const lumen_attn_rows *k,
   a.kv_heads = num_kv_heads;
   a.heads_per_tile = p.heads_per_tile;
   a.tile_tokens = p.tile_tokens;
-  a.scale_log2 = scale * 1.44269504088896341f;
+  a.scale_log2 = scale_log2(scale);
   a.out = static_cast<uint16_t *>(d_out);
   a.status = d_status;
   char *ws = static_cast<char *>(d_workspace);

@@ -243,3 +243,21 @@ def test_row_format_round_trip():
     lowest = q.reshape(50, 4, 32)[y == y.min(-1, keepdims=True)]
     assert (lowest == 0).all()
     assert (q.reshape(50, 4, 32)[y == y.max(-1, keepdims=True)] == 15).all()
+
+
+def test_scales_past_the_range_of_the_exponent(lib):
+    """A scale that times log2(e) is infinite makes every score infinite or
+    NaN: refused."""
+    def decode(scale):  # of no requests
+        return lib.lumen_attn_decode4(layout(), 0, FAKE, FAKE, 4, FAKE, 0,
+                                      rows(), 0, 8, scale, FAKE, FAKE, 0, FAKE,
+                                      None)
+
+    def prompt(scale):  # of no sequences
+        return lib.lumen_attn_prompt(rows(), rows(), rows(), 0, FAKE, FAKE, 0,
+                                     10, 10, 8, 2, 128, scale, FAKE, None, 0,
+                                     FAKE, None)
+    for call in (decode, prompt):
+        assert call(2e38) == kv.LUMEN_OK
+        for scale in (2.4e38, 3.4e38):
+            assert call(scale) == kv.LUMEN_ERR_INVALID_ARG
