@@ -6,6 +6,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include <float.h>
 #include <math.h>
 #include <stdint.h>
 
@@ -706,7 +707,12 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void decode4_kernel(DecodeArgs a
     uint32_t e = __builtin_bit_cast(uint32_t, big) >> 23;  // NaN: not the maximum
     e = e == 255 ? 140 : e < 14 ? 14 : e;
     const float up = __builtin_bit_cast(float, (267 - e) << 23);  // to 2^13..2^14
-    cq = a.scale_log2 * __builtin_bit_cast(float, (e - 13) << 23);
+    // Neither 0 (a masked key's -infinity times it would be NaN) nor infinite (a
+    // score of 0 would): a score is at most 2^38 times it, so where it is held up
+    // to 2^-126, for a row of zeros under a small scale, the scores stay below
+    // 2^-88.
+    cq = __builtin_amdgcn_fmed3f(a.scale_log2 * __builtin_bit_cast(float, (e - 13) << 23),
+                                 0x1p-126f, FLT_MAX);
     if constexpr (kTwice) asm volatile("" ::: "memory");
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {

@@ -1,0 +1,61 @@
+"""The serving operators at the ends of their inputs' ranges, against plain
+references: values and scales that 32 bits or 16 hold badly, rows that see
+only infinities, sizes past 2^31, streams and forms of a call."""
+import numpy as np
+import pytest
+import torch
+
+import attn_ref as ref
+from paper_2606_17787_amd import attn
+from gpu_util import dev
+from test_gpu_attn import (BF, FP, decode_case, decode_want, i32, prompt_want,
+                           word)
+
+pytestmark = pytest.mark.gpu
+
+
+def run_decode(sh, nb, cache, table, lens, q, scale=None):
+    out, status = torch.full_like(q, 7.0), word()
+    ws = attn.new_decode4_workspace(sh, lens.numel(), q.shape[1])
+    attn.lumen_attn_decode4(sh, nb, 0, cache, table, lens, q, out, ws, status,
+                            scale=scale)
+    assert int(status) == 0
+    return out
+
+
+def run_prompt(q, k, v, cu_q, cu_k=None, scale=None):
+    out, status = torch.full_like(q, 7.0), word()
+    attn.lumen_attn_prompt(q, k, v, out, i32(cu_q), status,
+                           cu_k=None if cu_k is None else i32(cu_k),
+                           scale=scale)
+    assert int(status) == 0
+    return out
+
+
+# ------------------------------------------- scales at the ends of the range
+
+@pytest.mark.parametrize("scale", [1e-45, 1e-9, 1.0, 2e38])
+@pytest.mark.parametrize("dtype", [BF, FP])
+def test_decode_of_zero_queries_is_the_mean(dtype, scale):
+    """A row of zeros has scores of 0 under any scale, masked keys beside the
+    seen ones in its last block or not."""
+    rng = np.random.default_rng(1)
+    sh, nb, cache, rows, table, lens, q = decode_case(
+        rng, [1, 31, 32, 45, 500], 2, 4, 128, 16, "NHD", dtype)
+    q[:, 1::2] = 0
+    q[:, ::2] *= min(1.0, 1 / scale)
+    want, slack = decode_want(rows(0), table, lens, q, 2, 16, scale, dtype)
+    ref.assert_close(run_decode(sh, nb, cache, table, lens, q, scale), want,
+                     slack, dtype)
+
+
+@pytest.mark.parametrize("scale", [1e-45, 1e-9, 2e38])
+@pytest.mark.parametrize("dtype", [BF, FP])
+def test_prompt_of_zero_queries_is_the_mean(dtype, scale):
+    g = torch.Generator(device=dev()).manual_seed(2)
+    q = torch.zeros(150, 4, 64, dtype=dtype, device=dev())
+    k, v = (torch.randn(150, 2, 64, generator=g, device=dev()).to(dtype)
+            for _ in range(2))
+    cu = [0, 1, 70, 150]
+    want, slack = prompt_want(q, k, v, cu, cu, scale, ref.UNIT[dtype])
+    ref.assert_close(run_prompt(q, k, v, cu, scale=scale), want, slack, dtype)
