@@ -67,9 +67,13 @@ constexpr int kKeys = 64;  // keys of a tile
 #define CONSTANT_PTR(T, p) ((const __attribute__((address_space(4))) T *)(p))
 
 constexpr float kSlack = 8.0f;
-// fp16 weights are taken times 2^kLift: up to 2^15 then, and a weight only
-// rounds to a subnormal or 0 when it is under 2^-21 or 2^-32 of the largest.
-constexpr float kLift = 7.0f;
+// Weights are taken times 2^lift.  bf16: at most 1, so that the sums overflow no
+// sooner than those of weights under the true maximum would (a mean of n values
+// under 3.4e38 / n never does).  fp16: up to 2^15, and where the maximum is not
+// behind, a weight only rounds to a subnormal or 0 when it is under 2^-21 or
+// 2^-32 of the largest.
+template <bool kBf16>
+constexpr float lift() { return kBf16 ? -kSlack : 7.0f; }
 constexpr int kMfma = 0x8, kDsRead = 0x100;  // of sched_group_barrier
 
 template <int D>
@@ -596,7 +600,7 @@ __device__ __forceinline__ bool prompt_tile(const PromptArgs &a, const int tid,
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[d][i] *= c;
     }
-    const float ms = m == -INFINITY ? 0.0f : m - (kBf16 ? 0.0f : kLift);
+    const float ms = m == -INFINITY ? 0.0f : m - lift<kBf16>();
     frag8 pr[4];
 #pragma unroll
     for (int t = 0; t < 2; ++t)

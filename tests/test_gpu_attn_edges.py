@@ -59,3 +59,32 @@ def test_prompt_of_zero_queries_is_the_mean(dtype, scale):
     cu = [0, 1, 70, 150]
     want, slack = prompt_want(q, k, v, cu, cu, scale, ref.UNIT[dtype])
     ref.assert_close(run_prompt(q, k, v, cu, scale=scale), want, slack, dtype)
+
+
+# ----------------------------------------------------------- large values
+
+@pytest.mark.parametrize("value", [2e36, -2e36])
+@pytest.mark.parametrize("H", [1, 64])
+def test_prompt_means_of_large_values_stay_finite(H, value):
+    """64 keys of score 0 and 64 whose weights are 2^7.9 of theirs, all of one
+    value: the sum of the weights under the true maximum times it is below
+    3.4e38.  (64 heads of 2,048 queries take the larger workgroups.)"""
+    n = 2048 if H == 64 else 1
+    q = torch.zeros(n, H, 64, dtype=BF, device=dev())
+    k = torch.zeros(128, 1, 64, dtype=BF, device=dev())
+    v = torch.full((128, 1, 64), value, dtype=BF, device=dev())
+    q[..., 0], k[64:, :, 0] = 1.0, 7.9 * 0.6931
+    # every query sees all keys: they are the ends of sequences of one query
+    out = torch.full_like(q, 7.0)
+    if n == 1:
+        out = run_prompt(q, k, v, [0, 1], [0, 128], scale=1.0)
+    else:
+        k = torch.cat([k, torch.full((n - 1, 1, 64), -9.0, dtype=BF,
+                                     device=dev())])
+        v = torch.cat([v, torch.zeros(n - 1, 1, 64, dtype=BF, device=dev())])
+        out = run_prompt(q, k, v, [0, n], [0, 127 + n], scale=1.0)
+    top = v[0, 0, 0].double()
+    # the later keys' weights are 2^-20 of the others', 2,047 of them
+    room = float(top.abs()) * (2 * ref.UNIT[BF] + 2.0 ** -9)
+    assert torch.isfinite(out).all()
+    assert float((out.double() - top).abs().max()) <= room
