@@ -147,7 +147,8 @@ size_t lumen_attn_decode4_workspace_bytes(const lumen_kv_layout *layout,
  * 16-byte aligned.  scale must be above 0 and scale * log2(e) finite.  A request
  * of length 0 gets zeros; a negative one too (RANGE).  Tokens in pages past bt_cols
  * (RANGE) or with a block id outside [0, num_blocks) (BLOCK_ID) are left out
- * of the sum.  What the cache holds past a request's length does not matter,
+ * of the sum; where all are, the row is zeros.  A row with a score of NaN or
+ * +infinity, or with none but -infinity, is NaN.  What the cache holds past a request's length does not matter,
  * NaN included.  The result does not depend on timing.  d_workspace:
  * lumen_attn_decode4_workspace_bytes bytes, 16-byte aligned, not shared by
  * calls in flight at the same time; what it holds does not matter. */

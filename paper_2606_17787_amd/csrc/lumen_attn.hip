@@ -477,6 +477,14 @@ __device__ __forceinline__ float quad_sum(float x) {
   return a + b;
 }
 
+// What a row's sums are multiplied by.  m is -infinity where no key counted, and
+// the row is zeros.  It is at least -FLT_MAX where one did: if the sum of the
+// weights is 0 then, every score was -infinity, and the row is NaN as the formula
+// has it.
+__device__ __forceinline__ float inverse(float m, float l) {
+  return m == -INFINITY ? 0.0f : 1.0f / l;
+}
+
 // What a wavefront's rows share: the workgroup's other heads' places and cache
 // lines that other workgroups read too; only the places; nothing.
 enum class Sharing { kLines, kStep, kNone };
@@ -809,15 +817,16 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void decode4_kernel(DecodeArgs a
 #pragma unroll
     for (int j = 0; j < 8; ++j) top = fmaxf(top, s[j / 4][j % 4]);
     top = quad_max(top) * cq;
+    m = fmaxf(m, -FLT_MAX);  // the block has a key that counts
     if (__any(top > m + kRise)) {
       const float mn = fmaxf(m, top);
-      const float c = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
+      const float c = __builtin_amdgcn_exp2f(m - mn);
       m = mn;
       l *= c;
 #pragma unroll
       for (int j = 0; j < kE; ++j) o[j] *= c;
     }
-    const float shift = kBias - (m == -INFINITY ? 0.0f : m);
+    const float shift = kBias - m;
     half8v p;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
@@ -947,7 +956,7 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void decode4_kernel(DecodeArgs a
       const int flags = read(seg_flags[part]), req = r + part;
       if (kbi == 0 && n < rows) {
         if (flags == 3) {  // the whole request
-          const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+          const float inv = inverse(m, l);
           uint16_t *out = a.out +
                           ((int64_t(req) * a.heads + h0 + hi) * a.group + g0 + n) * D +
                           4 * quad * kE;
@@ -1167,7 +1176,7 @@ __global__ __launch_bounds__(kJoinWaves *kWave) void decode4_join_kernel(DecodeA
       l += lds_l[w] * c;
       for (int e = 0; e < kE; ++e) o[e] += lds_o[w][lane * kE + e] * c;
     }
-    const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+    const float inv = inverse(m, l);
     for (int e = 0; e < kE; ++e)
       a.out[i * D + lane * kE + e] = rounded<kBf16>(o[e] * inv);
   }

@@ -88,3 +88,49 @@ def test_prompt_means_of_large_values_stay_finite(H, value):
     room = float(top.abs()) * (2 * ref.UNIT[BF] + 2.0 ** -9)
     assert torch.isfinite(out).all()
     assert float((out.double() - top).abs().max()) <= room
+
+
+# ------------------------------------------- scores that are not finite
+
+# Lengths of one key, of part of a block, of several workgroups' shares.
+@pytest.mark.parametrize("lens", [[1, 20, 33, 700, 0], [9000]])
+@pytest.mark.parametrize("H,order", [(2, "NHD"), (1, "NHD"), (2, "HND")])
+@pytest.mark.parametrize("dtype", [BF, FP])
+def test_decode_scores_that_are_not_finite(lens, H, order, dtype):
+    """Infinite and NaN queries: a row whose scores are all -infinity or that
+    has one of +infinity is NaN, as is one with a NaN; the rows beside it and
+    requests without keys are as ever."""
+    rng = np.random.default_rng(4)
+    D, G, bs = 128, 4, 16
+    sh, nb, cache, rows, table, dl, q = decode_case(rng, lens, H, G, D, bs,
+                                                    order, dtype)
+    # element 0 of every key is negative: its quarter's B is, by far
+    pairs = rows(0)[0][..., D // 2:D // 2 + 4].contiguous()
+    half = pairs.view(torch.float16)
+    half[..., 1] = -200.0
+    half[..., 0] = 0.5
+    stale = torch.zeros_like(half[..., 0], dtype=torch.bool)
+    for r, n in enumerate(lens):
+        if n % bs:
+            stale[table[r, n // bs].long(), n % bs:] = True
+    half[stale] = float("nan")
+    rows(0)[0][..., D // 2:D // 2 + 4] = half.view(torch.uint8)
+    zero = torch.zeros_like(q[:, 0])
+    first = zero.clone()
+    first[:, 0] = 1
+    heads = range(0, H * G, 4)
+    for h in heads:
+        q[:, h] = torch.where(first > 0, float("inf"), zero)       # all -inf
+        q[:, h + 1] = torch.where(first > 0, float("-inf"), zero)  # all +inf
+        q[:, h + 2, 5] = float("nan")
+    want, slack = decode_want(rows(0), table, dl, torch.nan_to_num(q), H, bs,
+                              D ** -0.5, dtype)
+    out = run_decode(sh, nb, cache, table, dl, q).double()
+    some = (dl > 0)[:, None, None]
+    bad = torch.zeros_like(want, dtype=torch.bool)
+    for h in heads:
+        bad[:, h:h + 3] = some
+    assert torch.equal(torch.isnan(out), bad)
+    z = torch.zeros_like(want)
+    ref.assert_close(torch.where(bad, z, out), torch.where(bad, z, want),
+                     torch.where(bad, z, slack), dtype)
