@@ -182,7 +182,8 @@ size_t lumen_attn_prompt_workspace_bytes(int32_t num_seqs, int64_t num_q_tokens,
  * not share queries.  Token counts at most LUMEN_ATTN_MAX_TOKENS; token strides
  * of k and v at most LUMEN_ATTN_MAX_STRIDE where they have more than one token.
  * What a query does not see does not reach its row, NaN and infinities
- * included; a NaN or infinity among the values it sees does.  d_workspace:
+ * included; a NaN or infinity among the values it sees does, and a row with a
+ * score of NaN or +infinity, or with none but -infinity, is NaN.  d_workspace:
  * lumen_attn_prompt_workspace_bytes bytes (NULL where that is 0), 16-byte aligned,
  * not shared by calls in flight at the same time; what it holds does not matter.
  * The result does not depend on timing. */

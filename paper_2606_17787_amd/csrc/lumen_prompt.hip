@@ -319,13 +319,16 @@ struct Row {
   int tok, nq;      // of the sequence
   int64_t q0;       // of the sequence's first query
   int hq, half;
+  bool sees;        // a key
 };
 
-// 32 elements of it from element 32 * d on.
+// 32 elements of it from element 32 * d on: zeros where it sees no key.  The sum
+// of the weights of one that does is 0 only if every score is -infinity: the row
+// is NaN then, as the formula has it.
 template <int D, bool kBf16>
 __device__ __forceinline__ void write_row(const PromptArgs &a, const Row &r, int d,
                                           const f32x16 &o, float l) {
-  const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+  const float inv = r.sees ? 1.0f / l : 0.0f;
   uint16_t *out = a.out + ((r.q0 + r.tok) * a.q_heads + r.hq) * D + d * 32;
 #pragma unroll
   for (int g = 0; g < 2; ++g) {
@@ -665,7 +668,7 @@ __device__ __forceinline__ bool prompt_tile(const PromptArgs &a, const int tid,
   } else if (here) {
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)
-      write_row<D, kBf16>(a, Row{tok, nq, q0, hq, half}, d, o[d], l);
+      write_row<D, kBf16>(a, Row{tok, nq, q0, hq, half, limit >= 0}, d, o[d], l);
   }
   return false;
 }
@@ -705,8 +708,8 @@ __global__ __launch_bounds__(kWaves *kWave, 2) void prompt_join_kernel(PromptArg
     const int d = item % (D / 32), hg = item / (D / 32) % groups;
     const Cut cut = a.cuts[item / (D / 32) / groups];
     const Unit u = a.units[cut.unit];
-    const Row r{u.t0 + wave / gp * 32 + (lane & 31), u.nq, u.q0, hg * gp + wave % gp,
-                lane >> 5};
+    const int tok = u.t0 + wave / gp * 32 + (lane & 31);
+    const Row r{tok, u.nq, u.q0, hg * gp + wave % gp, lane >> 5, tok + u.nk - u.nq >= 0};
     const int64_t apart = int64_t(groups) * part_floats(D, kWaves);
     const float *part = a.parts + (int64_t(u.place) * groups + hg) * part_floats(D, kWaves);
     const float *ms = part + kThreads * (D / 2) + tid, *ls = ms + kThreads;

@@ -134,3 +134,65 @@ def test_decode_scores_that_are_not_finite(lens, H, order, dtype):
     z = torch.zeros_like(want)
     ref.assert_close(torch.where(bad, z, out), torch.where(bad, z, want),
                      torch.where(bad, z, slack), dtype)
+
+
+def formula(q, k, v, scale, seen, dtype):
+    """(out, slack) of one head in 64 bits, with no special case for rows whose
+    scores are all -infinity; zeros for rows that see no key.  slack is that of
+    the finite rows, whose keys of score -infinity have no weight."""
+    s = (torch.matmul(q, k.transpose(0, 1).contiguous()) * scale)
+    s = s.masked_fill(~seen, float("-inf"))
+    p = torch.exp(s - s.amax(-1, keepdim=True))
+    out = torch.matmul(p / p.sum(-1, keepdim=True), v)
+    out[~seen.any(-1)] = 0.0
+    weighed = seen & torch.isfinite(s)
+    _, slack = ref.attend(torch.nan_to_num(q, 0.0, 0.0, 0.0),
+                          torch.nan_to_num(k, 0.0, 0.0, 0.0), v, scale,
+                          weighed, ref.UNIT[dtype])
+    return out, slack
+
+
+@pytest.mark.parametrize("nq,nk,H,G,D", [
+    ([70, 130], [70, 130], 2, 2, 64), ([33, 5], [150, 3], 1, 4, 128),
+    ([40, 3], [6000, 70], 1, 8, 128), ([2100], [2100], 8, 8, 64)])
+@pytest.mark.parametrize("dtype", [BF, FP])
+def test_prompt_scores_that_are_not_finite(nq, nk, H, G, D, dtype):
+    """Infinities and NaN in keys and queries: rows that see a score of NaN or
+    +infinity, or none but -infinity, are NaN; a score of -infinity among
+    others has no weight; rows that see no such key are as ever."""
+    g = torch.Generator(device=dev()).manual_seed(sum(nk))
+    q = torch.randn(sum(nq), H * G, D, generator=g, device=dev())
+    k, v = (torch.randn(sum(nk), H, D, generator=g, device=dev()).to(dtype)
+            for _ in range(2))
+    cu_q, cu_k = np.cumsum([0] + nq), np.cumsum([0] + nk)
+    q[..., 1] = q[..., 1].abs() + 0.5
+    q[::3, :, 1] *= -1  # an infinite element of a key is +infinity for others
+    q = q.to(dtype)
+    for s, n in enumerate(nk):
+        first = max(0, n - nq[s])  # the last key of the first query
+        k[cu_k[s], 0, 1] = float("-inf")        # every query sees it
+        if n > 9:
+            k[cu_k[s] + n // 2 + 1, 0, 1] = float("-inf")
+            k[cu_k[s + 1] - 2, 0, 1] = float("inf")   # the last two queries
+            k[cu_k[s + 1] - 1, 0, 7] = float("nan")   # the last one
+        q[cu_q[s + 1] - 3, G - 1, 9] = float("nan")
+        q[cu_q[s], :, 2] = float("inf")
+        k[cu_k[s]:cu_k[s] + first + 1, :, 2] = -1.0   # all of its scores
+    out = run_prompt(q, k, v, cu_q, cu_k).double()
+    nans = 0
+    for s in range(len(nq)):
+        a, b, e, f = cu_q[s], cu_q[s + 1], cu_k[s], cu_k[s + 1]
+        i = torch.arange(b - a, device=dev())[:, None] + (f - e) - (b - a)
+        seen = torch.arange(f - e, device=dev())[None] <= i
+        for h in range(H * G):
+            want, slack = formula(q[a:b, h].double(), k[e:f, h // G].double(),
+                                  v[e:f, h // G].double(), D ** -0.5, seen,
+                                  dtype)
+            bad = torch.isnan(want)
+            nans += int(bad.any(-1).sum())
+            z = torch.zeros_like(want)
+            assert torch.equal(torch.isnan(out[a:b, h]), bad), (s, h)
+            ref.assert_close(torch.where(bad, z, out[a:b, h]),
+                             torch.where(bad, z, want),
+                             torch.where(bad, z, slack), dtype, f"{s} {h}")
+    assert 0 < nans < sum(nq) * H * G
