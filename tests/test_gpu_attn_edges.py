@@ -196,3 +196,35 @@ def test_prompt_scores_that_are_not_finite(nq, nk, H, G, D, dtype):
                              torch.where(bad, z, want),
                              torch.where(bad, z, slack), dtype, f"{s} {h}")
     assert 0 < nans < sum(nq) * H * G
+
+
+# -------------------------------------------------- every pair that a row holds
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_read_rounds_a_value_once(D):
+    """Pairs of any size, whose value may need more bits than 32-bit arithmetic
+    holds: rounded to 16 bits once.  1986 * 2^-17 * 66 + 4000 is 2^-15 above the
+    middle of two 16-bit values."""
+    rng = np.random.default_rng(6)
+    H, bs, nb = 2, 16, 64
+    T = nb * bs
+    codes = rng.integers(0, 16, (2, T, H, D)).astype(np.uint8)
+    A = (rng.uniform(0.5, 1, (2, T, H, 4)) *
+         2.0 ** rng.integers(-20, 8, (2, T, H, 4))).astype(np.float16)
+    B = (rng.uniform(-1, 1, (2, T, H, 4)) *
+         2.0 ** rng.integers(-10, 13, (2, T, H, 4))).astype(np.float16)
+    A[:, 0], B[:, 0], codes[:, 0, :, ::3] = 1986 * 2.0 ** -17, 4000.0, 2
+    A[:, 1], B[:, 1] = 0.0, 5.0
+    A[:, 2], B[:, 2] = 2.0 ** -24, 2.0 ** -24  # subnormal
+    sh = attn.cache_shape4(1, H, D, bs)
+    cache = torch.from_numpy(ref.to_rows(codes, A, B)).to(dev()).reshape(-1)
+    want = ref.values(codes, A, B)
+    assert want[0, 0, 0, 0] == 4002.0
+    slots, status = torch.arange(T, device=dev()), word()
+    for dtype in (FP, BF):
+        k, v = (torch.empty(T, H, D, dtype=dtype, device=dev())
+                for _ in range(2))
+        attn.lumen_attn_read4(sh, nb, 0, cache, slots, k, v, status)
+        assert int(status) == 0
+        for got, w in ((k, want[0]), (v, want[1])):
+            assert torch.equal(got.cpu(), torch.from_numpy(w).to(dtype))
