@@ -363,16 +363,21 @@ struct PromptShape {
   static constexpr int kStages = kWaves == 8 ? 4 : 2;
 };
 
-// Infinities and NaN of a tile in LDS become 0.
-template <bool kBf16, int kElems, int kThreads>
-__device__ __forceinline__ void clear_nonfinite(uint16_t *tile, int tid) {
+// Infinities and NaN of a tile in LDS become 0; the rows that had some are set in
+// `rows`, a bit each.
+template <int D, bool kBf16, int kThreads>
+__device__ __forceinline__ void clear_nonfinite(uint16_t *tile, uint32_t *rows, int tid) {
   uint32_t *w = reinterpret_cast<uint32_t *>(tile);
 #pragma unroll 1
-  for (int i = tid; i < kElems / 2; i += kThreads) {
+  for (int i = tid; i < kKeys * D / 2; i += kThreads) {
     const uint32_t x = w[i];
     const uint32_t keep = (not_finite16<kBf16>(x) ? 0u : 0xffffu) |
                           (not_finite16<kBf16>(x >> 16) ? 0u : 0xffff0000u);
-    if (keep != 0xffffffffu) w[i] = x & keep;
+    if (keep != 0xffffffffu) {
+      w[i] = x & keep;
+      const int row = i / (D / 2);
+      atomicOr(&rows[row / 32], 1u << (row % 32));
+    }
   }
 }
 
@@ -418,10 +423,14 @@ __device__ __forceinline__ void add_nonfinite(const uint16_t *row, bool seen, f3
 // them in the products, which keeps it out unless it is an infinity or NaN.
 // Where a sum comes out as one, nothing is written and the call returns true:
 // the tile is then done again with kApart, where such values are taken out of
-// the products and added to the queries that see them.
+// the products and the rows that had some, found on the way, are added to the
+// queries that see them.  A prompt of 16,384 tokens (32 query heads over 8, D 128)
+// takes 4.6 ms instead of 2.1 with a NaN in an early value, and 43 with an
+// infinity in every second one.
 template <int D, bool kBf16, int kWaves, bool kApart>
 __device__ __forceinline__ bool prompt_tile(const PromptArgs &a, const int tid,
-                                            uint16_t *lds, bool *not_finite) {
+                                            uint16_t *lds, bool *not_finite,
+                                            uint32_t (*bad_rows)[2]) {
   using S = PromptShape<D, kWaves>;
   constexpr int kThreads = S::kThreads, kChunks = S::kChunks, kTile = S::kTile;
   constexpr int kStages = S::kStages, kStageBytes = 2 * kTile * 2;
@@ -524,6 +533,8 @@ __device__ __forceinline__ bool prompt_tile(const PromptArgs &a, const int tid,
     for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
   float m = -INFINITY, l = 0.0f;
 
+  if constexpr (kApart)  // of this step and the next, in turn
+    if (tid < 4) bad_rows[tid / 2][tid % 2] = 0;
 #pragma unroll
   for (int i = 0; i < kStages - 1; ++i)
     if (first_step + i < steps) load(first_step + i, i);
@@ -539,8 +550,10 @@ __device__ __forceinline__ bool prompt_tile(const PromptArgs &a, const int tid,
     lds_barrier();
     const int now = buf;
     if constexpr (kApart) {
-      clear_nonfinite<kBf16, kTile, kThreads>(lds + now * 2 * kTile + kTile, tid);
+      clear_nonfinite<D, kBf16, kThreads>(lds + now * 2 * kTile + kTile,
+                                          bad_rows[step & 1], tid);
       lds_barrier();
+      if (tid < 2) bad_rows[~step & 1][tid] = 0;
     }
     buf = buf + 1 < kStages ? buf + 1 : 0;
     if (step + kStages - 1 < steps)
@@ -631,11 +644,14 @@ __device__ __forceinline__ bool prompt_tile(const PromptArgs &a, const int tid,
         o[d] = mfma<kBf16>(v, pr[ks], o[d]);
       }
     if constexpr (kApart) {
-      const int end = step * kKeys + kKeys < nk ? step * kKeys + kKeys : nk;
+      uint64_t rows = uniform(uint64_t(bad_rows[step & 1][1]) << 32 | bad_rows[step & 1][0]);
 #pragma unroll 1
-      for (int key = step * kKeys; key < end; ++key)
+      for (; rows; rows &= rows - 1) {
+        const int key = step * kKeys + __builtin_ctzll(rows);
+        if (key >= nk) break;  // a copy of the last key
         add_nonfinite<D, kBf16>(vb + int64_t(key) * a.v.token + 4 * half,
                                 key <= limit, o);
+      }
     }
   }
   if constexpr (!kApart) {
@@ -678,7 +694,8 @@ __global__ __launch_bounds__(kWaves *kWave, 2) void prompt_kernel(PromptArgs a) 
   using S = PromptShape<D, kWaves>;
   __shared__ __attribute__((aligned(1024))) uint16_t lds[S::kStages * 2 * S::kTile];
   __shared__ bool not_finite[kWaves];
-  if (!prompt_tile<D, kBf16, kWaves, false>(a, threadIdx.x, lds, not_finite)) return;
+  __shared__ uint32_t bad_rows[2][kKeys / 32];
+  if (!prompt_tile<D, kBf16, kWaves, false>(a, threadIdx.x, lds, not_finite, bad_rows)) return;
   // from the arguments on, so that nothing is kept for this in the first loop
   auto *args = __builtin_amdgcn_kernarg_segment_ptr();
   int tid = threadIdx.x;
@@ -691,7 +708,7 @@ __global__ __launch_bounds__(kWaves *kWave, 2) void prompt_kernel(PromptArgs a) 
   PromptArgs again;
   static_assert(sizeof(words) == sizeof(again));
   __builtin_memcpy(&again, words, sizeof(again));
-  prompt_tile<D, kBf16, kWaves, true>(again, tid, lds, not_finite);
+  prompt_tile<D, kBf16, kWaves, true>(again, tid, lds, not_finite, bad_rows);
 }
 
 // Puts the parts of cut tiles together, in their order: a workgroup for 32

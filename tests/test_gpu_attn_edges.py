@@ -228,3 +228,36 @@ def test_read_rounds_a_value_once(D):
         assert int(status) == 0
         for got, w in ((k, want[0]), (v, want[1])):
             assert torch.equal(got.cpu(), torch.from_numpy(w).to(dtype))
+
+
+# ------------------------------------------------------- what a NaN costs
+
+def test_one_nan_does_not_slow_a_prompt_down_many_times():
+    """A NaN in an early value, key or a query makes the tiles that see it run
+    once more, with a look at each value: about two passes more, of which 8 are
+    allowed for."""
+    n, H, G, D = 8192, 2, 8, 128
+    g = torch.Generator(device=dev()).manual_seed(1)
+    q, k, v = (torch.randn(n, h, D, generator=g, device=dev()).to(BF)
+               for h in (H * G, H, H))
+    out, status = torch.empty_like(q), word()
+    call = attn.prepare_prompt(q, k, v, out, i32([0, n]), status)
+
+    def time():
+        call()
+        at = [torch.cuda.Event(enable_timing=True) for _ in range(6)]
+        for e in at:
+            e.record()
+            call()
+        torch.cuda.synchronize()
+        return min(a.elapsed_time(b) for a, b in zip(at, at[1:]))
+
+    clean = time()
+    for t, row in ((v, 5), (k, 5), (q, n - 7)):
+        was = t[row].clone()
+        t[row, :, 9] = float("nan")
+        assert time() < 8 * clean
+        assert torch.isnan(out).any() and torch.isfinite(out).any()
+        t[row] = was
+    call()
+    assert torch.isfinite(out).all() and int(status) == 0
