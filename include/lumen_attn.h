@@ -180,7 +180,9 @@ size_t lumen_attn_prompt_workspace_bytes(int32_t num_seqs, int64_t num_q_tokens,
  * scale * log2(e) finite.  A sequence whose bounds fall outside [0, num_q_tokens] or [0,
  * num_k_tokens], or end before they begin, is skipped (RANGE).  Sequences must
  * not share queries.  Token counts at most LUMEN_ATTN_MAX_TOKENS; token strides
- * of k and v at most LUMEN_ATTN_MAX_STRIDE where they have more than one token.
+ * of k and v at most LUMEN_ATTN_MAX_STRIDE where they have more than one token;
+ * sizes that would need a launch of 2^32 threads or more are refused
+ * (UNSUPPORTED).
  * What a query does not see does not reach its row, NaN and infinities
  * included; a NaN or infinity among the values it sees does, and a row with a
  * score of NaN or +infinity, or with none but -infinity, is NaN.  d_workspace:

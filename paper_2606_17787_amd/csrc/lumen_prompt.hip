@@ -824,9 +824,9 @@ PromptPlan prompt_plan(int32_t num_seqs, int64_t num_q, int64_t num_k,
   return p;
 }
 
-// A grid of more workgroups than a launch takes.
-bool too_many_groups(const PromptPlan &p) {
-  return (p.tiles + p.parts) * p.groups > INT32_MAX;
+// A grid of more threads than a launch takes.
+bool too_many_threads(const PromptPlan &p) {
+  return (p.tiles + p.parts) * p.groups * p.waves * kWave > int64_t(UINT32_MAX);
 }
 
 struct PromptKernels {
@@ -863,7 +863,7 @@ size_t lumen_attn_prompt_workspace_bytes(int32_t num_seqs, int64_t num_q_tokens,
     return 0;
   const PromptPlan p = prompt_plan(num_seqs, num_q_tokens, num_k_tokens, num_q_heads,
                                    num_kv_heads, head_dim, kMaxUnits);
-  return too_many_groups(p) ? 0 : p.bytes;
+  return too_many_threads(p) ? 0 : p.bytes;
 }
 
 int lumen_attn_prompt(const lumen_attn_rows *q, const lumen_attn_rows *k,
@@ -895,11 +895,13 @@ int lumen_attn_prompt(const lumen_attn_rows *q, const lumen_attn_rows *k,
       !aligned(d_cu_k, 4))
     return LUMEN_ERR_MISALIGNED;
   if (num_seqs == 0) return LUMEN_OK;
+  if (too_many_threads(prompt_plan(num_seqs, num_q_tokens, num_k_tokens, num_q_heads,
+                                   num_kv_heads, head_dim, kMaxUnits)))
+    return LUMEN_ERR_UNSUPPORTED;
   int cus = 0;
   if ((st = compute_units(&cus)) != LUMEN_OK) return st;
   const PromptPlan p = prompt_plan(num_seqs, num_q_tokens, num_k_tokens, num_q_heads,
                                    num_kv_heads, head_dim, cus);
-  if (too_many_groups(p)) return LUMEN_ERR_UNSUPPORTED;
   if (p.planned && (!d_workspace || workspace_bytes < p.bytes))
     return LUMEN_ERR_INVALID_ARG;
   (void)hipGetLastError();

@@ -261,3 +261,19 @@ def test_scales_past_the_range_of_the_exponent(lib):
         assert call(2e38) == kv.LUMEN_OK
         for scale in (2.4e38, 3.4e38):
             assert call(scale) == kv.LUMEN_ERR_INVALID_ARG
+
+
+def test_prompt_refuses_more_threads_than_a_launch_takes(lib):
+    """Heads so many that a few sequences need 2^32 threads: refused before
+    anything is enqueued, and without a workspace."""
+    g = lib.lumen_attn_prompt_workspace_bytes
+
+    def call(heads):
+        return lib.lumen_attn_prompt(
+            rows(), rows(), rows(), 0, FAKE, FAKE, 3, 3, 3, heads, heads, 64,
+            0.1, FAKE, FAKE, 1 << 40, FAKE, None)
+    # three tiles of 256 threads a head
+    assert g(3, 3, 3, 5592405, 5592405, 64) > 0
+    for heads in (5592406, 1 << 25, (1 << 31) - 1):
+        assert g(3, 3, 3, heads, heads, 64) == 0
+        assert call(heads) == kv.LUMEN_ERR_UNSUPPORTED
