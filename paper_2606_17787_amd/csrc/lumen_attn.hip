@@ -127,7 +127,8 @@ __global__ __launch_bounds__(kSlotThreads) void slots_kernel(SlotArgs a) {
   int64_t count64 = *a.free_count;
   if (count64 > a.free_cap) count64 = a.free_cap;
   if (count64 < 0) count64 = 0;
-  const uint32_t count = count64 < kHeld ? uint32_t(count64) : kHeld;
+  // pages that can be granted: below kHeld, so that a held sum never is
+  const uint32_t count = count64 < kHeld ? uint32_t(count64) : kHeld - 1;
   const bool first_wg = blockIdx.x == 0;
   uint32_t mine = 0;
   for (int r = r0; r < r1; ++r) {
@@ -201,7 +202,7 @@ __global__ __launch_bounds__(kSlotThreads) void slots_kernel(SlotArgs a) {
           if (!q.range && (q.need == 0 || add_held(b, q.need) <= count)) {
             // where nothing is new, every page is in the table
             id = q.need && page >= q.first
-                     ? a.free_ids[count - 1 - b - uint32_t(page - q.first)]
+                     ? a.free_ids[count64 - 1 - b - (page - q.first)]
                      : a.bt[int64_t(r) * a.bt_cols + page];
             if (id < 0 || id >= a.num_blocks) {
               id = -1;
@@ -226,7 +227,7 @@ __global__ __launch_bounds__(kSlotThreads) void slots_kernel(SlotArgs a) {
         hi = mid - 1;
     }
     const SlotReq q = slot_req(a, lo);
-    const int32_t id = a.free_ids[count - 1 - u];
+    const int32_t id = a.free_ids[count64 - 1 - u];
     if (id >= 0 && id < a.num_blocks)
       a.bt[int64_t(lo) * a.bt_cols + q.first + int32_t(u - base[lo])] = id;
     else

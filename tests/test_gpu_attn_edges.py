@@ -261,3 +261,22 @@ def test_one_nan_does_not_slow_a_prompt_down_many_times():
         t[row] = was
     call()
     assert torch.isfinite(out).all() and int(status) == 0
+
+
+# ------------------------------------------------------------ sizes past 2^31
+
+def test_slots_from_a_free_list_of_more_than_2_to_the_31_places():
+    """Pages come from the list's end, wherever that is."""
+    n = (1 << 31) + 5
+    free = torch.zeros(n, dtype=torch.int32, device=dev())
+    free[-6:] = i32([11, 12, 13, 14, 15, 16])
+    count, left = (torch.tensor([n], device=dev()) for _ in range(2))
+    table, status = i32(np.full((2, 4), -1)), word()
+    slots = torch.empty(50, dtype=torch.int64, device=dev())
+    cu, lens = i32(np.zeros(3)), i32(np.zeros(2))
+    attn.lumen_attn_slots(i32([0, 0]), i32([20, 30]), table, 16, 20, free,
+                          count, slots, cu, lens, left, status)
+    assert int(status) == 0 and int(left) == n - 4
+    assert table.tolist() == [[16, 15, -1, -1], [14, 13, -1, -1]]
+    assert slots[[0, 16, 20, 36]].tolist() == [256, 240, 224, 208]
+    assert lens.tolist() == [20, 30]
