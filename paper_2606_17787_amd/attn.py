@@ -391,13 +391,34 @@ def lumen_attn_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
           stream)
 
 
+class _OwnWorkspaceCall(_kv.PreparedCall):
+    """A prepared call with a workspace that no one else holds: a stream it
+    runs on is recorded, so that the memory is not given away while that
+    stream still uses it, whenever the object goes."""
+    __slots__ = ("_workspace", "_home")
+
+    def __init__(self, name: str, args: tuple, keep: tuple, workspace):
+        _lib()
+        super().__init__(name, args, (args, keep))
+        self._workspace = workspace
+        self._home = _kv._stream_handle(None)  # the allocation's
+
+    def __call__(self, stream: Optional[torch.cuda.Stream] = None) -> None:
+        super().__call__(stream)
+        if _kv._stream_handle(stream) != self._home:
+            self._workspace.record_stream(stream or
+                                          torch.cuda.current_stream())
+
+
 def prepare_prompt(q, k, v, out, cu_q, status, cu_k=None, scale=None,
                    workspace=None) -> "_kv.PreparedCall":
     """lumen_attn_prompt with its arguments checked once; workspace None: one
-    is allocated and kept, so the object must not be in flight twice at a
-    time."""
+    is allocated and kept, on the current stream, so the object must not be in
+    flight twice at a time, and a graph that holds its calls needs it alive."""
+    own = workspace is None
     workspace = _own_workspace(q, k, cu_q, workspace)
-    return _prepared("lumen_attn_prompt",
-                     _prompt_args(q, k, v, out, cu_q, status, cu_k, scale,
-                                  workspace),
-                     (q, k, v, out, cu_q, status, cu_k, workspace))
+    args = _prompt_args(q, k, v, out, cu_q, status, cu_k, scale, workspace)
+    keep = (q, k, v, out, cu_q, status, cu_k, workspace)
+    if own and workspace is not None:
+        return _OwnWorkspaceCall("lumen_attn_prompt", args, keep, workspace)
+    return _prepared("lumen_attn_prompt", args, keep)

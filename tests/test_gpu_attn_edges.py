@@ -280,3 +280,32 @@ def test_slots_from_a_free_list_of_more_than_2_to_the_31_places():
     assert table.tolist() == [[16, 15, -1, -1], [14, 13, -1, -1]]
     assert slots[[0, 16, 20, 36]].tolist() == [256, 240, 224, 208]
     assert lens.tolist() == [20, 30]
+
+
+# ------------------------------------------------------------------- streams
+
+def test_a_prepared_prompts_own_workspace_outlives_its_last_call():
+    """The object may go while another stream still runs its call: its
+    workspace is not given away before that has ended."""
+    g = torch.Generator(device=dev()).manual_seed(8)
+    q, k, v = (torch.randn(3000, h, 64, generator=g, device=dev()).to(BF)
+               for h in (4, 2, 2))
+    out, status, cu = torch.empty_like(q), word(), i32([0, 3000])
+    call = attn.prepare_prompt(q, k, v, out, cu, status)
+    workspace = call._keep[1][-1]
+    at, n = workspace.data_ptr(), workspace.numel()
+    assert n > 0
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(100_000_000)
+    call(side)
+    del workspace, call
+    others = [torch.empty(n, dtype=torch.uint8, device=dev()) for _ in range(3)]
+    still = not side.query()
+    assert at not in [t.data_ptr() for t in others] and still
+    side.synchronize()
+    want, slack = prompt_want(q, k, v, [0, 3000], [0, 3000], 0.125,
+                              ref.UNIT[BF])
+    assert int(status) == 0
+    ref.assert_close(out, want, slack, BF)
