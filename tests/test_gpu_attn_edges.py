@@ -309,3 +309,320 @@ def test_a_prepared_prompts_own_workspace_outlives_its_last_call():
                               ref.UNIT[BF])
     assert int(status) == 0
     ref.assert_close(out, want, slack, BF)
+
+
+class Step:
+    """One call of each operator: inputs, outputs and a twin of each output."""
+
+    def __init__(self, seed):
+        rng = np.random.default_rng(seed)
+        self.H, self.G, self.D, self.bs, self.R = 2, 4, 128, 16, 5
+        lens = [40, 700, 1, 5000, 33]
+        (self.sh, self.nb, self.cache, self.rows, self.table, self.lens,
+         self.q) = decode_case(rng, lens, self.H, self.G, self.D, self.bs,
+                               "NHD", BF)
+        self.start, self.end = self.lens, self.lens + 3
+        self.new_table = torch.nn.functional.pad(self.table, (0, 2), value=-1)
+        g = torch.Generator(device=dev()).manual_seed(seed)
+        self.k, self.v = (torch.randn(3 * self.R, self.H, self.D, generator=g,
+                                      device=dev()).to(BF) for _ in range(2))
+        self.free = torch.arange(self.nb, self.nb + 20, dtype=torch.int32,
+                                 device=dev())
+        self.big_nb = self.nb + 20
+        self.big = torch.zeros(self.sh.pool_elems(self.big_nb),
+                               dtype=torch.uint8, device=dev())
+        self.count = torch.tensor([20], device=dev())
+        self.ws = attn.new_decode4_workspace(self.sh, self.R, self.H * self.G)
+        # 3,000 queries behind 6,000 keys: planned and cut
+        self.pq = torch.randn(3000, 8, 128, generator=g, device=dev()).to(BF)
+        self.pk, self.pv = (torch.randn(6000, 2, 128, generator=g,
+                                        device=dev()).to(BF) for _ in range(2))
+        self.cu_q, self.cu_k = i32([0, 2990, 3000]), i32([0, 2990, 6000])
+        self.pws = attn.new_prompt_workspace(self.pq, self.pk, 2)
+        assert self.pws is not None
+
+    def outputs(self):
+        return dict(
+            table=self.new_table.clone(), cache=self.big.clone(),
+            slots=torch.full((15,), -9, dtype=torch.int64, device=dev()),
+            cu=i32(np.zeros(self.R + 1)), lens=i32(np.zeros(self.R)),
+            left=torch.zeros(1, dtype=torch.int64, device=dev()),
+            k=torch.zeros_like(self.k), v=torch.zeros_like(self.v),
+            out=torch.full_like(self.q, 7.0),
+            prompt=torch.full_like(self.pq, 7.0), status=word())
+
+    def arguments(self, o, workspace=True):
+        """(name, arguments, keywords) of the calls, in their order."""
+        st = o["status"]
+        return [
+            ("slots", (self.start, self.end, o["table"], self.bs, self.big_nb,
+                       self.free, self.count, o["slots"], o["cu"], o["lens"],
+                       o["left"], st), {}),
+            ("append4", (self.sh, self.big_nb, 0, o["cache"], self.k, self.v,
+                         o["slots"], st), {}),
+            ("read4", (self.sh, self.big_nb, 0, o["cache"], o["slots"], o["k"],
+                       o["v"], st), {}),
+            ("decode4", (self.sh, self.nb, 0, self.cache, self.table,
+                         self.lens, self.q, o["out"], self.ws, st), {}),
+            ("prompt", (self.pq, self.pk, self.pv, o["prompt"], self.cu_q, st),
+             dict(cu_k=self.cu_k, workspace=self.pws if workspace else None)),
+        ]
+
+    def call(self, o, **kw):
+        for name, args, more in self.arguments(o):
+            getattr(attn, "lumen_attn_" + name)(*args, **more, **kw)
+
+    def check(self, o):
+        torch.cuda.synchronize()
+        assert int(o["status"]) == 0
+        want, slack = decode_want(self.rows(0), self.table, self.lens, self.q,
+                                  self.H, self.bs, self.D ** -0.5, BF)
+        ref.assert_close(o["out"], want, slack, BF, "decode")
+        want, slack = prompt_want(self.pq, self.pk, self.pv,
+                                  self.cu_q.tolist(), self.cu_k.tolist(),
+                                  128 ** -0.5, ref.UNIT[BF])
+        ref.assert_close(o["prompt"], want, slack, BF, "prompt")
+        got = ref.slots(self.start.cpu().numpy(), self.end.cpu().numpy(),
+                        self.new_table.cpu().numpy(), self.bs, self.big_nb,
+                        self.free.cpu().numpy(), 20, 15)
+        for name, g in zip(("table", "slots", "cu", "lens"), got):
+            assert np.array_equal(o[name].cpu().numpy(), g), name
+        for name, x in (("k", self.k), ("v", self.v)):
+            val = ref.values(*ref.quantise(x.float().cpu().numpy()))
+            assert torch.equal(o[name].cpu(), torch.from_numpy(val).to(BF))
+
+
+def same(a, b):
+    for name in a:
+        assert torch.equal(a[name], b[name]), name
+
+
+def test_calls_take_a_stream():
+    """stream= runs a call there, in its order, and gives the current stream's
+    results; so does a current stream that is not the default one."""
+    s = Step(41)
+    here = s.outputs()
+    s.call(here)
+    s.check(here)
+    side = torch.cuda.Stream()
+    for inside in (False, True):
+        o = s.outputs()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(100_000_000)
+        if inside:
+            with torch.cuda.stream(side):
+                s.call(o)
+        else:
+            s.call(o, stream=side)
+        assert not side.query()  # nothing ran elsewhere, ahead of it
+        early = bool((o["out"][3] == 7.0).all())
+        side.synchronize()
+        assert early
+        same(o, here)
+
+
+def test_a_prompt_on_a_stream_of_its_own_and_a_workspace_of_the_calls():
+    s = Step(42)
+    here = s.outputs()
+    s.call(here)
+    side = torch.cuda.Stream()
+    o = s.outputs()
+    side.wait_stream(torch.cuda.current_stream())
+    for _ in range(3):
+        attn.lumen_attn_prompt(s.pq, s.pk, s.pv, o["prompt"], s.cu_q,
+                               o["status"], cu_k=s.cu_k, stream=side)
+    side.synchronize()
+    assert int(o["status"]) == 0
+    assert torch.equal(o["prompt"], here["prompt"])
+
+
+@pytest.mark.parametrize("workspace", [True, False])
+def test_prepared_calls_are_the_calls(workspace):
+    s = Step(43)
+    here, o = s.outputs(), s.outputs()
+    s.call(here)
+    calls = [getattr(attn, "prepare_" + name)(*args, **kw)
+             for name, args, kw in s.arguments(o, workspace)]
+    for c in calls:
+        c()
+    torch.cuda.synchronize()
+    s.check(o)
+    same(o, here)
+    # again, on another stream, over other outputs
+    side = torch.cuda.Stream()
+    for name, x in s.outputs().items():
+        o[name].copy_(x)
+    side.wait_stream(torch.cuda.current_stream())
+    for c in calls:
+        c(side)
+    side.synchronize()
+    same(o, here)
+
+
+@pytest.mark.parametrize("workspace", [True, False])
+def test_a_planned_prompt_in_a_graph(workspace):
+    """Plan, cut tiles and join, replayed between eager work that changes the
+    inputs, each replay against the eager result."""
+    s = Step(44)
+    o = s.outputs()
+    ws = s.pws if workspace else None
+
+    def one(out):
+        attn.lumen_attn_prompt(s.pq, s.pk, s.pv, out, s.cu_q, o["status"],
+                               cu_k=s.cu_k, workspace=ws)
+    one(o["prompt"])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        one(o["prompt"])
+    bounds = [([0, 2990, 3000], [0, 2990, 6000]),
+              ([0, 1, 3000], [0, 3000, 6000]), ([0, 1500, 1500], [0, 10, 10]),
+              ([0, 2990, 3000], [0, 2990, 6000])]
+    for cu_q, cu_k in bounds:
+        for t in (s.pq, s.pk, s.pv):
+            t.copy_(torch.randn(t.shape, device=dev()))
+        s.cu_q.copy_(i32(cu_q))
+        s.cu_k.copy_(i32(cu_k))
+        eager = torch.full_like(s.pq, 7.0)
+        one(eager)
+        o["prompt"].fill_(7.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(o["prompt"], eager)
+        n = cu_q[-1]
+        want, slack = prompt_want(s.pq[:n], s.pk, s.pv, cu_q, cu_k,
+                                  128 ** -0.5, ref.UNIT[BF])
+        ref.assert_close(eager[:n], want, slack, BF)
+        assert bool((eager[n:] == 7.0).all()) and int(o["status"]) == 0
+
+
+# -------------------------------------------------------- strides and values
+
+def by_head(x):
+    """x [tokens, heads, D] stored head by head, with a gap between them."""
+    T, H, D = x.shape
+    room = torch.full((H, T + 3, D + 8), float("nan"), dtype=x.dtype,
+                      device=x.device)
+    view = room[:, 1:T + 1, :D].transpose(0, 1)
+    view.copy_(x)
+    assert view.stride(1) > view.stride(0)
+    return view
+
+
+def test_rows_stored_head_by_head():
+    s = Step(45)
+    here, o = s.outputs(), s.outputs()
+    s.call(here)
+    st = o["status"]
+    s.call(o)
+    o["cache"].copy_(s.big)
+    k, v = by_head(torch.zeros_like(s.k)), by_head(torch.zeros_like(s.v))
+    attn.lumen_attn_append4(s.sh, s.big_nb, 0, o["cache"], by_head(s.k),
+                            by_head(s.v), o["slots"], st)
+    attn.lumen_attn_read4(s.sh, s.big_nb, 0, o["cache"], o["slots"], k, v, st)
+    attn.lumen_attn_decode4(s.sh, s.nb, 0, s.cache, s.table, s.lens,
+                            by_head(s.q), o["out"], s.ws, st)
+    attn.lumen_attn_prompt(by_head(s.pq), by_head(s.pk), by_head(s.pv),
+                           o["prompt"], s.cu_q, st, cu_k=s.cu_k,
+                           workspace=s.pws)
+    same(o, here)
+    assert torch.equal(k, here["k"]) and torch.equal(v, here["v"])
+    # the gaps between the rows are as they were
+    assert torch.isnan(k._base[:, 0]).all() and torch.isnan(v._base[:, -1]).all()
+
+
+@pytest.mark.parametrize("size,scale", [(1e30, 1e-31), (1e-30, 1e29),
+                                        (1e5, 1e-6), (3e38, 1e-40)])
+def test_decode_bf16_queries_of_any_size(size, scale):
+    rng = np.random.default_rng(16)
+    sh, nb, cache, rows, table, lens, q = decode_case(
+        rng, [70, 1, 600], 2, 4, 128, 16, "NHD", BF)
+    q = (q.float().clamp(-1, 1) * size).to(BF)
+    want, slack = decode_want(rows(0), table, lens, q, 2, 16, scale, BF)
+    ref.assert_close(run_decode(sh, nb, cache, table, lens, q, scale), want,
+                     slack, BF)
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+def test_decode_queries_with_elements_of_very_different_sizes(dtype):
+    """One element far above the others, over keys that are 0 there: what is
+    left of the others is all there is."""
+    rng = np.random.default_rng(17)
+    sh, nb, cache, rows, table, lens, q = decode_case(
+        rng, [70, 1, 600], 2, 4, 128, 16, "NHD", dtype)
+    q[..., 3] = 2.0 ** 15
+    # the first quarter of every key: codes of 0 under A = 0 and B = 0
+    first = rows(0)[0]
+    first[..., :16] = 0
+    first[..., 64:68] = 0
+    want, slack = decode_want(rows(0), table, lens, q, 2, 16, 128 ** -0.5,
+                              dtype)
+    ref.assert_close(run_decode(sh, nb, cache, table, lens, q), want, slack,
+                     dtype)
+
+
+# --------------------------------------------------------- forms of a prompt
+
+@pytest.mark.parametrize("R", [65, 128, 129, 200])
+@pytest.mark.parametrize("bad", [False, True])
+def test_more_sequences_than_lanes_without_a_plan(R, bad):
+    """Tiles that find themselves in a second round of sequences, also behind
+    bounds that are refused."""
+    g = torch.Generator(device=dev()).manual_seed(R)
+    n = np.random.default_rng(R).integers(1, 6, R)
+    cu = np.concatenate([[0], np.cumsum(n)])
+    T, H, G = int(cu[-1]), 1, 4
+    q = torch.randn(T, H * G, 64, generator=g, device=dev()).to(BF)
+    k, v = (torch.randn(T, H, 64, generator=g, device=dev()).to(BF)
+            for _ in range(2))
+    assert attn.new_prompt_workspace(q, k, R) is None
+    want, slack = prompt_want(q, k, v, cu, cu, 0.125, ref.UNIT[BF])
+    out, status, bounds = torch.full_like(q, 7.0), word(), cu.copy()
+    if bad:
+        bounds[64] = T + 1  # the 64th sequence and the one after it
+        gone = slice(int(cu[63]), int(cu[65]))
+        want[gone], slack[gone] = 7.0, 0.0
+    attn.lumen_attn_prompt(q, k, v, out, i32(bounds), status)
+    assert int(status) == (ref.RANGE if bad else 0)
+    ref.assert_close(out, want, slack, BF)
+
+
+@pytest.mark.parametrize("R", [65, 200])
+def test_bad_bounds_past_the_first_lanes_are_recorded(R):
+    """In the last sequence of all, which no tile looks for."""
+    T = 2 * R
+    q = torch.zeros(T, 4, 64, dtype=BF, device=dev())
+    k = torch.zeros(T, 1, 64, dtype=BF, device=dev())
+    cu = np.arange(0, T + 1, 2)
+    cu[-1] = T + 1
+    out, status = torch.full_like(q, 7.0), word()
+    attn.lumen_attn_prompt(q, k, k, out, i32(cu), status)
+    assert int(status) == ref.RANGE
+    assert bool((out[:-2] == 0).all()) and bool((out[-2:] == 7.0).all())
+
+
+@pytest.mark.parametrize("dtype,H,G,D", [(BF, 16, 4, 64), (FP, 2, 32, 128)])
+def test_values_that_are_not_finite_in_larger_workgroups(dtype, H, G, D):
+    """Eight wavefronts, four tiles in turn: some early, some late and some
+    neighbouring values are NaN or infinite."""
+    n = 2048
+    g = torch.Generator(device=dev()).manual_seed(18)
+    q = torch.randn(n, H * G, D, generator=g, device=dev()).to(dtype)
+    k, v = (torch.randn(n, H, D, generator=g, device=dev()).to(dtype)
+            for _ in range(2))
+    want, slack = prompt_want(q, k, v, [0, n], [0, n], D ** -0.5,
+                              ref.UNIT[dtype])
+    for key, h, e, x in ((0, 0, 1, "inf"), (700, 1, 5, "nan"),
+                         (701, 1, 5, "inf"), (702, 1, 6, "-inf"),
+                         (703, 1, 6, "inf"), (1151, 0, D - 1, "-inf"),
+                         (1152, 0, D - 2, "nan"), (n - 1, 1, 0, "inf")):
+        v[key, h, e] = float(x)
+        want[key:, h * G:h * G + G, e] += float(x)
+    out = run_prompt(q, k, v, [0, n]).double()
+    z, fine, inf = torch.zeros_like(want), want.isfinite(), want.isinf()
+    assert torch.equal(out.isnan(), want.isnan())
+    assert torch.equal(out.isinf(), inf) and torch.equal(out[inf], want[inf])
+    ref.assert_close(torch.where(fine, out, z), torch.where(fine, want, z),
+                     torch.where(fine, slack, z), dtype)
