@@ -486,10 +486,6 @@ __device__ __forceinline__ float inverse(float m, float l) {
   return m == -INFINITY ? 0.0f : 1.0f / l;
 }
 
-// What a wavefront's rows share: the workgroup's other heads' places and cache
-// lines that other workgroups read too; only the places; nothing.
-enum class Sharing { kLines, kStep, kNone };
-
 // Decode attention, bound by the cache's bytes: D/2 + 16 a row, read once.
 //
 // Work.  A workgroup takes wg_heads KV heads, those that lie side by side in a
@@ -523,10 +519,14 @@ enum class Sharing { kLines, kStep, kNone };
 // one, 119 us, 3.7 TB/s (a wavefront's own rows, 1,280 bytes of a page at a
 // time); three of 100,000, 96 us, 4.1 TB/s (the join is 4.5 us of it).  D 256, 64
 // requests of 4,096 tokens, 32 query heads over 8: 141 us, 4.3 TB/s.
-template <int D, Sharing kSharing>
+//
+// kPrivate: one head a workgroup, whose wavefronts load their own blocks' rows and
+// wait for nobody else's.  Rows are not kept in caches (nt), also where a workgroup
+// takes a part of the heads and shares lines with others: 64 requests around 2,048
+// tokens, 64 query heads over 16, D 128, take 96 us, and 103 with rows kept; 32 at D
+// 256 94 and 97; 64 of 32 over 32 176 both.
+template <int D, bool kPrivate>
 __global__ __launch_bounds__(kDecodeThreads, 2) void decode4_kernel(DecodeArgs a) {
-  constexpr bool kPrivate = kSharing == Sharing::kNone;
-  constexpr bool kStream = kSharing != Sharing::kLines;
   constexpr int kRow = D / 2 + 16;
   constexpr int kSteps = D / 32;  // products over head_dim
   constexpr int kE = D / 16;      // elements of V a lane holds of a key
@@ -637,7 +637,6 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void decode4_kernel(DecodeArgs a
   const uint8_t *const k_at = a.k + heads_at, *const v_of = a.v + heads_at;
 #pragma unroll
   for (int i = 0; i < kIssues; ++i) {
-    // kNone: a wavefront loads its own block's rows
     const int half = kPrivate ? kBlockKeys * kParts : step_keys * pieces;
     int c = kPrivate ? i * kWave + lane : i * kDecodeThreads + tid;
     const bool is_v = c >= half;
@@ -1067,7 +1066,7 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void decode4_kernel(DecodeArgs a
         const uint32_t to = ring_at + stage * kStage;
 #pragma unroll
         for (int c = 0; c < kIssues; ++c)
-          load_to_lds<kStream>(from[c], to + c * (kPrivate ? kWave : kDecodeThreads) * 16);
+          load_to_lds(from[c], to + c * (kPrivate ? kWave : kDecodeThreads) * 16);
       };
       const auto live_of = [&](int i) __attribute__((always_inline)) {
         return active ? uint32_t(read(int(live_keys[i * a.wg_blocks + kbi]))) : 0u;
@@ -1249,10 +1248,8 @@ struct DecodeKernels {
 };
 
 template <int D>
-DecodeKernels decode_kernels(bool bf16, Sharing sharing) {
-  return {sharing == Sharing::kNone   ? decode4_kernel<D, Sharing::kNone>
-          : sharing == Sharing::kStep ? decode4_kernel<D, Sharing::kStep>
-                                      : decode4_kernel<D, Sharing::kLines>,
+DecodeKernels decode_kernels(bool bf16, bool one_head) {
+  return {one_head ? decode4_kernel<D, true> : decode4_kernel<D, false>,
           bf16 ? decode4_join_kernel<D, true> : decode4_join_kernel<D, false>};
 }
 
@@ -1458,12 +1455,10 @@ int lumen_attn_decode4(const lumen_kv_layout *layout, int32_t layer,
   a.bf16 = dtype == LUMEN_ATTN_BF16;
   a.spans = shared ? static_cast<int2 *>(d_workspace) : nullptr;
   a.parts = reinterpret_cast<float *>(static_cast<char *>(d_workspace) + plan.parts_at);
-  const Sharing sharing = plan.wg_heads == 1         ? Sharing::kNone
-                          : plan.wg_heads == a.heads ? Sharing::kStep
-                                                     : Sharing::kLines;
-  const DecodeKernels k = at.head_dim == 64    ? decode_kernels<64>(a.bf16, sharing)
-                          : at.head_dim == 128 ? decode_kernels<128>(a.bf16, sharing)
-                                               : decode_kernels<256>(a.bf16, sharing);
+  const bool one = plan.wg_heads == 1;
+  const DecodeKernels k = at.head_dim == 64    ? decode_kernels<64>(a.bf16, one)
+                          : at.head_dim == 128 ? decode_kernels<128>(a.bf16, one)
+                                               : decode_kernels<256>(a.bf16, one);
   hipStream_t s = static_cast<hipStream_t>(stream);
   hipLaunchKernelGGL(k.main, dim3(unsigned(plan.workers * plan.sets)),
                      dim3(kDecodeThreads), 0, s, a);

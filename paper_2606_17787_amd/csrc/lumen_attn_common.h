@@ -73,21 +73,16 @@ __device__ __forceinline__ void both(float x, float *a, float *b) {
 }
 
 // Starts a load of 16 bytes a lane from the lane's address into LDS, at byte
-// `to` + 16 * lane (`to` the wavefront's; kStream: not to be kept in caches).  `to`
-// goes through m0, which the compiler writes, since it uses m0 itself.  The load is
+// `to` + 16 * lane (`to` the wavefront's), not to be kept in caches.  `to` goes
+// through m0, which the compiler writes, since it uses m0 itself.  The load is
 // counted like any load, but the compiler does not know of it: wait_loads<n> waits
 // until at most the last n are still under way, and keeps reads of the LDS behind
 // it.  That, unlike the builtin, lets a read wait for its own block alone.
-template <bool kStream>
 __device__ __forceinline__ void load_to_lds(const void *from, uint32_t to) {
-  if constexpr (kStream)
-    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt"
-                 :: "{m0}"(to), "v"(from) : "memory");
-  else
-    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
-                 :: "{m0}"(to), "v"(from) : "memory");
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt"
+               :: "{m0}"(to), "v"(from) : "memory");
 }
-// The same from byte `at` of the lane on, of memory at `from`.
+// The same from byte `at` of the lane on, of memory at `from`, kept in caches.
 __device__ __forceinline__ void load_to_lds(const void *from, uint32_t at, uint32_t to) {
   asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
                :: "{m0}"(to), "v"(at), "s"(from) : "memory");

@@ -29,8 +29,7 @@ __global__ void probe(const char *from, char *out) {
 
 
 @pytest.mark.skipif(not os.path.exists(HIPCC), reason="no hipcc")
-@pytest.mark.parametrize("call", ["load_to_lds<false>(from, 1024)",
-                                  "load_to_lds<true>(from, 1024)",
+@pytest.mark.parametrize("call", ["load_to_lds(from, 1024)",
                                   "load_to_lds(from, threadIdx.x * 16, 1024)"])
 def test_the_compiler_knows_that_a_load_into_lds_takes_m0(tmp_path, call):
     src = tmp_path / "probe.hip"
