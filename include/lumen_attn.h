@@ -45,6 +45,15 @@
  * (device int32, 4-byte aligned; write LUMEN_OK to it first) to the most
  * negative code seen while everything else is still computed.  No call
  * clears memory with a memset, so all can be captured in a graph.
+ *
+ * Arithmetic of decode4 and prompt.  Scores (before and after the scale), their
+ * maxima, and all sums are held in 32 bits; a score or a sum of weights times
+ * values that passes their range becomes infinite.  For the products with V the
+ * weights are rounded to 16 bits, prompt's to the type of the inputs (one part in
+ * 2^9 or 2^12 each), decode4's to 16-bit floats (2^12); the sum they are divided by
+ * is taken before that.  decode4 takes q as 16-bit floats under a power of two of
+ * the row's own: exact down to 2^-27 of the row's largest element.  Values of the
+ * 4-bit cache are exact.
  */
 #ifndef LUMEN_ATTN_H
 #define LUMEN_ATTN_H
@@ -144,12 +153,13 @@ size_t lumen_attn_decode4_workspace_bytes(const lumen_kv_layout *layout,
  * t < d_lens[r], G = num_q_heads / H (H must divide num_q_heads, at most
  * 65535).  q: rows
  * (r, h) of dtype; d_out [num_reqs][num_q_heads][D] of dtype, contiguous,
- * 16-byte aligned.  scale must be above 0 and scale * log2(e) finite.  A request
- * of length 0 gets zeros; a negative one too (RANGE).  Tokens in pages past bt_cols
- * (RANGE) or with a block id outside [0, num_blocks) (BLOCK_ID) are left out
- * of the sum; where all are, the row is zeros.  A row with a score of NaN or
- * +infinity, or with none but -infinity, is NaN.  What the cache holds past a request's length does not matter,
- * NaN included.  The result does not depend on timing.  d_workspace:
+ * 16-byte aligned.  scale must be above 0 and scale * log2(e) finite.  A
+ * request of length 0 gets zeros; a negative one too (RANGE).  Tokens in pages
+ * past bt_cols (RANGE) or with a block id outside [0, num_blocks) (BLOCK_ID)
+ * are left out of the sum; where all are, the row is zeros.  A row with a score
+ * of NaN or +infinity, or with none but -infinity, is NaN.  What the cache
+ * holds past a request's length does not matter, NaN included.  The result
+ * does not depend on timing.  d_workspace:
  * lumen_attn_decode4_workspace_bytes bytes, 16-byte aligned, not shared by
  * calls in flight at the same time; what it holds does not matter. */
 int lumen_attn_decode4(const lumen_kv_layout *layout, int32_t layer,
@@ -177,13 +187,12 @@ size_t lumen_attn_prompt_workspace_bytes(int32_t num_seqs, int64_t num_q_tokens,
  * uses KV head h / (num_q_heads / num_kv_heads).  d_out
  * [num_q_tokens][num_q_heads][head_dim], contiguous, 16-byte aligned; rows of
  * tokens in no sequence are not written.  head_dim 64 or 128.  scale above 0,
- * scale * log2(e) finite.  A sequence whose bounds fall outside [0, num_q_tokens] or [0,
- * num_k_tokens], or end before they begin, is skipped (RANGE).  Sequences must
- * not share queries.  Token counts at most LUMEN_ATTN_MAX_TOKENS; token strides
- * of k and v at most LUMEN_ATTN_MAX_STRIDE where they have more than one token;
- * sizes that would need a launch of 2^32 threads or more are refused
- * (UNSUPPORTED).
- * What a query does not see does not reach its row, NaN and infinities
+ * scale * log2(e) finite.  A sequence whose bounds fall outside [0,
+ * num_q_tokens] or [0, num_k_tokens], or end before they begin, is skipped
+ * (RANGE).  Sequences must not share queries.  Token counts at most
+ * LUMEN_ATTN_MAX_TOKENS; token strides of k and v at most LUMEN_ATTN_MAX_STRIDE
+ * where they have more than one token; sizes that would need a launch of 2^32
+ * threads or more are refused (UNSUPPORTED).  What a query does not see does not reach its row, NaN and infinities
  * included; a NaN or infinity among the values it sees does, and a row with a
  * score of NaN or +infinity, or with none but -infinity, is NaN.  d_workspace:
  * lumen_attn_prompt_workspace_bytes bytes (NULL where that is 0), 16-byte aligned,

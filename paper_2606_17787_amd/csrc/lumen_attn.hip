@@ -424,10 +424,18 @@ constexpr int kBlockKeys = 32;  // keys a wavefront takes at a time
 constexpr int kSegments = kWave;
 // A round's steps, tiles and blocks of 32 keys.
 constexpr int kRoundSteps = 128, kTiles = 1024, kLive = 512, kLast = 256;
-constexpr int kUnitBlocks = 4;  // a unit of work, in the workgroup's blocks
+// A unit of work, in the workgroup's blocks.  Shorter ones share more evenly and cut
+// more requests, whose parts the second kernel joins: with 1, 2, 4 and 8 of them 256
+// requests around 2,048 tokens take 179, 180, 180 and 186 us, 512 around 4,096 of one
+// KV head 118, 115, 118 and 124, 512 around 100 of 8 heads 51, 50, 52 and 59, four
+// around 1,000 24, 21, 23 and 28.
+constexpr int kUnitBlocks = 4;
 constexpr int kQueries = 16;    // columns of a product
-// Weights are 2^(s - m + kBias) with s - m at most kRise: within a 16-bit
-// float up to 2^14, and down to 2^-38 of the largest before they vanish.
+// Weights are 2^(s - m + kBias) with s - m at most kRise, rounded to 16-bit floats
+// for the products with V; their own sum is taken before that, in 32 bits.  They
+// stay under 2^14.  Where the maximum is not behind, one keeps its 11 bits down to
+// 2^-20 of the largest and vanishes under 2^-31 of it, so that n such keys lose at
+// most n * 2^-31 of the values' size.
 constexpr float kRise = 8.0f, kBias = 6.0f;
 
 template <int kE, bool kBf16>
@@ -514,11 +522,11 @@ __device__ __forceinline__ float inverse(float m, float l) {
 // are exact: code and pair give the stored value by one fused multiply-add that
 // rounds as the format says.
 //
-// Measured, D 128, a large copy being 4.85 TB/s: 256 requests around 2,048
-// tokens, 32 query heads over 8, 181 us, 4.9 TB/s; 512 around 4,096 of 8 over
-// one, 119 us, 3.7 TB/s (a wavefront's own rows, 1,280 bytes of a page at a
-// time); three of 100,000, 96 us, 4.1 TB/s (the join is 4.5 us of it).  D 256, 64
-// requests of 4,096 tokens, 32 query heads over 8: 141 us, 4.3 TB/s.
+// Measured, D 128: 256 requests around 2,048 tokens, 32 query heads over 8, 181
+// us, 4.9 TB/s; 512 around 4,096 of 8 over one, 118 us, 3.8 TB/s (a wavefront's own
+// rows, 1,280 bytes of a page at a time); three of 100,000, 96 us, 4.1 TB/s (the join
+// is 4.5 us of it).  D 256, 64 requests of 4,096 tokens, 32 query heads over 8: 126
+// us, 4.8 TB/s, with two registers spilled where heads lie together.
 //
 // kPrivate: one head a workgroup, whose wavefronts load their own blocks' rows and
 // wait for nobody else's.  Rows are not kept in caches (nt), also where a workgroup
@@ -681,8 +689,11 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void decode4_kernel(DecodeArgs a
   const uint32_t v_at = (kPrivate ? kBlockKeys : step_keys) * key_bytes;
   constexpr int kOwn = 2 * kBlockKeys * kRow;  // bytes of a wavefront's block
 
-  // ---- Q: 16-bit floats under a power of two of the row's own, so that bf16
-  // and fp16 keep all their bits whatever their range
+  // ---- Q: 16-bit floats under a power of two of the row's own, which takes its
+  // largest element to 2^13..2^14: bf16 has too wide a range for a 16-bit float, and
+  // the products with the exact K need one.  Elements down to 2^-27 of the largest
+  // keep all their bits; what smaller ones lose is under 2^-38 of the largest, far
+  // less than the rounding of the scores' sums to 32 bits.
   half8v q[kSteps];
   float cq = 0.0f;
   uint4 raw[D == 256 ? 1 : kSteps];
@@ -1227,7 +1238,10 @@ DecodePlan decode_plan(const lumen_kv_layout *l, int32_t head_dim,
   const int group = num_q_heads / l->num_kv_heads;
   DecodePlan p;
   // the most heads whose rows lie together, and blocks of keys for the rest of
-  // the wavefronts
+  // the wavefronts: 256 requests around 2,048 tokens over 8 heads take 371 us with one
+  // head a workgroup, 215 with 2, 191 with 4 and 180 with 8, 64 over 16 heads 198, 119,
+  // 107 and 103.  (Eight short requests of 2 heads take 12.8 with one and 14.8 with
+  // both.)
   p.wg_heads = 1;
   if (l->cache_order == LUMEN_CACHE_NHD)
     for (int d = 2; d <= kDecodeWaves; ++d)
@@ -1353,7 +1367,10 @@ int lumen_attn_slots(const int32_t *d_start, const int32_t *d_end,
              num_slots, d_cu,  d_lens,       d_free_left, d_status};
   const int64_t per = int64_t(kSlotThreads) * kSlotTokens;
   int64_t blocks = num_slots / per + (num_slots % per != 0);
-  // the new pages are at most this many, a thread each
+  // the new pages are at most this many, a thread each, on a workgroup for 16
+  // requests at most: each scans all of them (pages alone of 1,024 prompts of 512
+  // tokens: 9.5 us, and 8.4 with a workgroup for 2, 13.4 for 64; of 8 prompts of 8,192
+  // 7.6, 4.4 and 7.6)
   const int64_t pages = (free_cap + kSlotThreads - 1) / kSlotThreads;
   const int64_t page_wgs = pages < num_reqs / 16 + 1 ? pages : num_reqs / 16 + 1;
   if (blocks < page_wgs) blocks = page_wgs;

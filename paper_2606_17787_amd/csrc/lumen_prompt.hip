@@ -87,9 +87,15 @@ __device__ __forceinline__ int swizzle_v(int row) {
 }
 
 // Tiles are cut into parts of at least this many keys: shorter ones would cost
-// more to start and to join than they save.
+// more to start and to join than they save (3 sequences around 40 queries behind up
+// to 5,000 keys, 8 query heads over one: 30 us, 33 with 256 and 35 with 1,024; 2 of
+// 128 behind up to 16,384, 32 over 8: 68, 68 and 71).
 constexpr int kMinPartKeys = 512;
-// Keys of a call from which on tiles may be cut.
+// Keys of a call from which on tiles may be cut, in all its sequences: their own
+// lengths are on the device.  With 2,048, 4,096 and 8,192, 2 sequences around 100
+// queries behind up to 3,500 keys take 28, 63 and 63 us, one prompt of 2,048 tokens
+// 41, 38 and 39 (8 query heads over 2), 64 of 32 21, 17 and 17, where nothing is cut:
+// what the plan and the join cost a call is less than what long keys do uncut.
 constexpr int kCutKeys = 2048;
 
 __device__ __forceinline__ int steps_to(int keys) {
@@ -413,11 +419,11 @@ __device__ __forceinline__ void add_nonfinite(const uint16_t *row, bool seen, f3
 // Bound by the matrix units and the power they draw, the vector unit close behind
 // (32 exponentials and about 150 other instructions a wavefront and step, against
 // 32 products): one prompt of 16,384 tokens, 32 query heads over 8, D 128, takes
-// 1.89 ms, 1.16 PFLOP/s (a large library product: 1.37), with the units busy 56%
-// of the cycles at 1.7 GHz.  Letting half of the wavefronts lag behind by half a
-// step, so that products meet exponentials, or giving them priority changed
-// nothing.  Short sequences lose to the tiles' ragged ends and few steps: 24 of
-// 384 or so take 123 us, 0.64 PFLOP/s.
+// 1.92 to 2.17 ms on one card and another, 1.01 to 1.15 PFLOP/s (a large library
+// product: 1.37), with the units busy 56% of the cycles at 1.7 GHz.  Letting half of
+// the wavefronts lag behind by half a step, so that products meet exponentials, or
+// giving them priority changed nothing.  Short sequences lose to the tiles' ragged
+// ends and few steps: 24 of 384 or so take 126 us, 0.62 PFLOP/s.
 //
 // A value that is masked for some of a wavefront's queries has the weight 0 for
 // them in the products, which keeps it out unless it is an infinity or NaN.
@@ -624,7 +630,7 @@ __device__ __forceinline__ bool prompt_tile(const PromptArgs &a, const int tid,
       for (int i = 0; i < 16; ++i) {
         const float x =
             __builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][i], a.scale_log2, -ms));
-        l += x;
+        l += x;  // before the rounding, which the products need
         pr[2 * t + i / 8][i % 8] = short(rounded<kBf16>(x));
       }
     // ---- weighted values
@@ -774,13 +780,13 @@ struct PromptPlan {
 constexpr int kMaxUnits = 256;
 
 // Wavefronts of a workgroup. Eight share a tile of keys among twice the queries
-// and keep two more tiles under way: 2.03 ms against 2.17 for one prompt of
-// 16,384 tokens (32 query heads over 8, D 128), 144 us against 153 for 4,096,
-// 83 against 86 for 8 x 2,048 tokens of 8 heads over one. Four, of which two
+// and keep two more tiles under way: 1.92 ms against 1.96 for one prompt of
+// 16,384 tokens (32 query heads over 8, D 128), 142 us against 149 for 4,096,
+// 83 against 84 for 8 x 2,048 tokens of 8 heads over one. Four, of which two
 // workgroups run on a compute unit, leave fewer lanes idle at the ends of
-// sequences and spread few tiles better: 106 us against 122 for 64 prompts of
-// 256 tokens, 98 against 103 for 8 of 1,024, 67 against 70 for one of 2,048,
-// 76 against 87 for 4,096 tokens of 8 heads over one behind 16,384.
+// sequences and spread few tiles better: 101 us against 122 for 64 prompts of
+// 256 tokens, 89 against 100 for 8 of 1,024, 59 against 62 for one of 2,048,
+// 154 against 160 for 5 around 1,237 tokens of 8 heads over one behind up to 11,003.
 int prompt_waves(int32_t num_seqs, int64_t num_q, int32_t q_heads) {
   const bool long_ones = num_q >= int64_t(num_seqs) * 2048;
   const bool many = num_q * q_heads / (8 * 32) >= 2 * kMaxUnits;
@@ -811,8 +817,11 @@ PromptPlan prompt_plan(int32_t num_seqs, int64_t num_q, int64_t num_k,
     const int64_t most = p.tiles * (num_k / kMinPartKeys + 2);
     if (p.parts > most) p.parts = most;
   }
-  // the same for every device, as the workspace's size is: a small device takes
-  // a call's few tiles without a plan too, in another order
+  // Without a plan every workgroup looks its tile up, 64 sequences at a time: 9.3 us
+  // against 14.8 with one for 8 prompts around 216 tokens (4 query heads over 2), 17
+  // against 20 for 128 of 12 (32 over 8), but 49 against 40 for 400 of 4 and 155
+  // against 82 for 1,000 of 2.  The same for every device, as the workspace's size is:
+  // a small device takes a call's few tiles without a plan too, in another order.
   p.planned = p.parts > 0 || p.tiles > slots(kMaxUnits);
   const auto up = [](size_t n) { return (n + 255) & ~size_t(255); };
   p.units_at = 256;  // the number of cuts stands first
