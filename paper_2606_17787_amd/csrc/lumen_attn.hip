@@ -306,8 +306,8 @@ __device__ __forceinline__ float across(float x) {
 // Quantises rows: D/8 lanes a row, 8 elements a lane (one 16-byte load, one
 // dword of codes).  Memory-bound, 2*D bytes in and D/2 + 16 out a row, as long as
 // its arithmetic stays under 100 or so instructions a load: 16,411 tokens of 8
-// heads, D 128, take 20.7 us, 4.3 TB/s, and their reading back 16.9 us, 5.2 TB/s
-// (a large copy: 4.85).
+// heads, D 128, take 18.7 to 20.7 us, 4.3 to 4.7 TB/s, and their reading back 16.5 to
+// 16.9, 5.2 to 5.3 TB/s (a large library copy: 4.5 to 5.0).
 template <int D, bool kBf16>
 __global__ __launch_bounds__(kRowThreads) void append4_kernel(RowArgs a) {
   constexpr int kLanes = D / 8;        // lanes of a row
