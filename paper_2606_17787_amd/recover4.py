@@ -98,12 +98,16 @@ class Worker:
         single = bool((end - start == 1).all())
         before = 0 if single else int(start.sum())
         if before:
-            # every token's slot, and which of the packed keys are old ones
+            # every token's slot, which of the packed keys are old ones, and where
+            # the new ones go (by arithmetic: no wait for the device)
             zero = torch.zeros_like(start)
             all_slots, cu_k = self.pages(zero, end, before + tokens.numel())
             at = torch.arange(all_slots.numel(), device=self.device)
             r = torch.searchsorted(cu_k, at, right=True) - 1
             old = at - cu_k[r] < start[r]
+            new = torch.arange(tokens.numel(), device=self.device)
+            r = torch.searchsorted(cu, new, right=True) - 1
+            new = new - cu[r] + start[r] + cu_k[r]
         for layer in range(self.m.layers):
             q, k, v = self.m.project(layer, x)
             attn.lumen_attn_append4(self.shape, self.nb, layer, self.cache, k,
@@ -122,7 +126,8 @@ class Worker:
                 attn.lumen_attn_read4(
                     self.shape, self.nb, layer, self.cache,
                     torch.where(old, all_slots, -1), ka, va, self.status)
-                ka[~old], va[~old] = k, v
+                ka.index_copy_(0, new, k)
+                va.index_copy_(0, new, v)
                 attn.lumen_attn_prompt(q, ka, va, out, cu, self.status,
                                        cu_k=cu_k)
             x = self.m.add(layer, x, out)
