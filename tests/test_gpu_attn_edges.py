@@ -626,3 +626,28 @@ def test_values_that_are_not_finite_in_larger_workgroups(dtype, H, G, D):
     assert torch.equal(out.isinf(), inf) and torch.equal(out[inf], want[inf])
     ref.assert_close(torch.where(fine, out, z), torch.where(fine, want, z),
                      torch.where(fine, slack, z), dtype)
+
+
+def test_a_prepared_prompt_with_its_own_workspace_in_a_graph():
+    """Captured on a stream that is not the workspace's, and replayed between
+    eager work."""
+    s = Step(46)
+    o, here = s.outputs(), s.outputs()
+    call = attn.prepare_prompt(s.pq, s.pk, s.pv, o["prompt"], s.cu_q,
+                               o["status"], cu_k=s.cu_k)
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for _ in range(3):
+        for t in (s.pq, s.pk, s.pv):
+            t.copy_(torch.randn(t.shape, device=dev()))
+        attn.lumen_attn_prompt(s.pq, s.pk, s.pv, here["prompt"], s.cu_q,
+                               here["status"], cu_k=s.cu_k, workspace=s.pws)
+        o["prompt"].fill_(7.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(o["prompt"], here["prompt"])
+        assert int(o["status"]) == 0
