@@ -49,11 +49,12 @@
  * Arithmetic of decode4 and prompt.  Scores (before and after the scale), their
  * maxima, and all sums are held in 32 bits; a score or a sum of weights times
  * values that passes their range becomes infinite.  For the products with V the
- * weights are rounded to 16 bits, prompt's to the type of the inputs (one part in
- * 2^9 or 2^12 each), decode4's to 16-bit floats (2^12); the sum they are divided by
- * is taken before that.  decode4 takes q as 16-bit floats under a power of two of
- * the row's own: exact down to 2^-27 of the row's largest element.  Values of the
- * 4-bit cache are exact.
+ * weights are rounded to 16 bits, prompt's to the type of the inputs (one part
+ * in 2^9 or 2^12 each), decode4's to 16-bit floats (2^12); the sum they are
+ * divided by is taken before that.  As 16-bit floats, weights under 2^-20 of the
+ * row's largest keep fewer bits, and under 2^-31 of it none.  decode4 takes q as
+ * 16-bit floats under a power of two of the row's own: exact down to 2^-27 of
+ * the row's largest element.  Values of the 4-bit cache are exact.
  */
 #ifndef LUMEN_ATTN_H
 #define LUMEN_ATTN_H
