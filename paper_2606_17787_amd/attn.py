@@ -170,13 +170,16 @@ def _slots_args(start, end, block_tables, block_size, num_blocks, free,
     if free_count.numel() != 1 or free_left.numel() != 1:
         raise ValueError("free_count and free_left are one int64 element")
     _kv._check_tables(block_tables, R)
+    # an empty tensor has no address, which would say that no map is wanted
+    into = None if slots is None else (_kv._dev(slots, "slots", i64) or
+                                       free_left.data_ptr())
     return (_kv._dev(start, "start", i32), _kv._dev(end, "end", i32),
             None if have is None else _kv._dev(have, "have", i32), R,
             _kv._dev(block_tables, "block_tables", i32),
             block_tables.shape[1], int(block_size), int(num_blocks),
             _kv._dev(free, "free", i32),
             _kv._dev(free_count, "free_count", i64), free.numel(),
-            None if slots is None else _kv._dev(slots, "slots", i64),
+            into,
             0 if slots is None else slots.numel(),
             _kv._dev(cu, "cu", i32), _kv._dev(lens, "lens", i32),
             _kv._dev(free_left, "free_left", i64), _status(status))

@@ -651,3 +651,19 @@ def test_a_prepared_prompt_with_its_own_workspace_in_a_graph():
         torch.cuda.synchronize()
         assert torch.equal(o["prompt"], here["prompt"])
         assert int(o["status"]) == 0
+
+
+def test_slots_of_an_empty_map():
+    """A map without room for the tokens there are is an error; None is not."""
+    for slots, tokens, want in ((0, 3, ref.CAPACITY), (0, 0, 0), (None, 3, 0)):
+        table, status = i32(np.full((1, 2), -1)), word()
+        cu, lens, left = i32([0, 0]), i32([0]), torch.zeros(
+            1, dtype=torch.int64, device=dev())
+        if slots is not None:
+            slots = torch.empty(0, dtype=torch.int64, device=dev())
+        attn.lumen_attn_slots(i32([0]), i32([tokens]), table, 16, 9,
+                              i32([3, 4]), torch.tensor([2], device=dev()),
+                              slots, cu, lens, left, status)
+        assert int(status) == want
+        assert cu.tolist() == [0, tokens] and lens.tolist() == [tokens]
+        assert table[0, 0] == (4 if tokens else -1)
