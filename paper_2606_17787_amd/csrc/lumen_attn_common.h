@@ -103,8 +103,9 @@ __device__ __forceinline__ void lds_barrier() {
 
 // A value that is the same in all lanes, in scalar registers.
 __device__ __forceinline__ uint64_t uniform(uint64_t x) {
-  return uint64_t(__builtin_amdgcn_readfirstlane(uint32_t(x))) |
-         uint64_t(__builtin_amdgcn_readfirstlane(uint32_t(x >> 32))) << 32;
+  // (the builtin's result has a sign, which must not reach the upper half)
+  return uint64_t(uint32_t(__builtin_amdgcn_readfirstlane(uint32_t(x)))) |
+         uint64_t(uint32_t(__builtin_amdgcn_readfirstlane(uint32_t(x >> 32)))) << 32;
 }
 
 // lumen_attn_rows, typed.

@@ -220,6 +220,19 @@ def test_attend_bad_requests_and_pages(max_new):
     c.check(max_new=max_new)
 
 
+@pytest.mark.parametrize("m", [1, 9, 70])
+@pytest.mark.parametrize("dead", [(2,), (3,), (2, 3), (0, 3), (1,), (4, 7, 11)])
+@pytest.mark.parametrize("bs", [16, 8, 5])
+def test_attend_and_weigh_with_dead_pages_anywhere(m, dead, bs):
+    """Places of every part of a step left out, and counted ones around them."""
+    c = Case([200, 130], [m, m], 2, 4, 128, bs, seed=5, dtype=FP)
+    for page in dead:
+        c.table[0, page * 16 // bs] = -1
+        c.table[1, page % 8 * 16 // bs] = c.nb + 7
+    c.check(max_new=m)
+    check_weigh(c, max_new=m)
+
+
 def test_attend_skips_requests_with_bad_bounds():
     c = Case([300, 200, 100, 80, 50], [3, 60, 7, 0, 4], 2, 4, 128, seed=6)
     c.check(max_new=59)  # the second has too many: skipped
