@@ -45,10 +45,6 @@ struct AttendArgs : Call {
 
 constexpr int kKeys = 64;  // places of a step
 
-// Rows of places that are left out are read from here, so that what the cache
-// holds there reaches nothing.
-__device__ __attribute__((aligned(16))) const uint16_t kZeroRow[128] = {};
-
 __device__ __forceinline__ int steps_to(int places) {
   return places > 0 ? int((uint32_t(places) + kKeys - 1) / kKeys) : 0;
 }
@@ -305,13 +301,6 @@ __device__ __forceinline__ void write_lse(const AttendArgs &a, const Row &r, flo
                                        0.693147180559945309f;
 }
 
-// Starts a load of 16 bytes a lane from the lane's address into LDS at byte `to` +
-// 16 * lane, kept in caches; see load_to_lds.
-__device__ __forceinline__ void load_row(const void *from, uint32_t to) {
-  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
-               :: "{m0}"(to), "v"(from) : "memory");
-}
-
 template <int D, int kWaves>
 struct TileShape {
   static constexpr int kThreads = kWaves * kWave;
@@ -417,14 +406,25 @@ __global__ __launch_bounds__(kWaves *kWave, 2) void attend_kernel(AttendArgs a) 
   const auto load = [&](int at, int buf) __attribute__((always_inline)) {
     const uint32_t to = lds_at + buf * kStageBytes;
     const uint64_t live = live_at[at];
+    // all lookups first, so that one does not wait behind another's load
+    const uint8_t *from_k[kIssues], *from_v[kIssues];
 #pragma unroll
     for (int i = 0; i < kIssues; ++i) {
       const uint64_t run = run_at[(at << step_shift) + (row_in(i) >> run_shift)] +
                            uint32_t((row_in(i) & ((1 << run_shift) - 1)) * a.slot_bytes);
-      const bool in = live >> row_in(i) & 1;
-      const uint8_t *const zero = reinterpret_cast<const uint8_t *>(kZeroRow);
-      load_row((in ? kb + run : zero) + chunk_k(i), to + i * kThreads * 16);
-      load_row((in ? vb + run : zero) + chunk_v(i), to + i * kThreads * 16 + kTile * 2);
+      from_k[i] = kb + run;
+      from_v[i] = vb + run;
+    }
+    if (live != ~uint64_t(0)) {
+#pragma unroll
+      for (int i = 0; i < kIssues; ++i)
+        if (!(live >> row_in(i) & 1))
+          from_k[i] = from_v[i] = reinterpret_cast<const uint8_t *>(kZeroRow);
+    }
+#pragma unroll
+    for (int i = 0; i < kIssues; ++i) {
+      load_row(from_k[i] + chunk_k(i), to + i * kThreads * 16);
+      load_row(from_v[i] + chunk_v(i), to + i * kThreads * 16 + kTile * 2);
     }
   };
 

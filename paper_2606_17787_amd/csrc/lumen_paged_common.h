@@ -62,6 +62,17 @@ inline int check_queries(const lumen_kv_layout *l, int32_t bt_cols, int32_t num_
   return num_reqs > LUMEN_ATTN_MAX_REQS ? LUMEN_ERR_TOO_MANY : LUMEN_OK;
 }
 
+// Starts a load of 16 bytes a lane from the lane's address into LDS at byte `to` +
+// 16 * lane, kept in caches; see load_to_lds.
+__device__ __forceinline__ void load_row(const void *from, uint32_t to) {
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+               :: "{m0}"(to), "v"(from) : "memory");
+}
+
+// Rows of places that are left out are read from here, so that what the cache
+// holds there reaches nothing.
+__device__ __attribute__((aligned(16))) const uint16_t kZeroRow[128] = {};
+
 // What a kernel of a call with queries needs of it.
 struct Call {
   Rows q;

@@ -15,24 +15,107 @@ namespace {
 
 using namespace lumen_paged_detail;
 
-constexpr int kPlaces = 64;  // of a wavefront
 constexpr int kWaves = 4, kThreads = kWaves * kWave;
 
 struct WeighArgs : Call {
   const float *lse;
-  float *weights;  // of the layer
-  int32_t chunks;  // of kWaves * kPlaces places, of a request at most
+  float *weights;   // of the layer
+  int32_t chunks;  // of a request's places at most
+  int32_t chunk;   // weigh_few_kernel: places of one
 };
 
-// A wavefront takes 64 places of a request and a KV head, holds their keys as the
-// left operand of 32x32x16 products, and goes over the query rows that see them, 32
-// at a time: scores^T = K Q^T, queries across, so that a lane has one query's lse.
-// Its weights are added up by place in 32 bits, and over the lanes at the end.
+// The sums of x[0..15] over the 32 lanes of a half: element i's in lanes i and i + 16
+// of it.  Each step after the first adds two groups of lanes up and keeps half of the
+// elements in each.
+__device__ __forceinline__ float sum_by_lane(float *x, int lane) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    float p, q;
+    both<16>(x[i], &p, &q);
+    x[i] = p + q;
+  }
+#pragma unroll
+  for (int o = 8; o; o >>= 1) {
+    const bool high = lane & o;
+#pragma unroll
+    for (int i = 0; i < o; ++i) {
+      // (copies first: a choice among elements would be one by their number)
+      const float low_one = x[i], high_one = x[i + o];
+      const float send = high ? low_one : high_one;
+      x[i] = (high ? high_one : low_one) + __shfl_xor(send, o);
+    }
+  }
+  return x[0];
+}
+
+// The place, of 32 in a product's rows, that element i of half `half` is.
+__device__ __forceinline__ int place_of(int i, int half) {
+  return i / 4 * 8 + 4 * half + i % 4;
+}
+
+// What a query's scores are lowered by, in log2: one that saw nothing (lse
+// -infinity) adds nothing.
+__device__ __forceinline__ float shift_of(float lse) {
+  return lse == -INFINITY ? INFINITY : lse * 1.44269504088896341f;
+}
+
+// Which of `count` places from place0 on a query sees that sees those up to `limit`.
+__device__ __forceinline__ uint64_t sees_to(int limit, int place0) {
+  const int to = limit - place0;
+  return to >= 63 ? ~uint64_t(0) : to < 0 ? 0 : (uint64_t(2) << to) - 1;
+}
+
+// One place's slot: where its row of the keys starts, from the layer's, and its word
+// of the ledger, for head 0; in is false where it does not count.
+struct Slot {
+  int64_t row, word;
+  bool in;
+};
+
+__device__ __forceinline__ Slot slot_of(const Call &a, int r, int place, int n, int *err) {
+  Slot s{0, 0, place < n};
+  if (s.in) {
+    const int page = int(uint32_t(place) / uint32_t(a.block_size));
+    const int64_t block = a.bt[int64_t(r) * a.bt_cols + page];
+    const int at = place - page * a.block_size;
+    s.in = block >= 0 && block < a.num_blocks;
+    if (s.in) {
+      s.row = block * a.page + int64_t(at) * a.slot_bytes;
+      s.word = block * a.kv_heads * a.block_size + at;
+    } else {
+      *err = LUMEN_ERR_BLOCK_ID;
+    }
+  }
+  return s;
+}
+
+// ------------------------------------------------- more than 32 query rows
+
+constexpr int kRows = 32;     // query rows of a tile
+constexpr int kStages = 4;    // tiles in LDS
+constexpr int kRound = 32;    // tiles whose lse is in LDS
+constexpr int kChunk = 32 * kWaves;  // places of a workgroup
+
+// A workgroup takes 128 places of a request and a KV head, a wavefront 32 of them,
+// and holds their keys as the left operand of 32x32x16 products.  The query rows that
+// see them come through LDS, 32 at a time and kStages tiles in turn, for all four
+// wavefronts: scores^T = K Q^T, queries across, so that a lane has one query's lse.
+// Its weights are added up by place in 32 bits, and over the lanes at the end.  A
+// tile's 16-byte chunks are permuted by row as attend's keys are.
 template <int D, bool kBf16>
-__global__ __launch_bounds__(kThreads, 2) void weigh_kernel(WeighArgs a) {
+__global__ __launch_bounds__(kThreads, 4) void weigh_kernel(WeighArgs a) {
+  constexpr int kChunks = D / 8;
+  constexpr int kIssues = kRows * kChunks / kThreads;
+  constexpr int kTile = kRows * D * 2;  // bytes
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[kStages * kTile];
+  __shared__ float shifts[kRound * kRows];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 31, half = lane >> 5;
+  const uint32_t lds_at = uint32_t(__builtin_amdgcn_readfirstlane(
+      int(reinterpret_cast<uintptr_t>(LDS_PTR(uint8_t, lds))) + wave * kWave * 16));
+  const auto *lds_bytes = LDS_PTR(const char, lds);
+  const uint32_t read_q = col * D * 2 + 16 * (half ^ swizzle_k<D>(col));
   const int64_t items = int64_t(a.num_reqs) * a.chunks * a.kv_heads;
   for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
     const int64_t rest = item / a.kv_heads;
@@ -41,107 +124,265 @@ __global__ __launch_bounds__(kThreads, 2) void weigh_kernel(WeighArgs a) {
     Request q;
     int err = request(a, r, &q);
     if (chunk == 0 && h == 0 && wave == 0) record_wave(a.status, err);
-    const int place0 = (chunk * kWaves + wave) * kPlaces;
+    const int first_place = chunk * kChunk, place0 = first_place + wave * 32;
     const int n = q.n < a.cap ? q.n : a.cap;
-    if (q.m == 0 || place0 >= n) continue;
-    // ---- the places: the lane's own, and the keys of two of them as fragments
-    const int place = place0 + lane;
-    int64_t block = 0;
-    int at = 0;
-    bool in = place < n;
+    if (q.m == 0 || first_place >= n) continue;
+    // ---- the rows, from the first that sees a place of the workgroup's on
+    const int behind = q.n - q.m, rows = q.m * a.group;
+    const int first = (first_place > behind ? (first_place - behind) * a.group : 0) / kRows;
+    const int tiles = (rows + kRows - 1) / kRows - first;
+    const uint16_t *const qb = a.q.base + int64_t(q.q0) * a.q.token;
+    const float *const lse = a.lse + int64_t(q.q0) * a.q_heads;
+    const auto load = [&](int tile, int stage) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < kIssues; ++i) {
+        const int in = (i * kThreads + tid) / kChunks;
+        int row = (first + tile) * kRows + in;
+        row = row < rows ? row : rows - 1;
+        const int tok = row / a.group, head = h * a.group + (row - tok * a.group);
+        load_row(qb + int64_t(tok) * a.q.token + int64_t(head) * a.q.head +
+                     8 * ((tid % kChunks) ^ swizzle_k<D>(in)),
+                 lds_at + stage * kTile + i * kThreads * 16);
+      }
+    };
     err = LUMEN_OK;
-    if (in) {
-      const int page = int(uint32_t(place) / uint32_t(a.block_size));
-      block = a.bt[int64_t(r) * a.bt_cols + page];
-      at = place - page * a.block_size;
-      in = block >= 0 && block < a.num_blocks;
-      if (!in) err = LUMEN_ERR_BLOCK_ID;
-    }
+    const Slot slot = slot_of(a, r, place0 + col, n, &err);
     record_wave(a.status, err);
-    const uint64_t live = __ballot(in);
-    if (live == 0) continue;
-    const int64_t offset = block * a.page + int64_t(at) * a.slot_bytes;
-    const uint8_t *const kb = a.k + int64_t(h) * a.head_bytes + 16 * half;
-    frag8 k[2][D / 16];
+    frag8 k[D / 16];
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const int64_t from = __shfl(offset, t * 32 + col);
-      const bool there = live >> (t * 32 + col) & 1;
+    for (int i = 0; i < D / 16; ++i) {
+      k[i] = frag8{0, 0, 0, 0, 0, 0, 0, 0};
+      if (slot.in)
+        k[i] = *reinterpret_cast<const frag8 *>(a.k + int64_t(h) * a.head_bytes + slot.row +
+                                                16 * half + 32 * i);
+    }
+    f32x16 sum;
 #pragma unroll
-      for (int i = 0; i < D / 16; ++i) {
-        k[t][i] = frag8{0, 0, 0, 0, 0, 0, 0, 0};
-        if (there) k[t][i] = *reinterpret_cast<const frag8 *>(kb + from + 32 * i);
+    for (int i = 0; i < 16; ++i) sum[i] = 0.0f;
+    for (int base = 0; base < tiles; base += kRound) {
+      const int count = tiles - base < kRound ? tiles - base : kRound;
+      __syncthreads();  // the tiles before are done with
+      for (int i = tid; i < count * kRows; i += kThreads) {
+        int row = (first + base) * kRows + i;
+        row = row < rows ? row : rows - 1;
+        const int tok = row / a.group;
+        shifts[i] = shift_of(lse[int64_t(tok) * a.q_heads + h * a.group + (row - tok * a.group)]);
+      }
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < kStages - 1; ++i)
+        if (i < count) load(base + i, i);
+      int stage = 0;
+      for (int at = 0; at < count; ++at) {
+        const int tile = base + at, after = count - 1 - at;  // tiles loaded after this one
+        if (after >= 2)
+          wait_loads<2 * kIssues>();
+        else if (after == 1)
+          wait_loads<kIssues>();
+        else
+          wait_loads<0>();
+        lds_barrier();
+        if (at + kStages - 1 < count)
+          load(tile + kStages - 1, stage ? stage - 1 : kStages - 1);
+        const int row0 = (first + tile) * kRows;
+        const uint32_t from = stage * kTile;
+        f32x16 sc;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sc[i] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i)
+          sc = mfma<kBf16>(k[i],
+                           *reinterpret_cast<const __attribute__((address_space(3))) frag8 *>(
+                               lds_bytes + ((read_q ^ (32 * i)) + from)),
+                           sc);
+        const float shift = shifts[at * kRows + col];
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          sc[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i], a.scale_log2, -shift));
+        if (row0 + kRows > rows || behind + row0 / a.group < place0 + 31) {
+          const int row = row0 + col;
+          const uint64_t sees = row < rows ? sees_to(behind + row / a.group, place0) : 0;
+          const uint32_t mine = uint32_t(sees) >> (4 * half);
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (!(mine >> (i / 4 * 8 + i % 4) & 1)) sc[i] = 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sum[i] += sc[i];
+        stage = stage + 1 < kStages ? stage + 1 : 0;
       }
     }
-    f32x16 sum[2];
+    float s[16];
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+    for (int i = 0; i < 16; ++i) s[i] = sum[i];
+    const float total = sum_by_lane(s, lane);
+    const int mine = place_of(col % 16, half);
+    const int64_t word = __shfl(slot.word, mine) + int64_t(h) * a.block_size;
+    const bool in = __shfl(int(slot.in), mine);
+    if (col < 16 && in) a.weights[word] += total;
+  }
+}
+
+// ------------------------------------------------- up to 128 query rows
+
+constexpr int kPlaces = 32 * kWaves;  // places of a step
+constexpr int kEntries = 256;         // runs of places of a workgroup
+
+// A workgroup takes a stretch of a request's places for a KV head; each wavefront
+// holds all of the request's query rows, in kTiles tiles of 32, as right operands, and
+// takes 32 of a step's 128 places.  The keys come through LDS, two steps in turn.
+// Where the places' rows start is laid out in LDS
+// before, an entry for each run of places that cannot leave its page, as attend has it.
+// Bound by the keys' bytes.
+template <int D, bool kBf16, int kTiles>
+__global__ __launch_bounds__(kThreads, kTiles == 1 || D == 64 ? 2 : 1) void weigh_few_kernel(WeighArgs a) {
+  constexpr int kChunks = D / 8;
+  constexpr int kIssues = kPlaces * kChunks / kThreads;
+  constexpr int kTile = kPlaces * D * 2;  // bytes
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * kTile];
+  __shared__ int64_t run_row[kEntries];   // bytes from the layer's keys
+  __shared__ int64_t run_word[kEntries];  // of the ledger
+  __shared__ uint64_t live_at[kEntries * 16 / 64];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int col = lane & 31, half = lane >> 5;
+  const uint32_t lds_at = uint32_t(__builtin_amdgcn_readfirstlane(
+      int(reinterpret_cast<uintptr_t>(LDS_PTR(uint8_t, lds))) + wave * kWave * 16));
+  const auto *lds_bytes = LDS_PTR(const char, lds);
+  const uint32_t read_k = (wave * 32 + col) * D * 2 + 16 * (half ^ swizzle_k<D>(col));
+  const int low = a.block_size & -a.block_size;
+  const int run_shift = low >= 16 ? 4 : __builtin_ctz(low);
+  // the lane's place of the sums
+  const int mine = wave * 32 + place_of(col % 16, half);
+  const int64_t items = int64_t(a.num_reqs) * a.chunks * a.kv_heads;
+  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+    const int64_t rest = item / a.kv_heads;
+    const int h = int(item - rest * a.kv_heads);
+    const int r = int(rest / a.chunks), chunk = int(rest - int64_t(r) * a.chunks);
+    Request q;
+    int err = request(a, r, &q);
+    if (chunk == 0 && h == 0 && wave == 0) record_wave(a.status, err);
+    const int first = chunk * a.chunk;
+    const int n = q.n < a.cap ? q.n : a.cap;
+    if (q.m == 0 || first >= n) continue;
+    const int count = n - first < a.chunk ? n - first : a.chunk;
+    const int steps = (count + kPlaces - 1) / kPlaces;
+    // ---- the queries
+    const int rows = q.m * a.group, behind = q.n - q.m;
+    frag8 x[kTiles][D / 16];
+    float shift[kTiles];
+    int limit[kTiles];  // the last place that the lane's query sees
 #pragma unroll
-      for (int i = 0; i < 16; ++i) sum[t][i] = 0.0f;
-    // ---- the rows, from the first that sees place0 on
-    const int behind = q.n - q.m, rows = q.m * a.group;
-    const int first = place0 > behind ? (place0 - behind) * a.group : 0;
-    for (int row0 = first / 32 * 32; row0 < rows; row0 += 32) {
-      const int row = row0 + col < rows ? row0 + col : rows - 1;
-      const int tok = row / a.group;
+    for (int t = 0; t < kTiles; ++t) {
+      const int at = t * kRows + col, row = at < rows ? at : rows - 1, tok = row / a.group;
       const int head = h * a.group + (row - tok * a.group);
       const uint16_t *p = a.q.base + (int64_t(q.q0) + tok) * a.q.token +
                           int64_t(head) * a.q.head + 8 * half;
-      frag8 x[D / 16];
 #pragma unroll
-      for (int i = 0; i < D / 16; ++i) x[i] = *reinterpret_cast<const frag8 *>(p + 16 * i);
-      const float lse = a.lse[(int64_t(q.q0) + tok) * a.q_heads + head];
-      // a query that saw nothing adds nothing
-      const float shift = lse == -INFINITY ? INFINITY : lse * 1.44269504088896341f;
-      f32x16 sc[2];
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) sc[t][i] = 0.0f;
-#pragma unroll
-        for (int i = 0; i < D / 16; ++i) sc[t] = mfma<kBf16>(k[t][i], x[i], sc[t]);
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          sc[t][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][i], a.scale_log2, -shift));
-      }
-      if (row0 + 31 >= rows || behind + row0 / a.group < place0 + kPlaces - 1) {
-        const int to = behind + tok - place0;
-        const uint64_t sees = row0 + col >= rows ? 0
-                              : to >= kPlaces - 1 ? ~uint64_t(0)
-                              : to < 0            ? 0
-                                                  : (uint64_t(2) << to) - 1;
-        const uint64_t mine = sees >> (4 * half);
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (!(uint32_t(mine >> (32 * t)) >> (8 * (i / 4) + i % 4) & 1)) sc[t][i] = 0.0f;
-      }
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) sum[t][i] += sc[t][i];
+      for (int i = 0; i < D / 16; ++i) x[t][i] = *reinterpret_cast<const frag8 *>(p + 16 * i);
+      shift[t] = shift_of(a.lse[(int64_t(q.q0) + tok) * a.q_heads + head]);
+      limit[t] = at < rows ? behind + tok : -1;
     }
-    // ---- over the queries' lanes: each step halves the places that a lane holds
-    float s[32];
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[16 * t + i] = sum[t][i];
-#pragma unroll
-    for (int o = 16; o; o >>= 1) {
-      const bool high = lane & o;
-#pragma unroll
-      for (int i = 0; i < o; ++i) {
-        const float send = high ? s[i] : s[i + o];
-        s[i] = (high ? s[i + o] : s[i]) + __shfl_xor(send, o);
+    // ---- where the places are
+    __syncthreads();  // the item before is done with the tables and tiles
+    err = LUMEN_OK;
+    for (int i = tid; i < steps * kPlaces; i += kThreads) {
+      const Slot s = slot_of(a, r, first + i, n, &err);
+      const uint64_t live = __ballot(s.in);
+      if (lane == 0) live_at[i / 64] = live;
+      if ((i & ((1 << run_shift) - 1)) == 0) {
+        run_row[i >> run_shift] = s.row;
+        run_word[i >> run_shift] = s.word + int64_t(h) * a.block_size;
       }
     }
-    // the lane's place: element col of the list above
-    const int mine = (col / 16) * 32 + (col % 16 / 4) * 8 + 4 * half + col % 4;
-    const int64_t word = (block * a.kv_heads + h) * a.block_size + at;
-    const int64_t to = __shfl(word, mine);
-    if (live >> mine & 1) a.weights[to] += s[0];
+    if (h == 0) record_wave(a.status, err);
+    __syncthreads();
+    const auto in_run = [&](int i) { return i & ((1 << run_shift) - 1); };
+    const uint8_t *const kb = a.k + int64_t(h) * a.head_bytes;
+    const auto load = [&](int step, int buf) __attribute__((always_inline)) {
+      const int base = step * kPlaces;
+      // all lookups first, so that one does not wait behind another's load
+      const uint8_t *from[kIssues];
+#pragma unroll
+      for (int i = 0; i < kIssues; ++i) {
+        const int place = base + (i * kThreads + tid) / kChunks;
+        from[i] = kb + run_row[place >> run_shift] + int64_t(in_run(place)) * a.slot_bytes;
+      }
+      if (live_at[base / 64] != ~uint64_t(0) || live_at[base / 64 + 1] != ~uint64_t(0)) {
+#pragma unroll
+        for (int i = 0; i < kIssues; ++i) {
+          const int place = base + (i * kThreads + tid) / kChunks;
+          if (!(live_at[place / 64] >> (place % 64) & 1))
+            from[i] = reinterpret_cast<const uint8_t *>(kZeroRow);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kIssues; ++i)
+        load_row(from[i] + 16 * ((tid % kChunks) ^ swizzle_k<D>((i * kThreads + tid) / kChunks)),
+                 lds_at + buf * kTile + i * kThreads * 16);
+    };
+    // the weight of the lane's place of the sums
+    const auto weight = [&](int step) __attribute__((always_inline)) {
+      const int place = step * kPlaces + mine;
+      float w = 0.0f;
+      if (col < 16 && live_at[place / 64] >> (place % 64) & 1)
+        w = a.weights[run_word[place >> run_shift] + in_run(place)];
+      return w;
+    };
+    // the queries are here before the first keys' loads, which the compiler does not
+    // count, so that no wait for them is left in the loop
+    __builtin_amdgcn_s_waitcnt(0x0f70);
+    float next = weight(0);
+    load(0, 0);
+    bool stored = false;  // by the wavefront, after its last loads
+    for (int step = 0; step < steps; ++step) {
+      const int buf = step & 1;
+      if (stored)
+        wait_loads<1>();
+      else
+        wait_loads<0>();
+      lds_barrier();
+      // (here, so that the compiler's wait for it is not among the next loads')
+      asm volatile("" : "+v"(next));
+      const float before = next;
+      if (step + 1 < steps) {
+        next = weight(step + 1);
+        load(step + 1, buf ^ 1);
+      }
+      const int place0 = first + step * kPlaces + wave * 32;
+      stored = false;
+      if (place0 >= n) continue;
+      frag8 k[D / 16];
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i)
+        k[i] = *reinterpret_cast<const __attribute__((address_space(3))) frag8 *>(
+            lds_bytes + ((read_k ^ (32 * i)) + buf * kTile));
+      float sum[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sum[i] = 0.0f;
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t) {
+        if (t > 0 && t * kRows >= rows) break;
+        f32x16 sc;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sc[i] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) sc = mfma<kBf16>(k[i], x[t][i], sc);
+        const uint32_t sees = uint32_t(sees_to(limit[t], place0)) >> (4 * half);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float y =
+              __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i], a.scale_log2, -shift[t]));
+          sum[i] += sees >> (i / 4 * 8 + i % 4) & 1 ? y : 0.0f;
+        }
+      }
+      const float total = sum_by_lane(sum, lane);
+      const int place = step * kPlaces + mine;
+      const bool in = col < 16 && live_at[place / 64] >> (place % 64) & 1;
+      stored = __any(in);
+      if (in)
+        a.weights[run_word[place >> run_shift] + in_run(place)] = before + total;
+    }
   }
 }
 
@@ -192,15 +433,32 @@ int lumen_paged_weigh(const lumen_kv_layout *layout, int32_t layer, const void *
               num_tokens, max_new, num_q_heads, scale, d_status);
   a.lse = d_lse;
   a.weights = static_cast<float *>(d_ledger) + 2 * layer * ledger_words(layout);
-  a.chunks = (a.cap + kWaves * kPlaces - 1) / (kWaves * kPlaces);
-  if (a.chunks < 1) a.chunks = 1;  // which looks at the requests
-  int64_t groups = int64_t(num_reqs) * a.chunks;
-  groups = groups < kMostGroups / a.kv_heads ? groups * a.kv_heads : kMostGroups;
   const bool bf = dtype == LUMEN_ATTN_BF16;
-  const auto kernel = layout->head_dim == 64 ? (bf ? weigh_kernel<64, true> : weigh_kernel<64, false>)
-                                             : (bf ? weigh_kernel<128, true> : weigh_kernel<128, false>);
-  hipLaunchKernelGGL(kernel, dim3(unsigned(groups)), dim3(kThreads), 0,
-                     static_cast<hipStream_t>(stream), a);
+  const int D = layout->head_dim;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const auto launch = [&](void (*kernel)(WeighArgs)) {
+    a.chunks = (a.cap + a.chunk - 1) / a.chunk;
+    if (a.chunks < 1) a.chunks = 1;  // which looks at the requests
+    int64_t groups = int64_t(num_reqs) * a.chunks;
+    groups = groups < kMostGroups / a.kv_heads ? groups * a.kv_heads : kMostGroups;
+    hipLaunchKernelGGL(kernel, dim3(unsigned(groups)), dim3(kThreads), 0, s, a);
+  };
+  const int64_t rows = int64_t(max_new) * a.group;
+  if (rows <= 4 * kRows) {
+    const int low = a.block_size & -a.block_size;
+    a.chunk = kEntries * (low < 16 ? low : 16);
+    if (a.chunk > 1024) a.chunk = 1024;
+    if (rows <= kRows)
+      launch(D == 64 ? (bf ? weigh_few_kernel<64, true, 1> : weigh_few_kernel<64, false, 1>)
+                     : (bf ? weigh_few_kernel<128, true, 1> : weigh_few_kernel<128, false, 1>));
+    else
+      launch(D == 64 ? (bf ? weigh_few_kernel<64, true, 4> : weigh_few_kernel<64, false, 4>)
+                     : (bf ? weigh_few_kernel<128, true, 4> : weigh_few_kernel<128, false, 4>));
+  } else {
+    a.chunk = kChunk;
+    launch(D == 64 ? (bf ? weigh_kernel<64, true> : weigh_kernel<64, false>)
+                   : (bf ? weigh_kernel<128, true> : weigh_kernel<128, false>));
+  }
   return hipGetLastError() == hipSuccess ? LUMEN_OK : LUMEN_ERR_HIP;
 }
 
