@@ -225,35 +225,67 @@ __global__ __launch_bounds__(kThreads, 4) void weigh_kernel(WeighArgs a) {
 
 // ------------------------------------------------- up to 128 query rows
 
-constexpr int kPlaces = 32 * kWaves;  // places of a step
+constexpr int kPlaces = 16 * kWaves;  // places of a step
 constexpr int kEntries = 256;         // runs of places of a workgroup
+constexpr int kMostPlaces16 = 1024;   // places of a workgroup
+
+// The sum over a row of 16 lanes of s[i], for element i of 4 in the lanes with
+// lane / 4 % 4 = i: two steps add mirrored lanes up and keep half of the elements in
+// each, two more add what four lanes hold.
+template <int kControl>
+__device__ __forceinline__ float mirrored(float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(
+                                       0, __builtin_bit_cast(int, x), kControl, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float sum_of_four(const float *s, int lane) {
+  const bool upper = lane & 8, odd = lane & 4;
+  const float s0 = s[0], s1 = s[1], s2 = s[2], s3 = s[3];
+  const float a = (upper ? s2 : s0) + mirrored<0x140>(upper ? s0 : s2);
+  const float b = (upper ? s3 : s1) + mirrored<0x140>(upper ? s1 : s3);
+  float c = (odd ? b : a) + mirrored<0x141>(odd ? a : b);
+  c += mirrored<0x4e>(c);
+  return c + mirrored<0xb1>(c);
+}
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+template <bool kBf16>
+__device__ __forceinline__ f32x4 mfma16(frag8 a, frag8 b, f32x4 c) {
+  if constexpr (kBf16)
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+        __builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(
+        __builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
 
 // A workgroup takes a stretch of a request's places for a KV head; each wavefront
-// holds all of the request's query rows, in kTiles tiles of 32, as right operands, and
-// takes 32 of a step's 128 places.  The keys come through LDS, two steps in turn.
-// Where the places' rows start is laid out in LDS
-// before, an entry for each run of places that cannot leave its page, as attend has it.
-// Bound by the keys' bytes.
+// holds all of the request's query rows, in kTiles tiles of 16, as right operands of
+// 16x16x32 products, and takes 16 of a step's 64 places.  The keys come through LDS,
+// kStages steps in turn.  Where the places' rows start is laid out in LDS before, an
+// entry for each run of places that cannot leave its page, as attend has it, and so are
+// the weights that the places have; they are written back at the end.  Bound by the
+// keys' bytes.
 template <int D, bool kBf16, int kTiles>
-__global__ __launch_bounds__(kThreads, kTiles == 1 || D == 64 ? 2 : 1) void weigh_few_kernel(WeighArgs a) {
+__global__ __launch_bounds__(kThreads, 2) void weigh_few_kernel(WeighArgs a) {
   constexpr int kChunks = D / 8;
   constexpr int kIssues = kPlaces * kChunks / kThreads;
   constexpr int kTile = kPlaces * D * 2;  // bytes
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * kTile];
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[kStages * kTile];
+  __shared__ float weights[kMostPlaces16];
   __shared__ int64_t run_row[kEntries];   // bytes from the layer's keys
   __shared__ int64_t run_word[kEntries];  // of the ledger
-  __shared__ uint64_t live_at[kEntries * 16 / 64];
+  __shared__ uint64_t live_at[kMostPlaces16 / 64];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int col = lane & 31, half = lane >> 5;
+  const int col = lane & 15, quad = lane >> 4;
   const uint32_t lds_at = uint32_t(__builtin_amdgcn_readfirstlane(
       int(reinterpret_cast<uintptr_t>(LDS_PTR(uint8_t, lds))) + wave * kWave * 16));
   const auto *lds_bytes = LDS_PTR(const char, lds);
-  const uint32_t read_k = (wave * 32 + col) * D * 2 + 16 * (half ^ swizzle_k<D>(col));
+  const int my_row = wave * 16 + col;
+  const uint32_t read_k = my_row * D * 2 + 16 * (quad ^ swizzle_k<D>(my_row));
   const int low = a.block_size & -a.block_size;
   const int run_shift = low >= 16 ? 4 : __builtin_ctz(low);
-  // the lane's place of the sums
-  const int mine = wave * 32 + place_of(col % 16, half);
+  const auto in_run = [&](int i) { return i & ((1 << run_shift) - 1); };
   const int64_t items = int64_t(a.num_reqs) * a.chunks * a.kv_heads;
   for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
     const int64_t rest = item / a.kv_heads;
@@ -267,123 +299,114 @@ __global__ __launch_bounds__(kThreads, kTiles == 1 || D == 64 ? 2 : 1) void weig
     if (q.m == 0 || first >= n) continue;
     const int count = n - first < a.chunk ? n - first : a.chunk;
     const int steps = (count + kPlaces - 1) / kPlaces;
-    // ---- the queries
-    const int rows = q.m * a.group, behind = q.n - q.m;
-    frag8 x[kTiles][D / 16];
-    float shift[kTiles];
-    int limit[kTiles];  // the last place that the lane's query sees
-#pragma unroll
-    for (int t = 0; t < kTiles; ++t) {
-      const int at = t * kRows + col, row = at < rows ? at : rows - 1, tok = row / a.group;
-      const int head = h * a.group + (row - tok * a.group);
-      const uint16_t *p = a.q.base + (int64_t(q.q0) + tok) * a.q.token +
-                          int64_t(head) * a.q.head + 8 * half;
-#pragma unroll
-      for (int i = 0; i < D / 16; ++i) x[t][i] = *reinterpret_cast<const frag8 *>(p + 16 * i);
-      shift[t] = shift_of(a.lse[(int64_t(q.q0) + tok) * a.q_heads + head]);
-      limit[t] = at < rows ? behind + tok : -1;
-    }
-    // ---- where the places are
+    // ---- where the places are, and what they weigh
     __syncthreads();  // the item before is done with the tables and tiles
     err = LUMEN_OK;
     for (int i = tid; i < steps * kPlaces; i += kThreads) {
       const Slot s = slot_of(a, r, first + i, n, &err);
       const uint64_t live = __ballot(s.in);
       if (lane == 0) live_at[i / 64] = live;
-      if ((i & ((1 << run_shift) - 1)) == 0) {
+      const int64_t word = s.word + int64_t(h) * a.block_size;
+      if (in_run(i) == 0) {
         run_row[i >> run_shift] = s.row;
-        run_word[i >> run_shift] = s.word + int64_t(h) * a.block_size;
+        run_word[i >> run_shift] = word;
       }
+      weights[i] = s.in ? a.weights[word] : 0.0f;
     }
     if (h == 0) record_wave(a.status, err);
+    // ---- the queries
+    const int rows = q.m * a.group, behind = q.n - q.m;
+    frag8 x[kTiles][D / 32];
+    float shift[kTiles];
+    int limit[kTiles];  // the last place that the lane's query sees
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+      const int at = t * 16 + col, row = at < rows ? at : rows - 1, tok = row / a.group;
+      const int head = h * a.group + (row - tok * a.group);
+      const uint16_t *p = a.q.base + (int64_t(q.q0) + tok) * a.q.token +
+                          int64_t(head) * a.q.head + 8 * quad;
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i) x[t][i] = *reinterpret_cast<const frag8 *>(p + 32 * i);
+      shift[t] = shift_of(a.lse[(int64_t(q.q0) + tok) * a.q_heads + head]);
+      limit[t] = at < rows ? behind + tok : -1;
+    }
     __syncthreads();
-    const auto in_run = [&](int i) { return i & ((1 << run_shift) - 1); };
     const uint8_t *const kb = a.k + int64_t(h) * a.head_bytes;
     const auto load = [&](int step, int buf) __attribute__((always_inline)) {
       const int base = step * kPlaces;
       // all lookups first, so that one does not wait behind another's load
       const uint8_t *from[kIssues];
+      const uint64_t live = live_at[step];
 #pragma unroll
       for (int i = 0; i < kIssues; ++i) {
         const int place = base + (i * kThreads + tid) / kChunks;
         from[i] = kb + run_row[place >> run_shift] + int64_t(in_run(place)) * a.slot_bytes;
       }
-      if (live_at[base / 64] != ~uint64_t(0) || live_at[base / 64 + 1] != ~uint64_t(0)) {
+      if (live != ~uint64_t(0)) {
 #pragma unroll
-        for (int i = 0; i < kIssues; ++i) {
-          const int place = base + (i * kThreads + tid) / kChunks;
-          if (!(live_at[place / 64] >> (place % 64) & 1))
+        for (int i = 0; i < kIssues; ++i)
+          if (!(live >> ((i * kThreads + tid) / kChunks) & 1))
             from[i] = reinterpret_cast<const uint8_t *>(kZeroRow);
-        }
       }
 #pragma unroll
       for (int i = 0; i < kIssues; ++i)
         load_row(from[i] + 16 * ((tid % kChunks) ^ swizzle_k<D>((i * kThreads + tid) / kChunks)),
                  lds_at + buf * kTile + i * kThreads * 16);
     };
-    // the weight of the lane's place of the sums
-    const auto weight = [&](int step) __attribute__((always_inline)) {
-      const int place = step * kPlaces + mine;
-      float w = 0.0f;
-      if (col < 16 && live_at[place / 64] >> (place % 64) & 1)
-        w = a.weights[run_word[place >> run_shift] + in_run(place)];
-      return w;
-    };
     // the queries are here before the first keys' loads, which the compiler does not
     // count, so that no wait for them is left in the loop
     __builtin_amdgcn_s_waitcnt(0x0f70);
-    float next = weight(0);
-    load(0, 0);
-    bool stored = false;  // by the wavefront, after its last loads
+#pragma unroll
+    for (int i = 0; i < kStages - 1; ++i)
+      if (i < steps) load(i, i);
+    int buf = 0;
     for (int step = 0; step < steps; ++step) {
-      const int buf = step & 1;
-      if (stored)
-        wait_loads<1>();
+      const int after = steps - 1 - step;  // steps loaded after this one
+      if (after >= 2)
+        wait_loads<2 * kIssues>();
+      else if (after == 1)
+        wait_loads<kIssues>();
       else
         wait_loads<0>();
       lds_barrier();
-      // (here, so that the compiler's wait for it is not among the next loads')
-      asm volatile("" : "+v"(next));
-      const float before = next;
-      if (step + 1 < steps) {
-        next = weight(step + 1);
-        load(step + 1, buf ^ 1);
-      }
-      const int place0 = first + step * kPlaces + wave * 32;
-      stored = false;
-      if (place0 >= n) continue;
-      frag8 k[D / 16];
+      if (step + kStages - 1 < steps) load(step + kStages - 1, buf ? buf - 1 : kStages - 1);
+      const int place0 = first + step * kPlaces + wave * 16;
+      frag8 k[D / 32];
 #pragma unroll
-      for (int i = 0; i < D / 16; ++i)
+      for (int i = 0; i < D / 32; ++i)
         k[i] = *reinterpret_cast<const __attribute__((address_space(3))) frag8 *>(
-            lds_bytes + ((read_k ^ (32 * i)) + buf * kTile));
-      float sum[16];
-#pragma unroll
-      for (int i = 0; i < 16; ++i) sum[i] = 0.0f;
+            lds_bytes + ((read_k ^ (64 * i)) + buf * kTile));
+      float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int t = 0; t < kTiles; ++t) {
-        if (t > 0 && t * kRows >= rows) break;
-        f32x16 sc;
+        if (t > 0 && t * 16 >= rows) break;
+        f32x4 sc = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int i = 0; i < 16; ++i) sc[i] = 0.0f;
+        for (int i = 0; i < D / 32; ++i) sc = mfma16<kBf16>(k[i], x[t][i], sc);
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i) sc = mfma<kBf16>(k[i], x[t][i], sc);
-        const uint32_t sees = uint32_t(sees_to(limit[t], place0)) >> (4 * half);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
+        for (int i = 0; i < 4; ++i) {
           const float y =
               __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i], a.scale_log2, -shift[t]));
-          sum[i] += sees >> (i / 4 * 8 + i % 4) & 1 ? y : 0.0f;
+          sum[i] += place0 + 4 * quad + i <= limit[t] ? y : 0.0f;
         }
       }
-      const float total = sum_by_lane(sum, lane);
-      const int place = step * kPlaces + mine;
-      const bool in = col < 16 && live_at[place / 64] >> (place % 64) & 1;
-      stored = __any(in);
-      if (in)
-        a.weights[run_word[place >> run_shift] + in_run(place)] = before + total;
+      const float total = sum_of_four(sum, lane);
+      if (lane % 4 == 0)
+        weights[step * kPlaces + wave * 16 + 4 * quad + lane / 4 % 4] += total;
+      buf = buf + 1 < kStages ? buf + 1 : 0;
     }
+    __syncthreads();
+    for (int i = tid; i < count; i += kThreads)
+      if (live_at[i / 64] >> (i % 64) & 1)
+        a.weights[run_word[i >> run_shift] + in_run(i)] = weights[i];
   }
+}
+
+template <int kTiles>
+void (*few_kernel(int head_dim, bool bf16))(WeighArgs) {
+  if (head_dim == 64)
+    return bf16 ? weigh_few_kernel<64, true, kTiles> : weigh_few_kernel<64, false, kTiles>;
+  return bf16 ? weigh_few_kernel<128, true, kTiles> : weigh_few_kernel<128, false, kTiles>;
 }
 
 // Workgroups of a launch at most: more than run at once, and few enough that their
@@ -444,16 +467,15 @@ int lumen_paged_weigh(const lumen_kv_layout *layout, int32_t layer, const void *
     hipLaunchKernelGGL(kernel, dim3(unsigned(groups)), dim3(kThreads), 0, s, a);
   };
   const int64_t rows = int64_t(max_new) * a.group;
-  if (rows <= 4 * kRows) {
+  if (rows <= 128) {
     const int low = a.block_size & -a.block_size;
     a.chunk = kEntries * (low < 16 ? low : 16);
-    if (a.chunk > 1024) a.chunk = 1024;
-    if (rows <= kRows)
-      launch(D == 64 ? (bf ? weigh_few_kernel<64, true, 1> : weigh_few_kernel<64, false, 1>)
-                     : (bf ? weigh_few_kernel<128, true, 1> : weigh_few_kernel<128, false, 1>));
-    else
-      launch(D == 64 ? (bf ? weigh_few_kernel<64, true, 4> : weigh_few_kernel<64, false, 4>)
-                     : (bf ? weigh_few_kernel<128, true, 4> : weigh_few_kernel<128, false, 4>));
+#ifdef CH
+    if (a.chunk > CH) a.chunk = CH;
+#endif
+    if (a.chunk > kMostPlaces16) a.chunk = kMostPlaces16;
+    launch(rows <= 16 ? few_kernel<1>(D, bf) : rows <= 64 ? few_kernel<4>(D, bf)
+                                                          : few_kernel<8>(D, bf));
   } else {
     a.chunk = kChunk;
     launch(D == 64 ? (bf ? weigh_kernel<64, true> : weigh_kernel<64, false>)
