@@ -82,6 +82,7 @@ struct EvictArgs {
   int64_t words;      // of a layer's weights
   int32_t slot_bytes, head_bytes;
   int32_t block_size, heads;
+  Divisor by_block;  // block_size
   int64_t num_blocks;
   const int32_t *bt;
   int32_t bt_cols;
@@ -94,8 +95,7 @@ struct EvictArgs {
   int32_t *moves;
   uint64_t *kept;
   uint32_t *before;
-  int32_t strips;    // 64 places each, of a request at most
-  int32_t lds_keys;  // ranks that fit the workgroup's LDS
+  int32_t strips;  // 64 places each, of a request at most
 };
 
 __device__ __forceinline__ bool protects(int32_t pos, int32_t sinks, int32_t from) {
@@ -121,19 +121,27 @@ __device__ __forceinline__ Item item_of(const EvictArgs &a, int64_t i) {
   return Item{layer, int(lr - int64_t(layer) * a.num_reqs), int(i - lr * a.heads)};
 }
 
-// Which places of one layer, request and head are kept.  Protected places are counted
-// first: where they do not fill the budget, all of them are kept and the others are
-// ranked, where they do, they are ranked alone.  The rank of the last one kept comes
-// out of four counts over the ranks' bytes, from the highest on; the places of a
-// wavefront's own stretch are then counted and written with what the wavefronts before
-// it have.
-template <int kThreads>
+// What a workgroup does for one layer, request and head: which places are kept.
+//
+// Protected places are counted first: where they do not fill the budget, all of them
+// are kept and the others are ranked, where they do, they are ranked alone.  The rank
+// of the last one kept comes out of counts over the ranks' digits of 11 bits, from the
+// highest on, until every rank left is kept; which places are kept, and how many are
+// before them, then goes to the workspace by strips of 64 places.
+//
+// A thread holds the ranks of kPer places, one of each kThreads, for requests of up to
+// kThreads * kPer; where kPer is 0 (longer ones), each pass reads them again.
+constexpr int kDigit = 11, kBins = 1 << kDigit;
+
+template <int kThreads, int kPer>
 __global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictArgs a) {
   constexpr int kWaves = kThreads / kWave;
-  extern __shared__ uint32_t ranks[];
-  __shared__ uint32_t hist[256];
+  constexpr int kOwn = kBins / kThreads;  // bins of a thread
+  constexpr int kMostStrips = kPer ? kPer * kWaves : 1;
+  __shared__ uint32_t hist[kBins];
   __shared__ uint32_t wave_a[kWaves], wave_b[kWaves];
-  __shared__ uint32_t digit, above;
+  __shared__ uint32_t strip_more[kMostStrips], strip_same[kMostStrips];
+  __shared__ uint32_t digit, above, inside;
   __shared__ int guarded;
   const int64_t id = blockIdx.x;
   const Item it = item_of(a, id);
@@ -145,11 +153,60 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictArgs a) {
   bool alone = n < 0 || keep < 0 || int64_t(n) > int64_t(a.bt_cols) * a.block_size;
   if (alone) err = LUMEN_ERR_RANGE;
   const int32_t *table = a.bt + int64_t(it.r) * a.bt_cols;
+  const int32_t from = a.from[it.r];
+  const uint32_t *weights = a.ledger + int64_t(it.layer) * 2 * a.words +
+                            int64_t(it.h) * a.block_size;
+  const int64_t block_words = int64_t(a.heads) * a.block_size;
+  const auto page_of = [&](int i) __attribute__((always_inline)) {
+    return quotient(a.by_block, i);
+  };
+  const auto word_of = [&](int i, int page, int32_t block) __attribute__((always_inline)) {
+    return block * block_words + (i - page * a.block_size);
+  };
+  // ---- the weights and positions, and how many places are protected
+  uint32_t held[kPer ? kPer : 1];
+  bool guard[kPer ? kPer : 1];
+  int mine = 0;
   if (!alone && n > keep) {
-    const int pages = (n - 1) / a.block_size + 1;
-    int bad = 0;
-    for (int p = tid; p < pages; p += kThreads)
-      bad |= table[p] < 0 || table[p] >= a.num_blocks;
+    bool bad = a.num_blocks == 0;
+    if constexpr (kPer > 0) {
+      if (!bad) {
+        constexpr int kAtOnce = 4;
+#pragma unroll
+        for (int g = 0; g < kPer; g += kAtOnce) {
+          if (g * kThreads >= n) break;
+          int32_t block[kAtOnce], page[kAtOnce];
+          uint32_t w[kAtOnce];
+          int32_t pos[kAtOnce];
+#pragma unroll
+          for (int j = 0; j < kAtOnce; ++j) {
+            const int i = (g + j) * kThreads + tid, place = i < n ? i : n - 1;
+            page[j] = page_of(place);
+            block[j] = table[page[j]];
+          }
+#pragma unroll
+          for (int j = 0; j < kAtOnce; ++j) {
+            const int i = (g + j) * kThreads + tid, place = i < n ? i : n - 1;
+            const bool out = block[j] < 0 || block[j] >= a.num_blocks;
+            bad |= out;
+            const int64_t word = word_of(place, page[j], out ? 0 : block[j]);
+            w[j] = weights[word];
+            pos[j] = int32_t(weights[word + a.words]);
+          }
+#pragma unroll
+          for (int j = 0; j < kAtOnce; ++j) {
+            const int i = (g + j) * kThreads + tid;
+            guard[g + j] = protects(pos[j], a.sinks, from);
+            held[g + j] = rank_of(w[j]);
+            mine += i < n && guard[g + j];
+          }
+        }
+      }
+    } else {
+      const int pages = (n - 1) / a.block_size + 1;
+      for (int p = tid; p < pages; p += kThreads)
+        bad |= table[p] < 0 || table[p] >= a.num_blocks;
+    }
     if (__syncthreads_or(bad)) {
       alone = true;
       err = LUMEN_ERR_BLOCK_ID;
@@ -163,104 +220,161 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictArgs a) {
     if (tid == 0) a.moves[id] = 0;
     return;
   }
-  const int32_t from = a.from[it.r];
-  const uint32_t *weights = a.ledger + int64_t(it.layer) * 2 * a.words +
-                            int64_t(it.h) * a.block_size;
-  const auto word_of = [&](int i) __attribute__((always_inline)) {
-    const int page = int(uint32_t(i) / uint32_t(a.block_size));
-    return int64_t(table[page]) * a.heads * a.block_size + (i - page * a.block_size);
-  };
-  // the protected places are kept, or the ones kept are all among them
-  int mine = 0;
-  for (int i = tid; i < n; i += kThreads)
-    mine += protects(int32_t(weights[word_of(i) + a.words]), a.sinks, from);
+  if constexpr (kPer == 0)
+    for (int i = tid; i < n; i += kThreads)
+      mine += protects(int32_t(weights[word_of(i, page_of(i), table[page_of(i)]) + a.words]),
+                       a.sinks, from);
   if (tid == 0) guarded = 0;
   __syncthreads();
   for (int o = 1; o < kWave; o <<= 1) mine += __shfl_xor(mine, o);
   if (lane == 0) atomicAdd(&guarded, mine);
   __syncthreads();
   const bool among = guarded >= keep;
-  const auto rank_at = [&](int i) __attribute__((always_inline)) {
-    const int64_t word = word_of(i);
-    const bool guard = protects(int32_t(weights[word + a.words]), a.sinks, from);
-    if (guard != among) return guard ? kAllRanks : kNoRank;
-    return rank_of(weights[word]);
-  };
-  const bool held = n <= a.lds_keys;
-  if (held)
-    for (int i = tid; i < n; i += kThreads) ranks[i] = rank_at(i);
-  const auto rank = [&](int i) __attribute__((always_inline)) {
-    return held ? ranks[i] : rank_at(i);
-  };
-  uint32_t last = 0, mask = 0, want = uint32_t(keep);
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    for (int i = tid; i < 256; i += kThreads) hist[i] = 0;
-    __syncthreads();
-    for (int i = tid; i < n; i += kThreads) {
-      const uint32_t x = rank(i);
-      if ((x & mask) == last) atomicAdd(&hist[x >> shift & 255], 1u);
-    }
-    __syncthreads();
-    if (wave == 0) {  // four digits a lane, the highest first
-      uint32_t c[4], sum = 0;
-      for (int j = 0; j < 4; ++j) sum += c[j] = hist[255 - (4 * lane + j)];
-      uint32_t upto = sum;
-      for (int o = 1; o < kWave; o <<= 1) {
-        const uint32_t x = __shfl_up(upto, o);
-        if (lane >= o) upto += x;
-      }
-      uint32_t over = upto - sum;
-      if (over < want && want <= upto)
-        for (int j = 0; j < 4; ++j) {
-          if (want <= over + c[j]) {
-            digit = 255 - (4 * lane + j);
-            above = over;
-            break;
-          }
-          over += c[j];
+  if constexpr (kPer > 0) {
+#pragma unroll
+    for (int j = 0; j < kPer; ++j)
+      if (guard[j] != among) held[j] = guard[j] ? kAllRanks : kNoRank;
+  }
+  // calls f(i, rank, j) for the thread's places i: j of each kThreads
+  const auto each = [&](const auto &f) __attribute__((always_inline)) {
+    if constexpr (kPer > 0) {
+#pragma unroll
+      for (int j = 0; j < kPer; ++j)
+        if (j * kThreads < n) f(j * kThreads + tid, held[j], j);
+    } else {
+      for (int j = 0; j * kThreads < n; ++j) {
+        const int i = j * kThreads + tid;
+        uint32_t rank = kNoRank;
+        if (i < n) {
+          const int64_t word = word_of(i, page_of(i), table[page_of(i)]);
+          const bool g = protects(int32_t(weights[word + a.words]), a.sinks, from);
+          rank = g != among ? (g ? kAllRanks : kNoRank) : rank_of(weights[word]);
         }
+        f(i, rank, j);
+      }
+    }
+  };
+  // ---- the rank of the last place kept
+  uint32_t last = 0, mask = 0, want = uint32_t(keep);
+  for (int shift = 32 - kDigit; mask != 0xffffffffu; shift -= kDigit) {
+    const int low = shift > 0 ? shift : 0;  // the last digit has 10 bits
+    const uint32_t digits = (mask ? ~mask : 0xffffffffu) >> low;
+#pragma unroll
+    for (int b = 0; b < kOwn; ++b) hist[b * kThreads + tid] = 0;
+    __syncthreads();
+    each([&](int i, uint32_t x, int) __attribute__((always_inline)) {
+      if (i < n && (x & mask) == last) atomicAdd(&hist[x >> low & digits], 1u);
+    });
+    __syncthreads();
+    // the thread's bins, the highest first
+    uint32_t c[kOwn], sum = 0;
+#pragma unroll
+    for (int b = 0; b < kOwn; ++b) sum += c[b] = hist[kBins - 1 - (kOwn * tid + b)];
+    uint32_t upto = sum;
+    for (int o = 1; o < kWave; o <<= 1) {
+      const uint32_t x = __shfl_up(upto, o);
+      if (lane >= o) upto += x;
+    }
+    if (lane == kWave - 1) wave_a[wave] = upto;
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) upto += wave_a[w];
+    uint32_t over = upto - sum;
+    if (over < want && want <= upto) {
+#pragma unroll
+      for (int b = 0; b < kOwn; ++b) {
+        if (over < want && want <= over + c[b]) {
+          digit = kBins - 1 - (kOwn * tid + b);
+          above = over;
+          inside = c[b];
+        }
+        over += c[b];
+      }
     }
     __syncthreads();
-    last |= digit << shift;
-    mask |= 255u << shift;
+    last |= digit << low;
+    mask |= digits << low;
     want -= above;
+    if (inside == want) break;  // all that are left are kept
   }
-  // every place above `last` is kept, and the first `want` of those at it
+  // ---- every place above `last` is kept, and the first `want` of those at it
   const int strips = (n + kWave - 1) / kWave;
-  const int per = (strips + kWaves - 1) / kWaves;
-  const int s0 = wave * per < strips ? wave * per : strips;
-  const int s1 = s0 + per < strips ? s0 + per : strips;
-  uint32_t more = 0, same = 0;
-  for (int s = s0; s < s1; ++s) {
-    const int i = s * kWave + lane;
-    const uint32_t x = i < n ? rank(i) : 0;
-    more += __popcll(__ballot(i < n && x > last));
-    same += __popcll(__ballot(i < n && x == last));
-  }
-  if (lane == 0) wave_a[wave] = more, wave_b[wave] = same;
-  __syncthreads();
-  uint32_t kept_before = 0, same_before = 0;
-  for (int w = 0; w < wave; ++w) {
-    const uint32_t room = want > same_before ? want - same_before : 0;
-    kept_before += wave_a[w] + (wave_b[w] < room ? wave_b[w] : room);
-    same_before += wave_b[w];
-  }
   uint64_t *kept = a.kept + id * a.strips;
   uint32_t *before = a.before + id * a.strips;
-  for (int s = s0; s < s1; ++s) {
-    const int i = s * kWave + lane;
-    const uint32_t x = i < n ? rank(i) : 0;
-    const uint64_t at = __ballot(i < n && x == last);
-    const uint32_t nth = same_before + __popcll(at & ((uint64_t(1) << lane) - 1));
-    const uint64_t bits = __ballot(i < n && (x > last || (x == last && nth < want)));
+  const auto kept_of = [&](int s, uint64_t more, uint64_t same, uint32_t kept_before,
+                           uint32_t same_before) __attribute__((always_inline)) {
+    const uint32_t nth = same_before + __popcll(same & ((uint64_t(1) << lane) - 1));
+    const uint64_t bits = more | __ballot((same >> lane & 1) && nth < want);
     if (lane == 0) {
       kept[s] = bits;
       before[s] = kept_before;
       if (s == keep / kWave)
-        a.moves[id] = keep - int(kept_before + __popcll(bits & ((uint64_t(1) << keep % kWave) - 1)));
+        a.moves[id] =
+            keep - int(kept_before + __popcll(bits & ((uint64_t(1) << keep % kWave) - 1)));
     }
-    kept_before += __popcll(bits);
-    same_before += __popcll(at);
+    return bits;
+  };
+  if constexpr (kPer > 0) {
+    // strip j * kWaves + wave is the wavefront's j-th
+    each([&](int i, uint32_t x, int j) __attribute__((always_inline)) {
+      const uint64_t more = __ballot(i < n && (x & mask) > last);
+      const uint64_t same = __ballot(i < n && (x & mask) == last);
+      if (lane == 0) {
+        strip_more[j * kWaves + wave] = __popcll(more);
+        strip_same[j * kWaves + wave] = __popcll(same);
+      }
+    });
+    __syncthreads();
+    if (wave == 0) {  // what is before each strip
+      uint32_t kept_before = 0, same_before = 0;
+      for (int base = 0; base < strips; base += kWave) {
+        const int s = base + lane;
+        const uint32_t m = s < strips ? strip_more[s] : 0, e = s < strips ? strip_same[s] : 0;
+        uint32_t same_to = e;
+        for (int o = 1; o < kWave; o <<= 1) {
+          const uint32_t x = __shfl_up(same_to, o);
+          if (lane >= o) same_to += x;
+        }
+        const uint32_t b = same_before + same_to - e, room = want > b ? want - b : 0;
+        const uint32_t k = m + (e < room ? e : room);
+        uint32_t kept_to = k;
+        for (int o = 1; o < kWave; o <<= 1) {
+          const uint32_t x = __shfl_up(kept_to, o);
+          if (lane >= o) kept_to += x;
+        }
+        if (s < strips) strip_more[s] = kept_before + kept_to - k, strip_same[s] = b;
+        kept_before += __shfl(kept_to, kWave - 1);
+        same_before += __shfl(same_to, kWave - 1);
+      }
+    }
+    __syncthreads();
+    each([&](int i, uint32_t x, int j) __attribute__((always_inline)) {
+      const int s = j * kWaves + wave;
+      const uint64_t more = __ballot(i < n && (x & mask) > last);
+      const uint64_t same = __ballot(i < n && (x & mask) == last);
+      if (s < strips) kept_of(s, more, same, strip_more[s], strip_same[s]);
+    });
+  } else {
+    // a pass over the strips in order, kWaves at a time
+    uint32_t kept_before = 0, same_before = 0;
+    each([&](int i, uint32_t x, int j) __attribute__((always_inline)) {
+      const uint64_t more = __ballot(i < n && (x & mask) > last);
+      const uint64_t same = __ballot(i < n && (x & mask) == last);
+      __syncthreads();
+      if (lane == 0) wave_a[wave] = __popcll(more), wave_b[wave] = __popcll(same);
+      __syncthreads();
+      uint32_t k = kept_before, e = same_before;
+      for (int w = 0; w < kWaves; ++w) {
+        if (w == wave) {
+          const int s = j * kWaves + wave;
+          if (s < strips) kept_of(s, more, same, k, e);
+        }
+        const uint32_t room = want > e ? want - e : 0;
+        k += wave_a[w] + (wave_b[w] < room ? wave_b[w] : room);
+        e += wave_b[w];
+      }
+      kept_before = k;
+      same_before = e;
+    });
   }
 }
 
@@ -333,9 +447,8 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a, i
     int src = lo * kWave + nth_bit(kept[lo], inside + nth - before[lo]);
     src = src < n ? src : n - 1;
     const auto bytes = [&](int place, int64_t *word) __attribute__((always_inline)) {
-      const int page = int(uint32_t(place) / uint32_t(a.block_size));
-      const int at = place - page * a.block_size;
-      const int64_t block = table[page];
+      int at;
+      const int64_t block = table[quotient(a.by_block, place, &at)];
       *word = block * a.heads * a.block_size + at;
       return block * a.page + int64_t(at) * a.slot_bytes;
     };
@@ -595,6 +708,7 @@ int lumen_paged_evict(const lumen_kv_layout *layout, int32_t first_layer, int32_
   a.slot_bytes = p.slot;
   a.head_bytes = p.head;
   a.block_size = layout->block_size;
+  a.by_block = divisor(a.block_size);
   a.heads = layout->num_kv_heads;
   a.num_blocks = layout->num_blocks;
   a.bt = d_block_tables;
@@ -613,15 +727,20 @@ int lumen_paged_evict(const lumen_kv_layout *layout, int32_t first_layer, int32_
   a.strips = plan.strips;
   const int64_t cap = int64_t(bt_cols) * layout->block_size;
   const int64_t items = int64_t(num_layers) * num_reqs * a.heads;
-  constexpr int kMost = 14336;  // ranks in 56 of a workgroup's 64 KB of LDS
-  a.lds_keys = int32_t(cap < kMost ? cap : kMost);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (cap <= 4096)
-    hipLaunchKernelGGL(evict_select_kernel<256>, dim3(unsigned(items)), dim3(256),
-                       size_t(a.lds_keys) * 4, s, a);
+  const auto select = [&](void (*kernel)(EvictArgs), int threads) {
+    hipLaunchKernelGGL(kernel, dim3(unsigned(items)), dim3(unsigned(threads)), 0, s, a);
+  };
+  if (cap <= 256 * 8)
+    select(evict_select_kernel<256, 8>, 256);
+  else if (cap <= 256 * 16)
+    select(evict_select_kernel<256, 16>, 256);
+  else if (cap <= 1024 * 8)
+    select(evict_select_kernel<1024, 8>, 1024);
+  else if (cap <= 1024 * 32)
+    select(evict_select_kernel<1024, 32>, 1024);
   else
-    hipLaunchKernelGGL(evict_select_kernel<1024>, dim3(unsigned(items)), dim3(1024),
-                       size_t(a.lds_keys) * 4, s, a);
+    select(evict_select_kernel<1024, 0>, 1024);
   // a wavefront for 64 moves, of which a request has at most half its places
   int64_t parts = (cap / 2 + kMoveThreads - 1) / kMoveThreads;
   if (parts > 64) parts = 64;
@@ -655,10 +774,9 @@ int lumen_paged_release(const int32_t *d_lens, const int32_t *d_have, int32_t nu
   (void)hipGetLastError();
   const ReleaseArgs a{d_lens,  d_have,       num_reqs, d_block_tables, bt_cols,    block_size,
                       num_blocks, d_free, d_free_count, free_cap,       d_free_now, d_status};
-  // a thread a page, on a workgroup for 16 requests at most: each scans all of them
+  // a thread a page; each workgroup scans all requests
   const int64_t pages = int64_t(num_reqs) * bt_cols;
   int64_t blocks = (pages + kReleaseThreads - 1) / kReleaseThreads;
-  if (blocks > num_reqs / 16 + 1) blocks = num_reqs / 16 + 1;
   if (blocks > cus) blocks = cus;
   if (blocks < 1) blocks = 1;
   hipLaunchKernelGGL(release_kernel, dim3(unsigned(blocks)), dim3(kReleaseThreads),

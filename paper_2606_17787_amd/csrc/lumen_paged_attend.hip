@@ -56,7 +56,7 @@ __device__ __forceinline__ int tiles_of(const AttendArgs &a, const Request &q) {
 // Places that the rows up to `end` see at most, of those that the table has.
 __device__ __forceinline__ int seen_to(const AttendArgs &a, const Request &q, int end) {
   const int rows = q.m * a.group;
-  const int tok = ((end < rows ? end : rows) - 1) / a.group;
+  const int tok = quotient(a.by_group, (end < rows ? end : rows) - 1);
   const int to = q.n - q.m + tok + 1;
   return to < a.cap ? to : a.cap;
 }
@@ -262,9 +262,10 @@ struct Row {
 
 __device__ __forceinline__ Row row_of(const AttendArgs &a, const Unit &u, int h, int row,
                                       int half) {
-  const int tok = row / a.group;
+  int head;
+  const int tok = quotient(a.by_group, row, &head);
   return Row{row < u.m * a.group,
-             (int64_t(u.q0) + tok) * a.q_heads + h * a.group + (row - tok * a.group), half};
+             (int64_t(u.q0) + tok) * a.q_heads + h * a.group + head, half};
 }
 
 // 32 elements of it from element 32 * d on.  m is -infinity where the row has seen
@@ -367,7 +368,7 @@ __global__ __launch_bounds__(kWaves *kWave, 2) void attend_kernel(AttendArgs a) 
   const bool here = wave_row < rows;
   const int behind = u.n - u.m;
   const auto limit_of = [&](int x) __attribute__((always_inline)) {
-    return behind + (x < rows ? x : rows - 1) / a.group;
+    return behind + quotient(a.by_group, x < rows ? x : rows - 1);
   };
   const int limit = limit_of(row);              // last place that the lane's query sees
   const int wave_limit = limit_of(wave_row);    // that all of the wavefront's see
@@ -379,9 +380,10 @@ __global__ __launch_bounds__(kWaves *kWave, 2) void attend_kernel(AttendArgs a) 
   // ---- Q: the lane's query, as the right operand (k = 8 * half + j)
   frag8 q[D / 16];
   {
-    const int x = row < rows ? row : rows - 1, tok = x / a.group;
+    int head;
+    const int tok = quotient(a.by_group, row < rows ? row : rows - 1, &head);
     const uint16_t *p = a.q.base + (int64_t(u.q0) + tok) * a.q.token +
-                        int64_t(h * a.group + (x - tok * a.group)) * a.q.head + 8 * half;
+                        int64_t(h * a.group + head) * a.q.head + 8 * half;
 #pragma unroll
     for (int i = 0; i < D / 16; ++i)
       q[i] = *reinterpret_cast<const frag8 *>(p + 16 * i);
@@ -454,11 +456,12 @@ __global__ __launch_bounds__(kWaves *kWave, 2) void attend_kernel(AttendArgs a) 
       bool in = place < end;
       uint64_t at = 0;
       if (in) {
-        const int page = int(uint32_t(place) / uint32_t(a.block_size));
+        int in_page;
+        const int page = quotient(a.by_block, place, &in_page);
         const int32_t id = a.bt[int64_t(u.r) * a.bt_cols + page];
         in = id >= 0 && id < a.num_blocks;
         if (!in) err = LUMEN_ERR_BLOCK_ID;
-        if (in) at = uint64_t(id) * a.page + uint64_t(place - page * a.block_size) * a.slot_bytes;
+        if (in) at = uint64_t(id) * a.page + uint64_t(in_page) * a.slot_bytes;
       }
       const uint64_t live = __ballot(in);
       if (lane == 0) live_at[i / kKeys] = live;

@@ -10,6 +10,27 @@ namespace lumen_paged_detail {
 
 using namespace lumen_attn_detail;
 
+// Division by a number that the host knows: the product with its reciprocal is the
+// quotient or one less.
+struct Divisor {
+  uint32_t d, m;
+};
+
+inline Divisor divisor(int32_t d) {
+  return Divisor{uint32_t(d), uint32_t(UINT32_MAX / uint32_t(d))};
+}
+
+__device__ __forceinline__ int quotient(const Divisor &by, int x, int *rest) {
+  uint32_t q = __umulhi(uint32_t(x), by.m), r = uint32_t(x) - q * by.d;
+  const bool more = r >= by.d;
+  *rest = int(more ? r - by.d : r);
+  return int(more ? q + 1 : q);
+}
+__device__ __forceinline__ int quotient(const Divisor &by, int x) {
+  int rest;
+  return quotient(by, x, &rest);
+}
+
 // Sizes of a 16-bit cache, in bytes.
 struct Pages {
   int64_t half;     // K or V of a layer
@@ -89,6 +110,7 @@ struct Call {
   int64_t num_q;
   int32_t max_new;
   int32_t q_heads, kv_heads, group;
+  Divisor by_block, by_group;  // block_size, group
   float scale_log2;
   int32_t *status;
 };
@@ -121,6 +143,8 @@ inline Call call_of(const lumen_kv_layout *l, const Pages &p, int32_t layer, con
   c.q_heads = q_heads;
   c.kv_heads = l->num_kv_heads;
   c.group = q_heads / l->num_kv_heads;
+  c.by_block = divisor(c.block_size);
+  c.by_group = divisor(c.group);
   c.scale_log2 = scale_log2(scale);
   c.status = status;
   return c;

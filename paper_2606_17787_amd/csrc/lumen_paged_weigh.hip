@@ -75,9 +75,9 @@ struct Slot {
 __device__ __forceinline__ Slot slot_of(const Call &a, int r, int place, int n, int *err) {
   Slot s{0, 0, place < n};
   if (s.in) {
-    const int page = int(uint32_t(place) / uint32_t(a.block_size));
+    int at;
+    const int page = quotient(a.by_block, place, &at);
     const int64_t block = a.bt[int64_t(r) * a.bt_cols + page];
-    const int at = place - page * a.block_size;
     s.in = block >= 0 && block < a.num_blocks;
     if (s.in) {
       s.row = block * a.page + int64_t(at) * a.slot_bytes;
@@ -139,7 +139,9 @@ __global__ __launch_bounds__(kThreads, 4) void weigh_kernel(WeighArgs a) {
         const int in = (i * kThreads + tid) / kChunks;
         int row = (first + tile) * kRows + in;
         row = row < rows ? row : rows - 1;
-        const int tok = row / a.group, head = h * a.group + (row - tok * a.group);
+        int head;
+        const int tok = quotient(a.by_group, row, &head);
+        head += h * a.group;
         load_row(qb + int64_t(tok) * a.q.token + int64_t(head) * a.q.head +
                      8 * ((tid % kChunks) ^ swizzle_k<D>(in)),
                  lds_at + stage * kTile + i * kThreads * 16);
@@ -165,8 +167,9 @@ __global__ __launch_bounds__(kThreads, 4) void weigh_kernel(WeighArgs a) {
       for (int i = tid; i < count * kRows; i += kThreads) {
         int row = (first + base) * kRows + i;
         row = row < rows ? row : rows - 1;
-        const int tok = row / a.group;
-        shifts[i] = shift_of(lse[int64_t(tok) * a.q_heads + h * a.group + (row - tok * a.group)]);
+        int head;
+        const int tok = quotient(a.by_group, row, &head);
+        shifts[i] = shift_of(lse[int64_t(tok) * a.q_heads + h * a.group + head]);
       }
       __syncthreads();
 #pragma unroll
@@ -199,9 +202,9 @@ __global__ __launch_bounds__(kThreads, 4) void weigh_kernel(WeighArgs a) {
 #pragma unroll
         for (int i = 0; i < 16; ++i)
           sc[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i], a.scale_log2, -shift));
-        if (row0 + kRows > rows || behind + row0 / a.group < place0 + 31) {
+        if (row0 + kRows > rows || behind + quotient(a.by_group, row0) < place0 + 31) {
           const int row = row0 + col;
-          const uint64_t sees = row < rows ? sees_to(behind + row / a.group, place0) : 0;
+          const uint64_t sees = row < rows ? sees_to(behind + quotient(a.by_group, row), place0) : 0;
           const uint32_t mine = uint32_t(sees) >> (4 * half);
 #pragma unroll
           for (int i = 0; i < 16; ++i)
@@ -321,8 +324,10 @@ __global__ __launch_bounds__(kThreads, 2) void weigh_few_kernel(WeighArgs a) {
     int limit[kTiles];  // the last place that the lane's query sees
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
-      const int at = t * 16 + col, row = at < rows ? at : rows - 1, tok = row / a.group;
-      const int head = h * a.group + (row - tok * a.group);
+      const int at = t * 16 + col, row = at < rows ? at : rows - 1;
+      int head;
+      const int tok = quotient(a.by_group, row, &head);
+      head += h * a.group;
       const uint16_t *p = a.q.base + (int64_t(q.q0) + tok) * a.q.token +
                           int64_t(head) * a.q.head + 8 * quad;
 #pragma unroll

@@ -553,8 +553,11 @@ def test_evict_layers():
 
 @pytest.mark.parametrize("n,keep", [([5000], [4096]), ([5000], [4999]),
                                     ([9000, 100, 4500], [700, 90, 4400]),
-                                    ([20000], [9000])])
-@pytest.mark.parametrize("kind", ["mixed", "ties"])
+                                    ([20000], [9000]), ([40000], [30000]),
+                                    ([33000, 100], [5, 90]),
+                                    ([2048], [2047]), ([4096], [1]),
+                                    ([8192], [8000]), ([32768], [32767])])
+@pytest.mark.parametrize("kind", ["mixed", "ties", "odd"])
 def test_evict_long(n, keep, kind):
     Evict(n, keep, H=1, seed=5, kind=kind).check()
 
