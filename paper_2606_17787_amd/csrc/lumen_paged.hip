@@ -138,7 +138,9 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictArgs a) {
   constexpr int kWaves = kThreads / kWave;
   constexpr int kOwn = kBins / kThreads;  // bins of a thread
   constexpr int kMostStrips = kPer ? kPer * kWaves : 1;
-  __shared__ uint32_t hist[kBins];
+  // as many counts of a bin as keep lanes with the same digit from waiting for each other
+  constexpr int kCopies = kThreads == 1024 ? 4 : 2;
+  __shared__ __attribute__((aligned(16))) uint32_t hist[kCopies][kBins];
   __shared__ uint32_t wave_a[kWaves], wave_b[kWaves];
   __shared__ uint32_t strip_more[kMostStrips], strip_same[kMostStrips];
   __shared__ uint32_t digit, above, inside;
@@ -260,16 +262,25 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictArgs a) {
     const int low = shift > 0 ? shift : 0;  // the last digit has 10 bits
     const uint32_t digits = (mask ? ~mask : 0xffffffffu) >> low;
 #pragma unroll
-    for (int b = 0; b < kOwn; ++b) hist[b * kThreads + tid] = 0;
+    for (int b = 0; b < kOwn * kCopies; ++b) (&hist[0][0])[b * kThreads + tid] = 0;
     __syncthreads();
     each([&](int i, uint32_t x, int) __attribute__((always_inline)) {
-      if (i < n && (x & mask) == last) atomicAdd(&hist[x >> low & digits], 1u);
+      if (i < n && (x & mask) == last) atomicAdd(&hist[tid % kCopies][x >> low & digits], 1u);
     });
     __syncthreads();
     // the thread's bins, the highest first
     uint32_t c[kOwn], sum = 0;
 #pragma unroll
-    for (int b = 0; b < kOwn; ++b) sum += c[b] = hist[kBins - 1 - (kOwn * tid + b)];
+    for (int b = 0; b < kOwn; ++b) c[b] = 0;
+#pragma unroll
+    for (int y = 0; y < kCopies; ++y) {
+      typedef uint32_t own __attribute__((ext_vector_type(kOwn)));
+      const own x = *reinterpret_cast<const own *>(&hist[y][kBins - kOwn * (tid + 1)]);
+#pragma unroll
+      for (int b = 0; b < kOwn; ++b) c[b] += x[kOwn - 1 - b];
+    }
+#pragma unroll
+    for (int b = 0; b < kOwn; ++b) sum += c[b];
     uint32_t upto = sum;
     for (int o = 1; o < kWave; o <<= 1) {
       const uint32_t x = __shfl_up(upto, o);
