@@ -90,9 +90,11 @@ struct EvictArgs {
   int32_t sinks, num_reqs;
   int32_t *left;
   int32_t *status;
-  // the workspace, for each (layer, request, head): how many places move, and for
-  // each 64 of its places which are kept and how many are before them
+  // the workspace, for each (layer, request, head): how many places move, and the
+  // places given up and those that take them, the last first, or for each 64 of its
+  // places which are kept and how many are before them
   int32_t *moves;
+  uint16_t *lists;
   uint64_t *kept;
   uint32_t *before;
   int32_t strips;  // 64 places each, of a request at most
@@ -121,30 +123,81 @@ __device__ __forceinline__ Item item_of(const EvictArgs &a, int64_t i) {
   return Item{layer, int(lr - int64_t(layer) * a.num_reqs), int(i - lr * a.heads)};
 }
 
+// Moves `count` places of one layer, request and head, at most 64: lane l knows where
+// the l-th goes and where it is.  Rows of K and V go 16 bytes a lane, the ledger's
+// words by the lane itself.  No place is both read and written.
+typedef uint32_t piece __attribute__((ext_vector_type(4)));  // 16 bytes of a row
+template <int D>
+__device__ __forceinline__ void move_places(const EvictArgs &a, const Item &it, int to, int src,
+                                            int count) {
+  constexpr int kLanes = D / 8, kRows = kWave / kLanes;  // rows at a time
+  const int lane = threadIdx.x & (kWave - 1);
+  const int32_t *table = a.bt + int64_t(it.r) * a.bt_cols;
+  uint8_t *const k = a.cache + int64_t(it.layer) * 2 * a.half + int64_t(it.h) * a.head_bytes +
+                     lane % kLanes * 16;
+  uint32_t *const ledger = a.ledger + int64_t(it.layer) * 2 * a.words +
+                           int64_t(it.h) * a.block_size;
+  const auto bytes = [&](int place, int64_t *word) __attribute__((always_inline)) {
+    int at;
+    const int64_t block = table[quotient(a.by_block, place, &at)];
+    *word = block * a.heads * a.block_size + at;
+    return block * a.page + int64_t(at) * a.slot_bytes;
+  };
+  int64_t word_to, word_src;
+  const int64_t byte_to = bytes(to, &word_to), byte_src = bytes(src, &word_src);
+  if (lane < count) {
+    ledger[word_to] = ledger[word_src];
+    ledger[word_to + a.words] = ledger[word_src + a.words];
+  }
+  for (int i = 0; i < count; i += 4 * kRows) {  // four rows under way a lane
+    piece x[4], y[4];
+    int64_t to_row[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int row = i + u * kRows + lane / kLanes;  // below 64
+      const int64_t from_row = __shfl(byte_src, row);
+      to_row[u] = __shfl(byte_to, row);
+      if (row < count) {
+        x[u] = *reinterpret_cast<const piece *>(k + from_row);
+        y[u] = *reinterpret_cast<const piece *>(k + a.half + from_row);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (i + u * kRows + lane / kLanes < count) {
+        *reinterpret_cast<piece *>(k + to_row[u]) = x[u];
+        *reinterpret_cast<piece *>(k + a.half + to_row[u]) = y[u];
+      }
+  }
+}
+
 // What a workgroup does for one layer, request and head: which places are kept.
 //
 // Protected places are counted first: where they do not fill the budget, all of them
 // are kept and the others are ranked, where they do, they are ranked alone.  The rank
-// of the last one kept comes out of counts over the ranks' digits of 11 bits, from the
-// highest on, until every rank left is kept; which places are kept, and how many are
-// before them, then goes to the workspace by strips of 64 places.
+// of the last one kept comes out of counts over the ranks' digits of 10 or 11 bits, from
+// the highest on, until every rank left is kept.
 //
 // A thread holds the ranks of kPer places, one of each kThreads, for requests of up to
 // kThreads * kPer; where kPer is 0 (longer ones), each pass reads them again.
-constexpr int kDigit = 11, kBins = 1 << kDigit;
-
-template <int kThreads, int kPer>
+//
+// Where places move, the k-th place given up and the k-th one kept behind the budget
+// belong together.  D is 0 where evict_move_kernel moves them; otherwise this
+// workgroup does, with the two lists in LDS.
+template <int kThreads, int kPer, int D>
 __global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictArgs a) {
   constexpr int kWaves = kThreads / kWave;
+  constexpr int kDigit = kThreads == 1024 ? 11 : 10, kBins = 1 << kDigit;
   constexpr int kOwn = kBins / kThreads;  // bins of a thread
   constexpr int kMostStrips = kPer ? kPer * kWaves : 1;
   // as many counts of a bin as keep lanes with the same digit from waiting for each other
-  constexpr int kCopies = kThreads == 1024 ? 4 : 2;
+  constexpr int kCopies = kThreads == 1024 ? 4 : 1;
   __shared__ __attribute__((aligned(16))) uint32_t hist[kCopies][kBins];
   __shared__ uint32_t wave_a[kWaves], wave_b[kWaves];
   __shared__ uint32_t strip_more[kMostStrips], strip_same[kMostStrips];
+  __shared__ uint16_t lists[2][D ? kThreads * kPer / 2 : 1];
   __shared__ uint32_t digit, above, inside;
-  __shared__ int guarded;
+  __shared__ int guarded, moved;
   const int64_t id = blockIdx.x;
   const Item it = item_of(a, id);
   const int tid = threadIdx.x, lane = tid & (kWave - 1);
@@ -227,6 +280,8 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictArgs a) {
       mine += protects(int32_t(weights[word_of(i, page_of(i), table[page_of(i)]) + a.words]),
                        a.sinks, from);
   if (tid == 0) guarded = 0;
+#pragma unroll
+  for (int b = 0; b < kOwn * kCopies; ++b) (&hist[0][0])[b * kThreads + tid] = 0;
   __syncthreads();
   for (int o = 1; o < kWave; o <<= 1) mine += __shfl_xor(mine, o);
   if (lane == 0) atomicAdd(&guarded, mine);
@@ -259,11 +314,8 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictArgs a) {
   // ---- the rank of the last place kept
   uint32_t last = 0, mask = 0, want = uint32_t(keep);
   for (int shift = 32 - kDigit; mask != 0xffffffffu; shift -= kDigit) {
-    const int low = shift > 0 ? shift : 0;  // the last digit has 10 bits
+    const int low = shift > 0 ? shift : 0;  // the last digit has fewer bits
     const uint32_t digits = (mask ? ~mask : 0xffffffffu) >> low;
-#pragma unroll
-    for (int b = 0; b < kOwn * kCopies; ++b) (&hist[0][0])[b * kThreads + tid] = 0;
-    __syncthreads();
     each([&](int i, uint32_t x, int) __attribute__((always_inline)) {
       if (i < n && (x & mask) == last) atomicAdd(&hist[tid % kCopies][x >> low & digits], 1u);
     });
@@ -275,9 +327,11 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictArgs a) {
 #pragma unroll
     for (int y = 0; y < kCopies; ++y) {
       typedef uint32_t own __attribute__((ext_vector_type(kOwn)));
-      const own x = *reinterpret_cast<const own *>(&hist[y][kBins - kOwn * (tid + 1)]);
+      own *const at = reinterpret_cast<own *>(&hist[y][kBins - kOwn * (tid + 1)]);
+      const own x = *at;
 #pragma unroll
       for (int b = 0; b < kOwn; ++b) c[b] += x[kOwn - 1 - b];
+      *at = own(0);  // for the next digit
     }
 #pragma unroll
     for (int b = 0; b < kOwn; ++b) sum += c[b];
@@ -309,20 +363,31 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictArgs a) {
   }
   // ---- every place above `last` is kept, and the first `want` of those at it
   const int strips = (n + kWave - 1) / kWave;
-  uint64_t *kept = a.kept + id * a.strips;
-  uint32_t *before = a.before + id * a.strips;
+  const int half = (a.strips * kWave + 1) / 2;
+  const auto to_at = [&](int m) __attribute__((always_inline)) -> uint16_t & {
+    return D ? lists[0][m] : a.lists[id * 2 * half + m];
+  };
+  const auto src_at = [&](int m) __attribute__((always_inline)) -> uint16_t & {
+    return D ? lists[1][m] : a.lists[id * 2 * half + half + m];
+  };
+  // What becomes of strip s, of whose places `more` and `same` are above and at `last`.
   const auto kept_of = [&](int s, uint64_t more, uint64_t same, uint32_t kept_before,
                            uint32_t same_before) __attribute__((always_inline)) {
-    const uint32_t nth = same_before + __popcll(same & ((uint64_t(1) << lane) - 1));
+    const uint64_t below = (uint64_t(1) << lane) - 1;
+    const uint32_t nth = same_before + __popcll(same & below);
     const uint64_t bits = more | __ballot((same >> lane & 1) && nth < want);
-    if (lane == 0) {
-      kept[s] = bits;
-      before[s] = kept_before;
-      if (s == keep / kWave)
-        a.moves[id] =
-            keep - int(kept_before + __popcll(bits & ((uint64_t(1) << keep % kWave) - 1)));
+    if (s == keep / kWave && lane == 0)
+      moved = keep - int(kept_before + __popcll(bits & ((uint64_t(1) << keep % kWave) - 1)));
+    if constexpr (kPer > 0) {
+      const int i = s * kWave + lane;
+      const int rank = int(kept_before + __popcll(bits & below));  // among the kept ones
+      if (i < keep && !(bits >> lane & 1)) to_at(i - rank) = uint16_t(i);
+      // the last of them first: how many are under the budget is not known yet
+      if (i >= keep && bits >> lane & 1) src_at(keep - 1 - rank) = uint16_t(i);
+    } else if (lane == 0) {
+      a.kept[id * a.strips + s] = bits;
+      a.before[id * a.strips + s] = kept_before;
     }
-    return bits;
   };
   if constexpr (kPer > 0) {
     // strip j * kWaves + wave is the wavefront's j-th
@@ -387,6 +452,18 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictArgs a) {
       same_before = e;
     });
   }
+  __syncthreads();
+  if constexpr (D == 0) {
+    if (tid == 0) a.moves[id] = moved;
+  } else {
+    const int moves = moved, per_wave = (moves + kWaves - 1) / kWaves;
+    const int end = (wave + 1) * per_wave < moves ? (wave + 1) * per_wave : moves;
+    for (int m = wave * per_wave; m < end; m += kWave) {
+      const int count = end - m < kWave ? end - m : kWave;
+      const int x = m + (lane < count ? lane : count - 1);
+      move_places<D>(a, it, lists[0][x], lists[1][moves - 1 - x], count);
+    }
+  }
 }
 
 // The place of the n-th (from 0) set bit.
@@ -404,15 +481,12 @@ __device__ __forceinline__ int nth_bit(uint64_t bits, uint32_t n) {
   return at;
 }
 
-// Moves what evict_select_kernel has chosen: a wavefront takes 64 moves, a lane
-// finds the two places of one (the k-th place given up, the k-th one kept behind the
-// budget) by bisection over the counts, and the rows go 16 bytes a lane.  No place
-// is both read and written.
-typedef uint32_t piece __attribute__((ext_vector_type(4)));  // 16 bytes of a row
+// Moves what evict_select_kernel has chosen, 64 places a wavefront at a time.  With
+// kLists their numbers are in the workspace; without, a lane finds them by bisection
+// over the counts.
 constexpr int kMoveThreads = 256;
-template <int D>
+template <int D, bool kLists>
 __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a, int32_t parts) {
-  constexpr int kLanes = D / 8, kRows = kWave / kLanes;  // rows at a time
   const int lane = threadIdx.x & (kWave - 1);
   const int64_t id = blockIdx.x / unsigned(parts);
   const int part = int(blockIdx.x - id * parts);
@@ -426,94 +500,92 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a, i
   const int n = a.lens[it.r], strips = (n + kWave - 1) / kWave, border = keep / kWave;
   const uint64_t *kept = a.kept + id * a.strips;
   const uint32_t *before = a.before + id * a.strips;
-  const int32_t *table = a.bt + int64_t(it.r) * a.bt_cols;
-  uint8_t *const k = a.cache + int64_t(it.layer) * 2 * a.half + int64_t(it.h) * a.head_bytes +
-                     lane % kLanes * 16;
-  uint32_t *const ledger = a.ledger + int64_t(it.layer) * 2 * a.words +
-                           int64_t(it.h) * a.block_size;
+  const int half = (a.strips * kWave + 1) / 2;
+  const uint16_t *lists = a.lists + id * 2 * half;
   const uint32_t inside = uint32_t(keep - moves);  // kept places under `keep`
   for (; int64_t(c) * kWave < moves; c += waves) {
-    const int m = c * kWave + lane;
-    const int here = moves - c * kWave < kWave ? moves - c * kWave : kWave;
-    const uint32_t nth = uint32_t(m < moves ? m : moves - 1);
-    // the strip with the nth place given up: the last with at most nth before it
-    int lo = 0, hi = border;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) / 2;
-      if (uint32_t(mid) * kWave - before[mid] <= nth)
-        lo = mid;
-      else
-        hi = mid - 1;
-    }
-    int to = lo * kWave + nth_bit(~kept[lo], nth - (uint32_t(lo) * kWave - before[lo]));
-    to = to < keep ? to : keep - 1;  // (it is: the tables bound every access)
-    lo = border, hi = strips - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) / 2;
-      if (before[mid] <= inside + nth)
-        lo = mid;
-      else
-        hi = mid - 1;
-    }
-    int src = lo * kWave + nth_bit(kept[lo], inside + nth - before[lo]);
-    src = src < n ? src : n - 1;
-    const auto bytes = [&](int place, int64_t *word) __attribute__((always_inline)) {
-      int at;
-      const int64_t block = table[quotient(a.by_block, place, &at)];
-      *word = block * a.heads * a.block_size + at;
-      return block * a.page + int64_t(at) * a.slot_bytes;
-    };
-    int64_t word_to, word_src;
-    const int64_t byte_to = bytes(to, &word_to), byte_src = bytes(src, &word_src);
-    if (m < moves) {
-      ledger[word_to] = ledger[word_src];
-      ledger[word_to + a.words] = ledger[word_src + a.words];
-    }
-    for (int i = 0; i < here; i += 4 * kRows) {  // four rows under way a lane
-      piece x[4], y[4];
-      int64_t to_row[4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int row = i + u * kRows + lane / kLanes;  // below 64
-        const int64_t from_row = __shfl(byte_src, row);
-        to_row[u] = __shfl(byte_to, row);
-        if (row < here) {
-          x[u] = *reinterpret_cast<const piece *>(k + from_row);
-          y[u] = *reinterpret_cast<const piece *>(k + a.half + from_row);
-        }
+    const int count = moves - c * kWave < kWave ? moves - c * kWave : kWave;
+    const int m = c * kWave + (lane < count ? lane : count - 1);
+    int to, src;
+    if constexpr (kLists) {
+      to = lists[m];
+      src = lists[half + moves - 1 - m];
+    } else {
+      const uint32_t nth = uint32_t(m);
+      // the strip with the nth place given up: the last with at most nth before it
+      int lo = 0, hi = border;
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (uint32_t(mid) * kWave - before[mid] <= nth)
+          lo = mid;
+        else
+          hi = mid - 1;
       }
-#pragma unroll
-      for (int u = 0; u < 4; ++u)
-        if (i + u * kRows + lane / kLanes < here) {
-          *reinterpret_cast<piece *>(k + to_row[u]) = x[u];
-          *reinterpret_cast<piece *>(k + a.half + to_row[u]) = y[u];
-        }
+      to = lo * kWave + nth_bit(~kept[lo], nth - (uint32_t(lo) * kWave - before[lo]));
+      to = to < keep ? to : keep - 1;  // (it is: the tables bound every access)
+      lo = border, hi = strips - 1;
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (before[mid] <= inside + nth)
+          lo = mid;
+        else
+          hi = mid - 1;
+      }
+      src = lo * kWave + nth_bit(kept[lo], inside + nth - before[lo]);
+      src = src < n ? src : n - 1;
     }
+    move_places<D>(a, it, to, src, count);
   }
 }
 
 // A launch takes less than 2^32 threads.
 constexpr int64_t kMostItems = UINT32_MAX / 1024;
 
+// Places of a request up to which a thread of 1,024 holds its ranks, and counts of
+// (layer, request, head) from which on their workgroups move the places themselves.
+constexpr int kHeldPlaces = 1024 * 32, kMovingItems = 512;
+
 struct EvictPlan {
   int32_t strips;
-  size_t kept_at, before_at, bytes;
+  bool held, moving;
+  size_t lists_at, before_at, bytes;
 };
 
 int evict_plan(const lumen_kv_layout *l, int32_t layers, int32_t bt_cols, int32_t num_reqs,
                EvictPlan *p) {
   if (bt_cols < 0 || num_reqs < 0) return LUMEN_ERR_INVALID_ARG;
-  if (int64_t(bt_cols) * l->block_size > LUMEN_PAGED_MAX_PLACES) return LUMEN_ERR_UNSUPPORTED;
+  const int64_t cap = int64_t(bt_cols) * l->block_size;
+  if (cap > LUMEN_PAGED_MAX_PLACES) return LUMEN_ERR_UNSUPPORTED;
   int64_t items;
   if (__builtin_mul_overflow(int64_t(layers) * num_reqs, int64_t(l->num_kv_heads), &items) ||
       items > kMostItems)
     return LUMEN_ERR_UNSUPPORTED;
-  p->strips = int32_t((int64_t(bt_cols) * l->block_size + kWave - 1) / kWave);
+  p->strips = int32_t((cap + kWave - 1) / kWave);
+  p->held = cap <= kHeldPlaces;
+  p->moving = p->held && items >= kMovingItems;
   const auto up = [](size_t n) { return (n + 255) & ~size_t(255); };
-  p->kept_at = up(size_t(items) * sizeof(int32_t));
-  p->before_at = p->kept_at + up(size_t(items) * p->strips * sizeof(uint64_t));
-  p->bytes = p->before_at + up(size_t(items) * p->strips * sizeof(uint32_t));
+  const size_t strips = size_t(items) * p->strips;
+  p->lists_at = up(size_t(items) * sizeof(int32_t));
+  p->before_at = p->lists_at +
+                 up(p->moving ? 0 : strips * (p->held ? kWave * sizeof(uint16_t) : sizeof(uint64_t)));
+  p->bytes = p->before_at + up(p->held ? 0 : strips * sizeof(uint32_t));
   return LUMEN_OK;
+}
+
+template <int D>
+void (*select_kernel(int64_t cap, int *threads))(EvictArgs) {
+  *threads = cap <= 256 * 16 ? 256 : 1024;
+  return cap <= 256 * 8    ? evict_select_kernel<256, 8, D>
+         : cap <= 256 * 16 ? evict_select_kernel<256, 16, D>
+         : cap <= 1024 * 8 ? evict_select_kernel<1024, 8, D>
+                           : evict_select_kernel<1024, 32, D>;
+}
+
+template <bool kLists>
+void (*move_kernel(int head_dim))(EvictArgs, int32_t) {
+  return head_dim == 64    ? evict_move_kernel<64, kLists>
+         : head_dim == 128 ? evict_move_kernel<128, kLists>
+                           : evict_move_kernel<256, kLists>;
 }
 
 // --------------------------------------------------------------- release
@@ -733,34 +805,33 @@ int lumen_paged_evict(const lumen_kv_layout *layout, int32_t first_layer, int32_
   a.status = d_status;
   char *ws = static_cast<char *>(d_workspace);
   a.moves = reinterpret_cast<int32_t *>(ws);
-  a.kept = reinterpret_cast<uint64_t *>(ws + plan.kept_at);
+  a.lists = reinterpret_cast<uint16_t *>(ws + plan.lists_at);
+  a.kept = reinterpret_cast<uint64_t *>(ws + plan.lists_at);
   a.before = reinterpret_cast<uint32_t *>(ws + plan.before_at);
   a.strips = plan.strips;
   const int64_t cap = int64_t(bt_cols) * layout->block_size;
   const int64_t items = int64_t(num_layers) * num_reqs * a.heads;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const auto select = [&](void (*kernel)(EvictArgs), int threads) {
-    hipLaunchKernelGGL(kernel, dim3(unsigned(items)), dim3(unsigned(threads)), 0, s, a);
-  };
-  if (cap <= 256 * 8)
-    select(evict_select_kernel<256, 8>, 256);
-  else if (cap <= 256 * 16)
-    select(evict_select_kernel<256, 16>, 256);
-  else if (cap <= 1024 * 8)
-    select(evict_select_kernel<1024, 8>, 1024);
-  else if (cap <= 1024 * 32)
-    select(evict_select_kernel<1024, 32>, 1024);
-  else
-    select(evict_select_kernel<1024, 0>, 1024);
-  // a wavefront for 64 moves, of which a request has at most half its places
-  int64_t parts = (cap / 2 + kMoveThreads - 1) / kMoveThreads;
-  if (parts > 64) parts = 64;
-  if (parts > int64_t(UINT32_MAX / kMoveThreads) / items) parts = UINT32_MAX / kMoveThreads / items;
-  if (parts < 1) parts = 1;
-  hipLaunchKernelGGL(layout->head_dim == 64    ? evict_move_kernel<64>
-                     : layout->head_dim == 128 ? evict_move_kernel<128>
-                                               : evict_move_kernel<256>,
-                     dim3(unsigned(items * parts)), dim3(kMoveThreads), 0, s, a, int32_t(parts));
+  int threads = 1024;
+  const int D = layout->head_dim;
+  void (*select)(EvictArgs) = evict_select_kernel<1024, 0, 0>;
+  if (plan.held)
+    select = !plan.moving ? select_kernel<0>(cap, &threads)
+             : D == 64    ? select_kernel<64>(cap, &threads)
+             : D == 128   ? select_kernel<128>(cap, &threads)
+                          : select_kernel<256>(cap, &threads);
+  hipLaunchKernelGGL(select, dim3(unsigned(items)), dim3(unsigned(threads)), 0, s, a);
+  if (!plan.moving) {
+    // a wavefront for 64 moves, of which a request has at most half its places
+    int64_t parts = (cap / 2 + kMoveThreads - 1) / kMoveThreads;
+    if (parts > 64) parts = 64;
+    if (parts > int64_t(UINT32_MAX / kMoveThreads) / items)
+      parts = UINT32_MAX / kMoveThreads / items;
+    if (parts < 1) parts = 1;
+    const auto move = plan.held ? move_kernel<true>(D) : move_kernel<false>(D);
+    hipLaunchKernelGGL(move, dim3(unsigned(items * parts)), dim3(kMoveThreads), 0, s, a,
+                       int32_t(parts));
+  }
   return hipGetLastError() == hipSuccess ? LUMEN_OK : LUMEN_ERR_HIP;
 }
 

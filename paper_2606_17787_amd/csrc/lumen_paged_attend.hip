@@ -388,10 +388,6 @@ __global__ __launch_bounds__(kWaves *kWave, 2) void attend_kernel(AttendArgs a) 
     for (int i = 0; i < D / 16; ++i)
       q[i] = *reinterpret_cast<const frag8 *>(p + 16 * i);
   }
-  // the queries are here before the first tile's loads, which the compiler does
-  // not count, so that no wait for them is left in the loop
-  __builtin_amdgcn_s_waitcnt(0x0f70);
-
   const uint8_t *const kb = a.k + int64_t(h) * a.head_bytes;
   const uint8_t *const vb = a.v + int64_t(h) * a.head_bytes;
   const uint32_t lds_at = uint32_t(__builtin_amdgcn_readfirstlane(
@@ -469,6 +465,9 @@ __global__ __launch_bounds__(kWaves *kWave, 2) void attend_kernel(AttendArgs a) 
     }
     if (tid < 2) bad_rows[tid] = 0;
     __syncthreads();
+    // the queries are here before the first tile's loads, which the compiler does not
+    // count, so that no wait for them is left in the loop
+    __builtin_amdgcn_s_waitcnt(0x0f70);
 #pragma unroll
     for (int i = 0; i < kStages - 1; ++i)
       if (i < count) load(i, i);
@@ -615,7 +614,8 @@ __global__ __launch_bounds__(kWaves *kWave, 2) void attend_kernel(AttendArgs a) 
   both<32>(l, &la, &lb);
   l = la + lb;
   if (seen && m == -INFINITY) m = -FLT_MAX;
-  if (u.place >= 0) {
+  if (!here) {
+  } else if (u.place >= 0) {
     float *part = a.parts + (int64_t(u.place) * a.kv_heads + h) * part_floats(D, kWaves);
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)
@@ -625,7 +625,7 @@ __global__ __launch_bounds__(kWaves *kWave, 2) void attend_kernel(AttendArgs a) 
             float4{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
     part[kThreads * (D / 2) + tid] = m;
     part[kThreads * (D / 2 + 1) + tid] = l;
-  } else if (here) {
+  } else {
     const Row r = row_of(a, u, h, row, half);
 #pragma unroll
     for (int d = 0; d < D / 32; ++d) write_row<D, kBf16>(a, r, d, o[d], m, l);
@@ -645,6 +645,7 @@ __global__ __launch_bounds__(kWaves *kWave, 2) void attend_join_kernel(AttendArg
     const int d = item % (D / 32), h = item / (D / 32) % a.kv_heads;
     const Cut cut = a.cuts[item / (D / 32) / a.kv_heads];
     const Unit u = a.units[cut.unit];
+    if (u.row0 + wave * 32 >= u.m * a.group) continue;  // no rows of this wavefront
     const Row r = row_of(a, u, h, u.row0 + wave * 32 + (lane & 31), lane >> 5);
     const int64_t apart = int64_t(a.kv_heads) * part_floats(D, kWaves);
     const float *part = a.parts + (int64_t(u.place) * a.kv_heads + h) * part_floats(D, kWaves);

@@ -562,10 +562,19 @@ def test_evict_long(n, keep, kind):
     Evict(n, keep, H=1, seed=5, kind=kind).check()
 
 
-def test_evict_many_requests():
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("H,long", [(1, 120), (2, 120), (2, 3000), (2, 7000),
+                                    (2, 20000)])
+def test_evict_many_requests(H, long, D):
+    """Few and many (layer, request, head), whose workgroups then move their
+    places themselves; one of the requests longer than the others."""
     rng = np.random.default_rng(6)
-    n = rng.integers(0, 120, 300)
-    Evict(n, rng.integers(0, 100, 300), H=1, seed=6).check()
+    R = 300 if D == 64 else 256
+    n = rng.integers(0, 120, R)
+    n[7] = long
+    keep = rng.integers(0, 100, R)
+    keep[7] = long // 3
+    Evict(n, keep, H=H, D=D, seed=6).check()
 
 
 def test_evict_bad_requests():
