@@ -91,31 +91,35 @@ __device__ __forceinline__ Slot slot_of(const Call &a, int r, int place, int n, 
 
 // ------------------------------------------------- more than 32 query rows
 
-constexpr int kRows = 32;     // query rows of a tile
+constexpr int kGroups = 2;    // of four wavefronts
+constexpr int kRows = 32 * kGroups;  // query rows of a tile
 constexpr int kStages = 4;    // tiles in LDS
-constexpr int kRound = 32;    // tiles whose lse is in LDS
+constexpr int kRound = 16;    // tiles whose lse is in LDS
 constexpr int kChunk = 32 * kWaves;  // places of a workgroup
 
 // A workgroup takes 128 places of a request and a KV head, a wavefront 32 of them,
 // and holds their keys as the left operand of 32x32x16 products.  The query rows that
-// see them come through LDS, 32 at a time and kStages tiles in turn, for all four
-// wavefronts: scores^T = K Q^T, queries across, so that a lane has one query's lse.
-// Its weights are added up by place in 32 bits, and over the lanes at the end.  A
-// tile's 16-byte chunks are permuted by row as attend's keys are.
+// see them come through LDS, 64 at a time and kStages tiles in turn, 32 for the first
+// four wavefronts and 32 for the others, so that four of them share a SIMD: scores^T =
+// K Q^T, queries across, so that a lane has one query's lse.  Its weights are added up
+// by place in 32 bits, and over the lanes and the two groups at the end.  A tile's
+// 16-byte chunks are permuted by row as attend's keys are.
 template <int D, bool kBf16>
-__global__ __launch_bounds__(kThreads, 4) void weigh_kernel(WeighArgs a) {
+__global__ __launch_bounds__(kGroups *kThreads, 4) void weigh_kernel(WeighArgs a) {
   constexpr int kChunks = D / 8;
-  constexpr int kIssues = kRows * kChunks / kThreads;
+  constexpr int kAll = kGroups * kThreads;
+  constexpr int kIssues = kRows * kChunks / kAll;
   constexpr int kTile = kRows * D * 2;  // bytes
   __shared__ __attribute__((aligned(1024))) uint8_t lds[kStages * kTile];
-  __shared__ float shifts[kRound * kRows];
+  __shared__ float shifts[kRound * kRows], merged[kChunk];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 31, half = lane >> 5;
   const uint32_t lds_at = uint32_t(__builtin_amdgcn_readfirstlane(
       int(reinterpret_cast<uintptr_t>(LDS_PTR(uint8_t, lds))) + wave * kWave * 16));
   const auto *lds_bytes = LDS_PTR(const char, lds);
-  const uint32_t read_q = col * D * 2 + 16 * (half ^ swizzle_k<D>(col));
+  const int group = wave / kWaves;  // of the wavefront
+  const uint32_t read_q = (group * 32 + col) * D * 2 + 16 * (half ^ swizzle_k<D>(col));
   const int64_t items = int64_t(a.num_reqs) * a.chunks * a.kv_heads;
   for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
     const int64_t rest = item / a.kv_heads;
@@ -124,7 +128,7 @@ __global__ __launch_bounds__(kThreads, 4) void weigh_kernel(WeighArgs a) {
     Request q;
     int err = request(a, r, &q);
     if (chunk == 0 && h == 0 && wave == 0) record_wave(a.status, err);
-    const int first_place = chunk * kChunk, place0 = first_place + wave * 32;
+    const int first_place = chunk * kChunk, place0 = first_place + wave % kWaves * 32;
     const int n = q.n < a.cap ? q.n : a.cap;
     if (q.m == 0 || first_place >= n) continue;
     // ---- the rows, from the first that sees a place of the workgroup's on
@@ -133,18 +137,37 @@ __global__ __launch_bounds__(kThreads, 4) void weigh_kernel(WeighArgs a) {
     const int tiles = (rows + kRows - 1) / kRows - first;
     const uint16_t *const qb = a.q.base + int64_t(q.q0) * a.q.token;
     const float *const lse = a.lse + int64_t(q.q0) * a.q_heads;
-    const auto load = [&](int tile, int stage) __attribute__((always_inline)) {
+    // the lane's row of each load of the next tile: its place in memory goes on by 32
+    // rows with a few additions
+    int row[kIssues], head[kIssues];
+    const uint16_t *from[kIssues], *last;
+    const auto row_at = [&](int x, int *hd) __attribute__((always_inline)) {
+      const int tok = quotient(a.by_group, x, hd);
+      return qb + int64_t(tok) * a.q.token + int64_t(h * a.group + *hd) * a.q.head;
+    };
+    int step_heads;
+    const int step_toks = quotient(a.by_group, kRows, &step_heads);
+    const int64_t step = step_toks * a.q.token + step_heads * a.q.head;
+    const int64_t wrap = a.q.token - a.group * a.q.head;
+    last = row_at(rows - 1, &row[0]);
+#pragma unroll
+    for (int i = 0; i < kIssues; ++i) {
+      row[i] = first * kRows + (i * kAll + tid) / kChunks;
+      from[i] = row_at(row[i], &head[i]);
+    }
+    const auto load_next = [&](int stage) __attribute__((always_inline)) {
 #pragma unroll
       for (int i = 0; i < kIssues; ++i) {
-        const int in = (i * kThreads + tid) / kChunks;
-        int row = (first + tile) * kRows + in;
-        row = row < rows ? row : rows - 1;
-        int head;
-        const int tok = quotient(a.by_group, row, &head);
-        head += h * a.group;
-        load_row(qb + int64_t(tok) * a.q.token + int64_t(head) * a.q.head +
-                     8 * ((tid % kChunks) ^ swizzle_k<D>(in)),
-                 lds_at + stage * kTile + i * kThreads * 16);
+        load_row((row[i] < rows ? from[i] : last) +
+                     8 * ((tid % kChunks) ^ swizzle_k<D>((i * kAll + tid) / kChunks)),
+                 lds_at + stage * kTile + i * kAll * 16);
+        row[i] += kRows;
+        head[i] += step_heads;
+        from[i] += step;
+        if (head[i] >= a.group) {
+          head[i] -= a.group;
+          from[i] += wrap;
+        }
       }
     };
     err = LUMEN_OK;
@@ -164,17 +187,16 @@ __global__ __launch_bounds__(kThreads, 4) void weigh_kernel(WeighArgs a) {
     for (int base = 0; base < tiles; base += kRound) {
       const int count = tiles - base < kRound ? tiles - base : kRound;
       __syncthreads();  // the tiles before are done with
-      for (int i = tid; i < count * kRows; i += kThreads) {
-        int row = (first + base) * kRows + i;
-        row = row < rows ? row : rows - 1;
-        int head;
-        const int tok = quotient(a.by_group, row, &head);
-        shifts[i] = shift_of(lse[int64_t(tok) * a.q_heads + h * a.group + head]);
+      for (int i = tid; i < count * kRows; i += kAll) {
+        const int x = (first + base) * kRows + i;
+        int hd;
+        const int tok = quotient(a.by_group, x < rows ? x : rows - 1, &hd);
+        shifts[i] = shift_of(lse[int64_t(tok) * a.q_heads + h * a.group + hd]);
       }
       __syncthreads();
 #pragma unroll
       for (int i = 0; i < kStages - 1; ++i)
-        if (i < count) load(base + i, i);
+        if (i < count) load_next(i);
       int stage = 0;
       for (int at = 0; at < count; ++at) {
         const int tile = base + at, after = count - 1 - at;  // tiles loaded after this one
@@ -185,10 +207,9 @@ __global__ __launch_bounds__(kThreads, 4) void weigh_kernel(WeighArgs a) {
         else
           wait_loads<0>();
         lds_barrier();
-        if (at + kStages - 1 < count)
-          load(tile + kStages - 1, stage ? stage - 1 : kStages - 1);
-        const int row0 = (first + tile) * kRows;
-        const uint32_t from = stage * kTile;
+        if (at + kStages - 1 < count) load_next(stage ? stage - 1 : kStages - 1);
+        const int row0 = (first + tile) * kRows + group * 32;
+        const uint32_t in_stage = stage * kTile;
         f32x16 sc;
 #pragma unroll
         for (int i = 0; i < 16; ++i) sc[i] = 0.0f;
@@ -196,15 +217,15 @@ __global__ __launch_bounds__(kThreads, 4) void weigh_kernel(WeighArgs a) {
         for (int i = 0; i < D / 16; ++i)
           sc = mfma<kBf16>(k[i],
                            *reinterpret_cast<const __attribute__((address_space(3))) frag8 *>(
-                               lds_bytes + ((read_q ^ (32 * i)) + from)),
+                               lds_bytes + ((read_q ^ (32 * i)) + in_stage)),
                            sc);
-        const float shift = shifts[at * kRows + col];
+        const float shift = shifts[at * kRows + group * 32 + col];
 #pragma unroll
         for (int i = 0; i < 16; ++i)
           sc[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i], a.scale_log2, -shift));
-        if (row0 + kRows > rows || behind + quotient(a.by_group, row0) < place0 + 31) {
-          const int row = row0 + col;
-          const uint64_t sees = row < rows ? sees_to(behind + quotient(a.by_group, row), place0) : 0;
+        if (row0 + 32 > rows || behind + quotient(a.by_group, row0 < rows ? row0 : rows - 1) < place0 + 31) {
+          const int x = row0 + col;
+          const uint64_t sees = x < rows ? sees_to(behind + quotient(a.by_group, x), place0) : 0;
           const uint32_t mine = uint32_t(sees) >> (4 * half);
 #pragma unroll
           for (int i = 0; i < 16; ++i)
@@ -221,8 +242,11 @@ __global__ __launch_bounds__(kThreads, 4) void weigh_kernel(WeighArgs a) {
     const float total = sum_by_lane(s, lane);
     const int mine = place_of(col % 16, half);
     const int64_t word = __shfl(slot.word, mine) + int64_t(h) * a.block_size;
-    const bool in = __shfl(int(slot.in), mine);
-    if (col < 16 && in) a.weights[word] += total;
+    const bool in = __shfl(int(slot.in), mine) && col < 16;
+    __syncthreads();  // of the item before
+    if (group && col < 16) merged[wave % kWaves * 32 + mine] = total;
+    __syncthreads();
+    if (!group && in) a.weights[word] += total + merged[wave % kWaves * 32 + mine];
   }
 }
 
@@ -464,12 +488,12 @@ int lumen_paged_weigh(const lumen_kv_layout *layout, int32_t layer, const void *
   const bool bf = dtype == LUMEN_ATTN_BF16;
   const int D = layout->head_dim;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const auto launch = [&](void (*kernel)(WeighArgs)) {
+  const auto launch = [&](void (*kernel)(WeighArgs), int threads) {
     a.chunks = (a.cap + a.chunk - 1) / a.chunk;
     if (a.chunks < 1) a.chunks = 1;  // which looks at the requests
     int64_t groups = int64_t(num_reqs) * a.chunks;
     groups = groups < kMostGroups / a.kv_heads ? groups * a.kv_heads : kMostGroups;
-    hipLaunchKernelGGL(kernel, dim3(unsigned(groups)), dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL(kernel, dim3(unsigned(groups)), dim3(unsigned(threads)), 0, s, a);
   };
   const int64_t rows = int64_t(max_new) * a.group;
   if (rows <= 128) {
@@ -480,11 +504,13 @@ int lumen_paged_weigh(const lumen_kv_layout *layout, int32_t layer, const void *
 #endif
     if (a.chunk > kMostPlaces16) a.chunk = kMostPlaces16;
     launch(rows <= 16 ? few_kernel<1>(D, bf) : rows <= 64 ? few_kernel<4>(D, bf)
-                                                          : few_kernel<8>(D, bf));
+                                                          : few_kernel<8>(D, bf),
+           kThreads);
   } else {
     a.chunk = kChunk;
     launch(D == 64 ? (bf ? weigh_kernel<64, true> : weigh_kernel<64, false>)
-                   : (bf ? weigh_kernel<128, true> : weigh_kernel<128, false>));
+                   : (bf ? weigh_kernel<128, true> : weigh_kernel<128, false>),
+           kGroups * kThreads);
   }
   return hipGetLastError() == hipSuccess ? LUMEN_OK : LUMEN_ERR_HIP;
 }
