@@ -697,11 +697,25 @@ constexpr int kMaxUnits = 256;
 // Places of a request from which on tiles may be cut.
 constexpr int kCutKeys = 1024;
 
+// Wavefronts of a workgroup.  Eight share a tile of places among twice the rows and
+// keep two more tiles under way, one workgroup a compute unit: a chunk of 2,048 tokens
+// behind 14,336 (32 query heads over 8, D 128) takes 507 us against 543, a prompt of
+// 4,096 157 against 173, 4 chunks of 2,048 behind 4,096 664 against 711.  Four leave
+// fewer lanes idle and spread what does not fill the chip evenly: 405 against 419 for
+// 3,000 behind 6,000 (12,000 rows a head: not looked at here), and at D 64, where three
+// of them share a compute unit, 848 against 1,206 for 2,300 behind 30,000.
+int attend_waves(const lumen_kv_layout *l, int32_t num_reqs, int64_t num_q, int group) {
+  const int64_t rows = num_q * group;
+  const bool long_ones = rows >= int64_t(num_reqs) * 4096;
+  const bool many = rows / (8 * 32) * l->num_kv_heads >= kMaxUnits;
+  return l->head_dim == 128 && long_ones && many ? 8 : 4;
+}
+
 AttendPlan attend_plan(const lumen_kv_layout *l, int64_t cap, int32_t num_reqs, int64_t num_q,
                        int32_t max_new, int32_t q_heads, int cus) {
   AttendPlan p;
   const int group = q_heads / l->num_kv_heads;
-  p.waves = 4;
+  p.waves = attend_waves(l, num_reqs, num_q, group);
   p.tile_rows = 32 * p.waves;
   const auto slots = [&](int units) {
     const int n = units * 8 / p.waves / l->num_kv_heads;
@@ -816,7 +830,9 @@ int lumen_paged_attend(const lumen_kv_layout *layout, int32_t layer, const void 
   a.parts = reinterpret_cast<float *>(ws + p.parts_at);
   const bool bf = dtype == LUMEN_ATTN_BF16;
   const int D = layout->head_dim;
-  const AttendKernels kernels = D == 64 ? attend_kernels<64, 4>(bf) : attend_kernels<128, 4>(bf);
+  const AttendKernels kernels = D == 64        ? attend_kernels<64, 4>(bf)
+                                : p.waves == 4 ? attend_kernels<128, 4>(bf)
+                                               : attend_kernels<128, 8>(bf);
   const dim3 threads(unsigned(p.waves * kWave));
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (p.planned)

@@ -194,6 +194,9 @@ __global__ __launch_bounds__(kGroups *kThreads, 4) void weigh_kernel(WeighArgs a
         shifts[i] = shift_of(lse[int64_t(tok) * a.q_heads + h * a.group + hd]);
       }
       __syncthreads();
+      // the keys are here before the first rows' loads, which the compiler does not
+      // count, so that no wait for them is left in the loop
+      __builtin_amdgcn_s_waitcnt(0x0f70);
 #pragma unroll
       for (int i = 0; i < kStages - 1; ++i)
         if (i < count) load_next(i);
@@ -326,21 +329,7 @@ __global__ __launch_bounds__(kThreads, 2) void weigh_few_kernel(WeighArgs a) {
     if (q.m == 0 || first >= n) continue;
     const int count = n - first < a.chunk ? n - first : a.chunk;
     const int steps = (count + kPlaces - 1) / kPlaces;
-    // ---- where the places are, and what they weigh
     __syncthreads();  // the item before is done with the tables and tiles
-    err = LUMEN_OK;
-    for (int i = tid; i < steps * kPlaces; i += kThreads) {
-      const Slot s = slot_of(a, r, first + i, n, &err);
-      const uint64_t live = __ballot(s.in);
-      if (lane == 0) live_at[i / 64] = live;
-      const int64_t word = s.word + int64_t(h) * a.block_size;
-      if (in_run(i) == 0) {
-        run_row[i >> run_shift] = s.row;
-        run_word[i >> run_shift] = word;
-      }
-      weights[i] = s.in ? a.weights[word] : 0.0f;
-    }
-    if (h == 0) record_wave(a.status, err);
     // ---- the queries
     const int rows = q.m * a.group, behind = q.n - q.m;
     frag8 x[kTiles][D / 32];
@@ -359,6 +348,19 @@ __global__ __launch_bounds__(kThreads, 2) void weigh_few_kernel(WeighArgs a) {
       shift[t] = shift_of(a.lse[(int64_t(q.q0) + tok) * a.q_heads + head]);
       limit[t] = at < rows ? behind + tok : -1;
     }
+    // ---- where the places are
+    err = LUMEN_OK;
+    for (int i = tid; i < steps * kPlaces; i += kThreads) {
+      const Slot s = slot_of(a, r, first + i, n, &err);
+      const uint64_t live = __ballot(s.in);
+      if (lane == 0) live_at[i / 64] = live;
+      const int64_t word = s.word + int64_t(h) * a.block_size;
+      if (in_run(i) == 0) {
+        run_row[i >> run_shift] = s.row;
+        run_word[i >> run_shift] = word;
+      }
+    }
+    if (h == 0) record_wave(a.status, err);
     __syncthreads();
     const uint8_t *const kb = a.k + int64_t(h) * a.head_bytes;
     const auto load = [&](int step, int buf) __attribute__((always_inline)) {
@@ -382,12 +384,17 @@ __global__ __launch_bounds__(kThreads, 2) void weigh_few_kernel(WeighArgs a) {
         load_row(from[i] + 16 * ((tid % kChunks) ^ swizzle_k<D>((i * kThreads + tid) / kChunks)),
                  lds_at + buf * kTile + i * kThreads * 16);
     };
-    // the queries are here before the first keys' loads, which the compiler does not
-    // count, so that no wait for them is left in the loop
-    __builtin_amdgcn_s_waitcnt(0x0f70);
 #pragma unroll
     for (int i = 0; i < kStages - 1; ++i)
       if (i < steps) load(i, i);
+    // what the places weigh, beside the first keys
+    for (int i = tid; i < steps * kPlaces; i += kThreads)
+      weights[i] = live_at[i / 64] >> (i % 64) & 1
+                       ? a.weights[run_word[i >> run_shift] + in_run(i)]
+                       : 0.0f;
+    // the compiler's own loads are here before the loop, so that no wait for them is
+    // left in it
+    __builtin_amdgcn_s_waitcnt(0x0f70);
     int buf = 0;
     for (int step = 0; step < steps; ++step) {
       const int after = steps - 1 - step;  // steps loaded after this one

@@ -258,6 +258,28 @@ def test_attend_without_lse_without_requests_or_tokens():
     c.check()
 
 
+@pytest.mark.parametrize("n,m,H,G", [([5000], [4100], 16, 1),
+                                     ([2100, 2300], [2100, 2200], 16, 2),
+                                     ([9000], [2050], 4, 8)])
+@pytest.mark.parametrize("dtype", [BF, FP])
+def test_attend_large_tiles(n, m, H, G, dtype):
+    """Rows enough for workgroups of eight wavefronts."""
+    Case(n, m, H, G, 128, seed=n[0], dtype=dtype).check(max_new=max(m))
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+def test_attend_large_tiles_with_values_that_are_not_finite(dtype):
+    c = Case([4200], [4100], 16, 1, 128, dtype=dtype, seed=2)
+    base, _, _ = c.attend()
+    rows = ref.by_slot(c.cache, c.sh, c.nb)
+    j = 3000  # seen by the last 1,200 queries
+    rows[0, 1, int(c.table[0, j // 16]), j % 16, 3, 9] = float("inf")
+    got, _, _ = c.attend()
+    want = base.clone()
+    want[j - 100:, 3, 9] = float("inf")
+    assert torch.equal(got, want)
+
+
 @pytest.mark.parametrize("dtype", [BF, FP])
 @pytest.mark.parametrize("m", [1, 5, 70])
 def test_attend_hidden_values_that_are_not_finite(dtype, m):
