@@ -16,6 +16,8 @@ using namespace lumen_paged_detail;
 
 constexpr int kRowThreads = 256;
 
+typedef uint32_t piece __attribute__((ext_vector_type(4)));  // 16 bytes of a row
+
 struct AppendArgs {
   uint8_t *k, *v;  // of the layer
   Rows rk, rv;
@@ -26,6 +28,7 @@ struct AppendArgs {
   int64_t page;
   int32_t slot_bytes, head_bytes;
   int32_t block_size, heads;
+  Divisor by_block;  // block_size
   uint32_t tokens;
   uint32_t at_once;  // tokens that the grid takes at a time
   int32_t *status;
@@ -50,25 +53,37 @@ __global__ __launch_bounds__(kRowThreads) void append_kernel(AppendArgs a) {
   uint8_t *const cached = (is_v ? a.v : a.k) + int64_t(h) * a.head_bytes + lane * 16;
   if (t >= a.at_once) t = a.tokens;  // past the last whole token
   int err = LUMEN_OK;
-  for (; t < a.tokens; t += a.at_once, row += step) {
-    const int64_t slot = a.slots[t];
+  const auto store = [&](uint32_t tok, int64_t slot, const piece &x)
+      __attribute__((always_inline)) {
     if (slot < 0 || slot >= a.slot_limit) {
       if (slot >= 0) err = LUMEN_ERR_BLOCK_ID;
-      continue;
+      return;
     }
-    const uint4 x = *reinterpret_cast<const uint4 *>(row);
-    const int64_t block = slot <= UINT32_MAX
-                              ? int64_t(uint32_t(slot) / uint32_t(a.block_size))
-                              : slot / a.block_size;
-    const int32_t at = int32_t(slot - block * a.block_size);
-    *reinterpret_cast<uint4 *>(cached + block * a.page + int64_t(at) * a.slot_bytes) = x;
+    int at;
+    int64_t block;
+    if (slot <= INT32_MAX) {
+      block = quotient(a.by_block, int(slot), &at);
+    } else {
+      block = slot / a.block_size;
+      at = int32_t(slot - block * a.block_size);
+    }
+    *reinterpret_cast<piece *>(cached + block * a.page + int64_t(at) * a.slot_bytes) = x;
     if (lane == 0 && a.weights) {
       const int64_t word = (block * a.heads + h) * a.block_size + at;
       if (is_v)
-        a.places[word] = a.positions[t];
+        a.places[word] = a.positions[tok];
       else
         a.weights[word] = 0;
     }
+  };
+  // two tokens at a time, their rows read beside their slots
+  for (; t < a.tokens; t += 2 * a.at_once, row += 2 * step) {
+    const bool two = a.tokens - t > a.at_once;
+    const int64_t slot0 = a.slots[t], slot1 = two ? a.slots[t + a.at_once] : -1;
+    const piece x0 = *reinterpret_cast<const piece *>(row);
+    const piece x1 = *reinterpret_cast<const piece *>(two ? row + step : row);
+    store(t, slot0, x0);
+    store(t + a.at_once, slot1, x1);
   }
   record_wave(a.status, err);
 }
@@ -126,7 +141,6 @@ __device__ __forceinline__ Item item_of(const EvictArgs &a, int64_t i) {
 // Moves `count` places of one layer, request and head, at most 64: lane l knows where
 // the l-th goes and where it is.  Rows of K and V go 16 bytes a lane, the ledger's
 // words by the lane itself.  No place is both read and written.
-typedef uint32_t piece __attribute__((ext_vector_type(4)));  // 16 bytes of a row
 template <int D>
 __device__ __forceinline__ void move_places(const EvictArgs &a, const Item &it, int to, int src,
                                             int count) {
@@ -717,6 +731,7 @@ int lumen_paged_append(const lumen_kv_layout *layout, int32_t layer, void *d_cac
   a.slot_bytes = p.slot;
   a.head_bytes = p.head;
   a.block_size = layout->block_size;
+  a.by_block = divisor(a.block_size);
   a.heads = layout->num_kv_heads;
   a.weights = d_ledger ? static_cast<int32_t *>(d_ledger) + 2 * layer * ledger_words(layout)
                        : nullptr;
