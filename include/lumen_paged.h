@@ -50,8 +50,9 @@
  *
  * Arithmetic.  Scores, their maxima, all sums, lse and the ledger's weights
  * are held in 32 bits.  attend rounds its weights to the type of the inputs for
- * the products with V (one part in 2^9 or 2^12 each); the sum they are divided by
- * is taken before that.  weigh rounds nothing but its sums.
+ * the products with V (one part in 2^9 or 2^12 each).  The sum that rows are
+ * divided by is of the weights before that in bf16 and after it in fp16; lse's is
+ * before.  weigh rounds nothing but its sums.
  */
 #ifndef LUMEN_PAGED_H
 #define LUMEN_PAGED_H

@@ -371,6 +371,36 @@ def test_attend_large_scores():
     c.check()
 
 
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("m", [1, 3, 60])
+@pytest.mark.parametrize("n", [400, 16000])
+@pytest.mark.parametrize("down", [9, 21, 23, 30])
+def test_attend_many_small_weights_beside_a_large_one(dtype, m, n, down):
+    """One place's score is `down` powers of two over all the others': their
+    weights, some of which round to subnormals, count in the sum as in the
+    products.  (The others' values are ones, the large one's are zeros.)"""
+    c = Case([n], [m], 1, 2, 64, dtype=dtype, seed=1)
+    c.q[:] = 0
+    c.q[:, :, 0] = 1
+    rows = ref.by_slot(c.cache, c.sh, c.nb)
+    keep = rows.isfinite()
+    rows[0, 0] = torch.where(keep[0, 0], 0.0, rows[0, 0])
+    rows[0, 1] = torch.where(keep[0, 1], 1.0, rows[0, 1])
+    b, o = int(c.table[0, 5]), 3
+    rows[0, 0, b, o, 0, 0] = down
+    rows[0, 1, b, o] = 0
+    out, lse, _ = c.attend(scale=math.log(2.0))
+    last = out[-1].double()
+    rest = (n - 1) * 2.0 ** -down
+    want = rest / (1 + rest)
+    # a weight of 2^-down of the largest has an absolute rounding of at most
+    # 2^-25 in fp16's subnormals, at 2^7 of them or more for the largest one
+    lost = 2.0 ** (down - 32) if dtype == FP else 0.0
+    assert ((last / want - 1).abs() <= 2 * UNIT[dtype] + lost + 2.0 ** -14).all()
+    full = math.log(2.0) * down + math.log1p(rest)
+    assert ((lse[-1].double() - full).abs() <= 2.0 ** -14 + 2.0 ** -22 * full).all()
+
+
 def test_attend_repeats_itself():
     c = Case([4000, 3000, 100, 900, 7], [200, 1, 100, 3, 7], 2, 4, 128, seed=14)
     a, la, _ = c.attend()
