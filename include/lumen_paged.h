@@ -40,7 +40,7 @@
  * to the most negative code seen while everything else is still computed.  No
  * call clears memory with a memset, so all can be captured in a graph.  A
  * workspace is not shared by calls in flight at the same time; what it holds
- * does not matter.  Results do not depend on timing.
+ * does not matter.  Results do not overlap what a call reads.  Results do not depend on timing.
  *
  * A block that two requests' tables name (a shared prefix) can be attended to
  * by both; weigh, evict and release need the blocks of a call's requests to be
@@ -163,8 +163,8 @@ size_t lumen_paged_evict_workspace_bytes(const lumen_kv_layout *layout,
  * the larger weight first (NaN after everything, 0 and -0 alike), then the lower
  * place.  The kept places from d_keep[r] on move into the places under it that
  * were given up, the lowest into the lowest: rows of K and V and both words of the
- * ledger.  What lies behind is left as it is.  d_left[r]: min(n, d_keep[r]), which
- * must not overlap the inputs.  head_dim 64, 128 or 256; block_size * bt_cols at most
+ * ledger.  What lies behind is left as it is.  d_left[r]: min(n, d_keep[r]);
+ * INVALID_ARG where it overlaps d_lens, d_keep, d_recent_from or the tables.  head_dim 64, 128 or 256; block_size * bt_cols at most
  * LUMEN_PAGED_MAX_PLACES.
  *
  * A request is left alone, with d_left[r] = d_lens[r], where n or d_keep[r] is
@@ -188,7 +188,8 @@ int lumen_paged_evict(const lumen_kv_layout *layout, int32_t first_layer,
  * Blocks past free_cap are not written and not counted (CAPACITY); a request with
  * lens < 0, have < 0 or pages past bt_cols gives none back (RANGE); an id outside
  * [0, num_blocks) goes to the list as it is (BLOCK_ID).  num_reqs at most
- * LUMEN_ATTN_MAX_REQS (TOO_MANY).  d_free_now must not overlap the inputs. */
+ * LUMEN_ATTN_MAX_REQS (TOO_MANY).  INVALID_ARG where d_free_now overlaps another
+ * argument. */
 int lumen_paged_release(const int32_t *d_lens, const int32_t *d_have,
                         int32_t num_reqs, const int32_t *d_block_tables,
                         int32_t bt_cols, int32_t block_size,

@@ -796,6 +796,12 @@ int lumen_paged_evict(const lumen_kv_layout *layout, int32_t first_layer, int32_
       !aligned(d_block_tables, 4) || !aligned(d_lens, 4) || !aligned(d_keep, 4) ||
       !aligned(d_recent_from, 4) || !aligned(d_left, 4))
     return LUMEN_ERR_MISALIGNED;
+  // workgroups read these while others write d_left
+  const size_t words = size_t(num_reqs) * sizeof(int32_t);
+  if (overlap(d_left, words, d_lens, words) || overlap(d_left, words, d_keep, words) ||
+      overlap(d_left, words, d_recent_from, words) ||
+      overlap(d_left, words, d_block_tables, words * size_t(bt_cols)))
+    return LUMEN_ERR_INVALID_ARG;
   (void)hipGetLastError();
   EvictArgs a;
   a.words = ledger_words(layout);
@@ -866,6 +872,13 @@ int lumen_paged_release(const int32_t *d_lens, const int32_t *d_have, int32_t nu
   if (!aligned(d_lens, 4) || !aligned(d_have, 4) || !aligned(d_block_tables, 4) ||
       !aligned(d_free, 4) || !aligned(d_free_count, 8) || !aligned(d_free_now, 8))
     return LUMEN_ERR_MISALIGNED;
+  // workgroups read these, or write the list, while one writes d_free_now
+  const size_t words = size_t(num_reqs) * sizeof(int32_t), now = sizeof(int64_t);
+  if (overlap(d_free_now, now, d_free_count, now) || overlap(d_free_now, now, d_lens, words) ||
+      overlap(d_free_now, now, d_have, words) ||
+      overlap(d_free_now, now, d_block_tables, words * size_t(bt_cols)) ||
+      overlap(d_free_now, now, d_free, size_t(free_cap) * sizeof(int32_t)))
+    return LUMEN_ERR_INVALID_ARG;
   int cus = 0;
   if ((st = compute_units(&cus)) != LUMEN_OK) return st;
   (void)hipGetLastError();

@@ -115,6 +115,12 @@ struct Call {
   int32_t *status;
 };
 
+// Whether two ranges of bytes share some.
+inline bool overlap(const void *a, size_t a_bytes, const void *b, size_t b_bytes) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return a_bytes && b_bytes && (x < y ? y - x < a_bytes : x - y < b_bytes);
+}
+
 // So that a step's places are counted in 32 bits.
 constexpr int64_t kMostPlaces = INT32_MAX - 255;
 

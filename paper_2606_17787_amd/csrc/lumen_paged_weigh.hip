@@ -89,7 +89,7 @@ __device__ __forceinline__ Slot slot_of(const Call &a, int r, int place, int n, 
   return s;
 }
 
-// ------------------------------------------------- more than 32 query rows
+// ------------------------------------------------- more than 128 query rows
 
 constexpr int kGroups = 2;    // of four wavefronts
 constexpr int kRows = 32 * kGroups;  // query rows of a tile
@@ -496,7 +496,7 @@ int lumen_paged_weigh(const lumen_kv_layout *layout, int32_t layer, const void *
   const int D = layout->head_dim;
   hipStream_t s = static_cast<hipStream_t>(stream);
   const auto launch = [&](void (*kernel)(WeighArgs), int threads) {
-    a.chunks = (a.cap + a.chunk - 1) / a.chunk;
+    a.chunks = int32_t((uint32_t(a.cap) + uint32_t(a.chunk) - 1) / uint32_t(a.chunk));
     if (a.chunks < 1) a.chunks = 1;  // which looks at the requests
     int64_t groups = int64_t(num_reqs) * a.chunks;
     groups = groups < kMostGroups / a.kv_heads ? groups * a.kv_heads : kMostGroups;
@@ -506,9 +506,6 @@ int lumen_paged_weigh(const lumen_kv_layout *layout, int32_t layer, const void *
   if (rows <= 128) {
     const int low = a.block_size & -a.block_size;
     a.chunk = kEntries * (low < 16 ? low : 16);
-#ifdef CH
-    if (a.chunk > CH) a.chunk = CH;
-#endif
     if (a.chunk > kMostPlaces16) a.chunk = kMostPlaces16;
     launch(rows <= 16 ? few_kernel<1>(D, bf) : rows <= 64 ? few_kernel<4>(D, bf)
                                                           : few_kernel<8>(D, bf),

@@ -253,6 +253,42 @@ def test_caches_past_32_bits(order):
     assert left.tolist() == [40, 30] and int(status) == 0
 
 
+@pytest.mark.parametrize("m", [2, 200])
+def test_tables_of_as_many_places_as_32_bits_count(m):
+    """2,048 pages of 2^20 places each, of which one is there."""
+    sh = CacheShape(1, 1, 64, 1 << 20, NHD)
+    cache = torch.zeros(sh.pool_elems(1), dtype=BF, device=dev())
+    n, cu = 2500, [0, m]
+    g = gen(8)
+    k, v = (torch.randn(n, 1, 64, generator=g, device=dev()).to(BF)
+            for _ in range(2))
+    q = torch.randn(m, 2, 64, generator=g, device=dev()).to(BF)
+    ledger = torch.zeros(paged.ledger_dims(sh, 1), dtype=torch.int32,
+                         device=dev())
+    status, out = word(), torch.empty_like(q)
+    lse = torch.empty(m, 2, device=dev())
+    table = np.full((1, 2048), -1, np.int32)
+    table[0, 0] = 0
+    every = torch.arange(n, device=dev())
+    paged.lumen_paged_append(sh, 1, 0, cache, k, v, every, status,
+                             ledger=ledger, positions=every.to(torch.int32))
+    args = (sh, 1, 0, cache, i32(table), i32([n]), i32(cu), q)
+    paged.lumen_paged_attend(*args, out, status, lse=lse)
+    paged.lumen_paged_weigh(*args, lse, ledger, status)
+    # the definitions, over a cache of pages of 25 that holds the same
+    small = CacheShape(1, 1, 64, 25, NHD)
+    pool = torch.zeros(small.pool_elems(100), dtype=BF, device=dev())
+    rows = ref.by_slot(pool, small, 100)
+    rows[0, 0] = k.view(100, 25, 1, 64)
+    rows[0, 1] = v.view(100, 25, 1, 64)
+    places = np.arange(100, dtype=np.int32)[None]
+    want, slack = ref.weighed(q, lse, pool, small, 100, places, [n], cu,
+                              torch.zeros(100, 1, 25, device=dev()))
+    close(paged.weights_of(ledger)[0, 0, 0, :n], want.flatten(),
+          slack.flatten(), 0.0, "weights")
+    assert int(status) == 0 and not paged.weights_of(ledger)[0, 0, 0, n:].any()
+
+
 def test_more_requests_than_lanes_and_errors_among_the_last():
     for max_new in (1, 4):
         n = [20] * 200

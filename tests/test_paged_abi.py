@@ -205,6 +205,35 @@ def test_release_refusals(lib):
         assert call(**kw) == kv.LUMEN_ERR_MISALIGNED, kw
 
 
+def apart(*names):
+    return {name: FAKE + (i << 20) for i, name in enumerate(names)}
+
+
+@pytest.mark.parametrize("name,bytes_", [("lens", 8), ("keep", 8), ("frm", 8),
+                                         ("bt", 32)])
+@pytest.mark.parametrize("by", ["all", "first", "last"])
+def test_evict_refuses_results_among_its_inputs(lib, name, bytes_, by):
+    """Other workgroups read the inputs while d_left is written."""
+    at = apart("cache", "ledger", "bt", "lens", "keep", "frm", "left", "ws",
+               "status")
+    at["left"] = at[name] + {"all": 0, "first": -4, "last": bytes_ - 4}[by]
+    assert lib.lumen_paged_evict(
+        layout(), 0, 2, at["cache"], at["ledger"], at["bt"], 4, at["lens"],
+        at["keep"], at["frm"], 0, 2, at["left"], at["ws"], 1 << 16,
+        at["status"], None) == BAD
+
+
+@pytest.mark.parametrize("name,bytes_", [("lens", 8), ("have", 8),
+                                         ("count", 8), ("bt", 32),
+                                         ("free", 64)])
+def test_release_refuses_its_count_among_its_inputs(lib, name, bytes_):
+    at = apart("lens", "have", "bt", "free", "count", "now", "status")
+    for now in (at[name], at[name] + bytes_ - 8):
+        assert lib.lumen_paged_release(
+            at["lens"], at["have"], 2, at["bt"], 4, 16, 8, at["free"],
+            at["count"], 16, now, at["status"], None) == BAD
+
+
 def test_binding_refuses_host_tensors_and_shapes():
     sh = CacheShape(2, 2, 128, 16, NHD)
     cache = torch.zeros(sh.pool_elems(2), dtype=torch.bfloat16)
