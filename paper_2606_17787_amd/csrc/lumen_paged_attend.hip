@@ -104,7 +104,9 @@ __device__ __forceinline__ Unit find_tile(const AttendArgs &a, int rank) {
   return found;
 }
 
-// Tiles are cut into parts of at least this many places.
+// Tiles are cut into parts of at least this many places.  With 256, 512 and 1,024 a
+// single token (32 query heads over 8) behind 2,000 takes 22.7, 26.2 and 51.1 us, behind
+// 16,000 55.8, 40.5 and 41.5.
 constexpr int kMinPartKeys = 512;
 
 // The plan: every tile by falling work, so that the long ones start first and the
@@ -168,9 +170,14 @@ __global__ __launch_bounds__(kPlanThreads) void attend_plan_kernel(AttendArgs a)
     tiles_to[i] = int(to < a.num_units ? to : a.num_units);
   }
   __syncthreads();
-  // more steps than this: a cut into parts of `part` steps or a little less
+  // More steps than twice `part`: a cut into parts of `part` steps or a little less.
+  // At 5/8 of a share no part is long when the last ones run, at 1/2 even work is cut
+  // that needs no cut.  For 1/2, 5/8, 3/4 and 1: 64 requests around 4,096 places with 5
+  // tokens each 255, 242, 253 and 295 us, chunks of 512 among 96 requests 128, 124, 128
+  // and 139, a chunk of 2,048 behind 14,336 592, 511, 511 and 511.  A cut from 1.5 times
+  // `part` on would cost the chunks 4 % and the long one 28 %.
   const uint64_t share = sum / uint32_t(a.slots);
-  const int most = share < 0x1fffffff ? int(share * 3 / 4) + 1 : 0x1fffffff;
+  const int most = share < 0x1fffffff ? int(share * 5 / 8) + 1 : 0x1fffffff;
   const int part = most > kMinPartKeys / kKeys ? most : kMinPartKeys / kKeys;
   const int whole = a.max_parts ? 2 * part : 0x7fffffff;
   // a bin of work, the most in bin 0
@@ -720,7 +727,10 @@ struct AttendPlan {
 // its size needs no device.
 constexpr int kMaxUnits = 256;
 
-// Places of a request from which on tiles may be cut.
+// Places of a request from which on tiles may be cut.  That takes two more kernels, of
+// 12 us together: single tokens of 1 request with 1,100, 1,500 and 2,000 places take 24,
+// 26 and 26 us with them and 28, 35 and 44 without, of 16 requests 30 and 39 against 29
+// and 46 (1,100, 2,000), of 100 requests with 2,000 each 172 against 170.
 constexpr int kCutKeys = 1024;
 
 // Wavefronts of a workgroup.  Eight share a tile of places among twice the rows and
@@ -752,8 +762,8 @@ AttendPlan attend_plan(const lumen_kv_layout *l, int64_t cap, int32_t num_reqs, 
   p.tiles = num_q * group / p.tile_rows + (num_reqs < num_q ? num_reqs : num_q);
   p.parts = 0;
   if (cap >= kCutKeys) {
-    // a cut tile has less than twice its steps over `part`'s parts, and `part` is
-    // at least three quarters of a slot's share of all steps
+    // a cut tile has fewer parts than one and a half times its steps over `part`, and
+    // `part` is at least five eighths of a slot's share of all steps: 2.4 for each slot
     p.parts = int64_t(p.slots) * 4;
     const int64_t most = p.tiles * (cap / kMinPartKeys + 2);
     if (p.parts > most) p.parts = most;
