@@ -36,7 +36,8 @@ struct AppendArgs {
 
 // Rows of K and V as they are, 16 bytes a lane, D/8 lanes a row; a lane keeps its
 // head of K or V for all of its tokens.  Bound by bytes: 4 D a token and head in
-// and as many out.
+// and as many out.  16,411 tokens of 8 heads with D 128 take 30 us, 4.5 TB/s, 256 take 4,
+// of which the launch and two dependent reads are all.
 template <int D>
 __global__ __launch_bounds__(kRowThreads) void append_kernel(AppendArgs a) {
   constexpr uint32_t kLanes = D / 8, kRows = kRowThreads / kLanes;
@@ -198,6 +199,11 @@ __device__ __forceinline__ void move_places(const EvictArgs &a, const Item &it, 
 // Where places move, the k-th place given up and the k-th one kept behind the budget
 // belong together.  D is 0 where evict_move_kernel moves them; otherwise this
 // workgroup does, with the two lists in LDS.
+//
+// Bound by what comes one after the other in a workgroup: the table, the words, two or
+// three digits' counts, the lists, the rows.  64 requests of 2,064 places, 2,048 of them
+// kept, in four layers of 8 heads: 41 us with the moves, for 34 MB of words and 17 MB of
+// rows.  16 prompts around 8,192 tokens to 1,024 in two layers: 76 us.
 template <int kThreads, int kPer, int D>
 __global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictArgs a) {
   constexpr int kWaves = kThreads / kWave;
@@ -555,9 +561,19 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a, i
 // A launch takes less than 2^32 threads.
 constexpr int64_t kMostItems = UINT32_MAX / 1024;
 
-// Places of a request up to which a thread of 1,024 holds its ranks, and counts of
-// (layer, request, head) from which on their workgroups move the places themselves.
-constexpr int kHeldPlaces = 1024 * 32, kMovingItems = 512;
+// Places of a request up to which a thread of 1,024 holds its ranks: 16 prompts around
+// 8,192 tokens take 114 us against 178 where each pass reads them again.
+constexpr int kHeldPlaces = 1024 * 32;
+
+// Counts of (layer, request, head) from which on their workgroups move the places
+// themselves.  With fewer, the moves of one take longer than a second kernel over the
+// whole chip.  In us, with the ledger's restoring copy, together against apart:
+//     items              64       128       256       512
+//     4,096 -> 1,024    35/37    46/54     67/100   115/180
+//     16,000 -> 2,048   85/94   107/157
+//     16,000 -> 8,000  159/114  188/181   291/323
+//     32,000 -> 4,096  165/121  196/172   292/293
+constexpr int kMovingItems = 128;
 
 struct EvictPlan {
   int32_t strips;
@@ -586,6 +602,11 @@ int evict_plan(const lumen_kv_layout *l, int32_t layers, int32_t bt_cols, int32_
   return LUMEN_OK;
 }
 
+// Threads, and how many places each holds, for requests of up to `cap` places: small
+// workgroups share a compute unit, so that one counts while another waits.  With the
+// ledger's restoring copy, 256 threads take 54 us for 64 requests of 2,064 places in
+// four layers of 8 heads, 1,024 threads of 8 places 115 and of 32 places 175; for 8
+// requests of 4,096 in eight layers 116, 118 and 132.
 template <int D>
 void (*select_kernel(int64_t cap, int *threads))(EvictArgs) {
   *threads = cap <= 256 * 16 ? 256 : 1024;
@@ -626,7 +647,7 @@ __device__ __forceinline__ int32_t pages_of(int32_t places, int32_t bs) {
 
 // Every workgroup sums up the requests' pages in LDS (no second launch), then the
 // grid strides over the pages that go back, each of which finds its request by
-// bisection.
+// bisection.  5 us for 64 requests and for 16 prompts' 7,000 pages: launch and latency.
 __global__ __launch_bounds__(kReleaseThreads) void release_kernel(ReleaseArgs a) {
   extern __shared__ int64_t upto[];  // pages of the requests up to each, with it
   __shared__ int64_t wave_sum[kReleaseThreads / kWave];
