@@ -103,7 +103,10 @@ constexpr int kChunk = 32 * kWaves;  // places of a workgroup
 // four wavefronts and 32 for the others, so that four of them share a SIMD: scores^T =
 // K Q^T, queries across, so that a lane has one query's lse.  Its weights are added up
 // by place in 32 bits, and over the lanes and the two groups at the end.  A tile's
-// 16-byte chunks are permuted by row as attend's keys are.
+// 16-byte chunks are permuted by row as attend's keys are.  Bound by the exponentials
+// and sums, which take as many cycles as the products they wait for: 2,048 tokens behind
+// 6,144 places (32 query heads over 8, D 128) take 162 us, 0.74 PFLOP/s; with one group of
+// wavefronts 201 against 169.
 template <int D, bool kBf16>
 __global__ __launch_bounds__(kGroups *kThreads, 4) void weigh_kernel(WeighArgs a) {
   constexpr int kChunks = D / 8;
@@ -294,7 +297,9 @@ __device__ __forceinline__ f32x4 mfma16(frag8 a, frag8 b, f32x4 c) {
 // kStages steps in turn.  Where the places' rows start is laid out in LDS before, an
 // entry for each run of places that cannot leave its page, as attend has it, and so are
 // the weights that the places have; they are written back at the end.  Bound by the
-// keys' bytes.
+// keys' bytes: 256 tokens behind around 2,048 places each (8 KV heads, D 128) take 310 us,
+// 4.6 TB/s.  Writing the weights back is about 50 of them: each write is 64 bytes of
+// another page.
 template <int D, bool kBf16, int kTiles>
 __global__ __launch_bounds__(kThreads, 2) void weigh_few_kernel(WeighArgs a) {
   constexpr int kChunks = D / 8;
@@ -445,6 +450,13 @@ void (*few_kernel(int head_dim, bool bf16))(WeighArgs) {
   return bf16 ? weigh_few_kernel<128, true, kTiles> : weigh_few_kernel<128, false, kTiles>;
 }
 
+// Query rows up to which a wavefront holds them all (weigh_few_kernel, in 1, 4 or 8
+// tiles of 16).  Of 16 prompts around 4,096 tokens 32, 64 and 128 rows take 41, 47 and 65
+// us so and 93, 94 and 100 in weigh_kernel, of one with 16,384 tokens 128 rows take 22 and
+// 22.  In 8 tiles always, 32 and 64 rows take 43 and 50 us, and 4 rows of 256 requests
+// around 2,048 places 319 against 311.
+constexpr int kFewRows = 128;
+
 // Workgroups of a launch at most: more than run at once, and few enough that their
 // threads are counted in 32 bits.
 constexpr int64_t kMostGroups = 1 << 22;
@@ -485,6 +497,8 @@ int lumen_paged_weigh(const lumen_kv_layout *layout, int32_t layer, const void *
   if (lumen_paged_weigh_workspace_bytes(layout, bt_cols, num_reqs, num_tokens, max_new,
                                         num_q_heads) > (d_workspace ? workspace_bytes : 0))
     return LUMEN_ERR_INVALID_ARG;
+  int cus = 0;
+  if ((st = compute_units(&cus)) != LUMEN_OK) return st;
   (void)hipGetLastError();
   WeighArgs a;
   static_cast<Call &>(a) =
@@ -503,10 +517,17 @@ int lumen_paged_weigh(const lumen_kv_layout *layout, int32_t layer, const void *
     hipLaunchKernelGGL(kernel, dim3(unsigned(groups)), dim3(unsigned(threads)), 0, s, a);
   };
   const int64_t rows = int64_t(max_new) * a.group;
-  if (rows <= 128) {
+  if (rows <= kFewRows) {
     const int low = a.block_size & -a.block_size;
     a.chunk = kEntries * (low < 16 ? low : 16);
     if (a.chunk > kMostPlaces16) a.chunk = kMostPlaces16;
+    // Smaller stretches where these would not fill the chip: one token behind 1,000 and
+    // 16,384 places 5.7 and 11.2 us against 13.2 and 14.0, 32 tokens of 4 requests with
+    // 8,000 places 25.7 against 28.6.  (256 requests around 2,048 places take 383 us in
+    // stretches of 256, 331 of 512, 310 of 1,024 and 311 of 2,048.)
+    while (a.chunk > kEntries &&
+           int64_t(num_reqs) * a.kv_heads * ((int64_t(a.cap) + a.chunk - 1) / a.chunk) < 2 * cus)
+      a.chunk /= 2;
     launch(rows <= 16 ? few_kernel<1>(D, bf) : rows <= 64 ? few_kernel<4>(D, bf)
                                                           : few_kernel<8>(D, bf),
            kThreads);
