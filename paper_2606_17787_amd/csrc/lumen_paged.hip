@@ -202,8 +202,8 @@ __device__ __forceinline__ void move_places(const EvictArgs &a, const Item &it, 
 //
 // Bound by what comes one after the other in a workgroup: the table, the words, two or
 // three digits' counts, the lists, the rows.  64 requests of 2,064 places, 2,048 of them
-// kept, in four layers of 8 heads: 41 us with the moves, for 34 MB of words and 17 MB of
-// rows.  16 prompts around 8,192 tokens to 1,024 in two layers: 76 us.
+// kept, in four layers of 8 heads: 41 us with the moves, for 34 MB of words and as many
+// of rows.  16 prompts around 8,192 tokens to 1,024 in two layers: 76 us.
 template <int kThreads, int kPer, int D>
 __global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictArgs a) {
   constexpr int kWaves = kThreads / kWave;

@@ -357,6 +357,11 @@ constexpr int kEntries = 1024; // runs of rows among them
 // weight 0 keeps a hidden value out of the products unless it is an infinity or NaN.
 // Such values are taken out of the tile in LDS there, and the rows that had some are
 // added to the queries that see them.
+//
+// Bound by the cache's bytes where a request has few new tokens: 256 of one around 2,048
+// places (32 query heads over 8, D 128, bf16) take 500 us, 5.5 TB/s.  Bound by the
+// products with the maxima, exponentials and roundings between them where it has many: a
+// chunk of 2,048 behind 14,336 takes 492 to 515 us, 1.0 PFLOP/s.
 template <int D, bool kBf16, int kWaves>
 __global__ __launch_bounds__(kWaves *kWave, 2) void attend_kernel(AttendArgs a) {
   using S = TileShape<D, kWaves>;
