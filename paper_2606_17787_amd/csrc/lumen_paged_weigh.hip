@@ -105,8 +105,8 @@ constexpr int kChunk = 32 * kWaves;  // places of a workgroup
 // by place in 32 bits, and over the lanes and the two groups at the end.  A tile's
 // 16-byte chunks are permuted by row as attend's keys are.  Bound by the exponentials
 // and sums, which take as many cycles as the products they wait for: 2,048 tokens behind
-// 6,144 places (32 query heads over 8, D 128) take 162 us, 0.74 PFLOP/s; with one group of
-// wavefronts 201 against 169.
+// 6,144 places (32 query heads over 8, D 128) take 157 us, 0.77 PFLOP/s; with one group of
+// wavefronts 201 against 169, and 167 with rows' addresses and ends looked at one by one.
 template <int D, bool kBf16>
 __global__ __launch_bounds__(kGroups *kThreads, 4) void weigh_kernel(WeighArgs a) {
   constexpr int kChunks = D / 8;
@@ -140,10 +140,13 @@ __global__ __launch_bounds__(kGroups *kThreads, 4) void weigh_kernel(WeighArgs a
     const int tiles = (rows + kRows - 1) / kRows - first;
     const uint16_t *const qb = a.q.base + int64_t(q.q0) * a.q.token;
     const float *const lse = a.lse + int64_t(q.q0) * a.q_heads;
-    // the lane's row of each load of the next tile: its place in memory goes on by 32
-    // rows with a few additions
-    int row[kIssues], head[kIssues];
-    const uint16_t *from[kIssues], *last;
+    // where each load of the next tile reads in the lane's row: it goes on by 64 rows with
+    // one addition where whole tokens have as many, and with a few where they do not
+    int next = first, head[kIssues];
+    const uint16_t *from[kIssues];
+    const auto chunk_of = [&](int i) __attribute__((always_inline)) {
+      return 8 * ((tid % kChunks) ^ swizzle_k<D>((i * kAll + tid) / kChunks));
+    };
     const auto row_at = [&](int x, int *hd) __attribute__((always_inline)) {
       const int tok = quotient(a.by_group, x, hd);
       return qb + int64_t(tok) * a.q.token + int64_t(h * a.group + *hd) * a.q.head;
@@ -152,24 +155,33 @@ __global__ __launch_bounds__(kGroups *kThreads, 4) void weigh_kernel(WeighArgs a
     const int step_toks = quotient(a.by_group, kRows, &step_heads);
     const int64_t step = step_toks * a.q.token + step_heads * a.q.head;
     const int64_t wrap = a.q.token - a.group * a.q.head;
-    last = row_at(rows - 1, &row[0]);
+    const uint16_t *const last = row_at(rows - 1, &head[0]);
 #pragma unroll
-    for (int i = 0; i < kIssues; ++i) {
-      row[i] = first * kRows + (i * kAll + tid) / kChunks;
-      from[i] = row_at(row[i], &head[i]);
-    }
+    for (int i = 0; i < kIssues; ++i)
+      from[i] = row_at(first * kRows + (i * kAll + tid) / kChunks, &head[i]) + chunk_of(i);
     const auto load_next = [&](int stage) __attribute__((always_inline)) {
+      const uint32_t to = lds_at + stage * kTile;
+      const int left = rows - next * kRows;
+      ++next;
+      if (left >= kRows) {
 #pragma unroll
-      for (int i = 0; i < kIssues; ++i) {
-        load_row((row[i] < rows ? from[i] : last) +
-                     8 * ((tid % kChunks) ^ swizzle_k<D>((i * kAll + tid) / kChunks)),
-                 lds_at + stage * kTile + i * kAll * 16);
-        row[i] += kRows;
-        head[i] += step_heads;
-        from[i] += step;
-        if (head[i] >= a.group) {
-          head[i] -= a.group;
-          from[i] += wrap;
+        for (int i = 0; i < kIssues; ++i) load_row(from[i], to + i * kAll * 16);
+      } else {  // the last row again behind it
+#pragma unroll
+        for (int i = 0; i < kIssues; ++i)
+          load_row((i * kAll + tid) / kChunks < left ? from[i] : last + chunk_of(i),
+                   to + i * kAll * 16);
+      }
+#pragma unroll
+      for (int i = 0; i < kIssues; ++i) from[i] += step;
+      if (step_heads) {
+#pragma unroll
+        for (int i = 0; i < kIssues; ++i) {
+          head[i] += step_heads;
+          if (head[i] >= a.group) {
+            head[i] -= a.group;
+            from[i] += wrap;
+          }
         }
       }
     };
