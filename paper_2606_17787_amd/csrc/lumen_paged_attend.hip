@@ -104,10 +104,13 @@ __device__ __forceinline__ Unit find_tile(const AttendArgs &a, int rank) {
   return found;
 }
 
-// Tiles are cut into parts of at least this many places.  With 256, 512 and 1,024 a
-// single token (32 query heads over 8) behind 2,000 takes 22.7, 26.2 and 51.1 us, behind
-// 16,000 55.8, 40.5 and 41.5.
-constexpr int kMinPartKeys = 512;
+// Tiles are cut into parts of at least this many places where the parts of all run at
+// once, and at least an eighth of the longest up to twice as many; of at least twice as
+// many elsewhere.  With 256 and 512 throughout single tokens (32 query heads over 8) of 1
+// request with 2,000 places take 22.7 and 26.2 us, with 16,000 55.8 and 40.5, of 4 around
+// 1,500 26.5 and 36.7, of 16 with 2,000 47.3 and 39.3; with 1,024 the first two take 51.1
+// and 41.5.
+constexpr int kMinPartKeys = 256;
 
 // The plan: every tile by falling work, so that the long ones start first and the
 // short ones fill the end; tiles that are long beside a workgroup slot's share of
@@ -178,7 +181,10 @@ __global__ __launch_bounds__(kPlanThreads) void attend_plan_kernel(AttendArgs a)
   // `part` on would cost the chunks 4 % and the long one 28 %.
   const uint64_t share = sum / uint32_t(a.slots);
   const int most = share < 0x1fffffff ? int(share * 5 / 8) + 1 : 0x1fffffff;
-  const int part = most > kMinPartKeys / kKeys ? most : kMinPartKeys / kKeys;
+  constexpr int kMinPart = kMinPartKeys / kKeys;
+  const int eighth = share < kMinPart ? top / 8 : 2 * kMinPart;
+  const int least = eighth < kMinPart ? kMinPart : eighth < 2 * kMinPart ? eighth : 2 * kMinPart;
+  const int part = most > least ? most : least;
   const int whole = a.max_parts ? 2 * part : 0x7fffffff;
   // a bin of work, the most in bin 0
   const float scale = float(kPlanThreads - 1) / float(top + 1);
@@ -733,8 +739,8 @@ struct AttendPlan {
 constexpr int kMaxUnits = 256;
 
 // Places of a request from which on tiles may be cut.  That takes two more kernels, of
-// 12 us together: single tokens of 1 request with 1,100, 1,500 and 2,000 places take 24,
-// 26 and 26 us with them and 28, 35 and 44 without, of 16 requests 30 and 39 against 29
+// 12 us together: single tokens of 1 request with 1,100, 1,500 and 2,000 places take 23,
+// 24 and 23 us with them and 28, 35 and 44 without, of 16 requests 30 and 39 against 29
 // and 46 (1,100, 2,000), of 100 requests with 2,000 each 172 against 170.
 constexpr int kCutKeys = 1024;
 
