@@ -104,7 +104,7 @@ constexpr int kChunk = 32 * kWaves;  // places of a workgroup
 // K Q^T, queries across, so that a lane has one query's lse.  Its weights are added up
 // by place in 32 bits, and over the lanes and the two groups at the end.  A tile's
 // 16-byte chunks are permuted by row as attend's keys are.  Bound by the exponentials
-// and sums, which take as many cycles as the products they wait for: 2,048 tokens behind
+// and sums, which take twice the cycles of the products they wait for: 2,048 tokens behind
 // 6,144 places (32 query heads over 8, D 128) take 157 us, 0.77 PFLOP/s; with one group of
 // wavefronts 201 against 169, and 167 with rows' addresses and ends looked at one by one.
 template <int D, bool kBf16>
