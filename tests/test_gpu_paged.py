@@ -702,3 +702,70 @@ def test_release_past_the_list_and_bad_requests():
     lens[20] = lens[21] = 20
     assert check_release(lens, have, table, 16, nb, np.zeros(1000, np.int32),
                          4) == ref.BLOCK_ID
+
+
+# ----------------------------------- weigh: rows that a wavefront holds, keys
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("G,window", [(1, 65), (4, 17), (3, 32), (1, 127),
+                                      (4, 32), (8, 16), (1, 129), (3, 43)])
+@pytest.mark.parametrize("bs,order", [(16, NHD), (5, HND)])
+def test_weigh_up_to_and_past_128_rows(dtype, D, G, window, bs, order):
+    """Every tile of rows that a wavefront holds, part-filled and full, and the
+    first count of rows that it does not hold."""
+    w = window
+    n = [w, w + 1, 64 + w, 300, 1500, 0, w + 3, 1100]
+    m = [w, w, w, w - 1, w, 0, 1, w // 2]
+    c = Case(n, m, 2, G, D, bs, order, dtype, seed=G + w)
+    assert check_weigh(c, max_new=w) == 0
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("m", [1, 6, 30, 70])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("whole", [True, False])
+def test_weigh_keys_that_are_not_finite(dtype, m, D, whole):
+    """NaN and infinities among the keys (a whole row, or one element, whose
+    scores are then infinite): a query with a score of NaN or +infinity makes the
+    places that it sees NaN, and no others; a score of -infinity weighs 0."""
+    n, G = [200, 90, 150, 1300], 4
+    c = Case(n, [m] * 4, 2, G, D, dtype=dtype, seed=m)
+    rows = ref.by_slot(c.cache, c.sh, c.nb)
+    for r, (back, bad) in enumerate(((1, "nan"), ((m + 1) // 2, "inf"),
+                                     ((m + 2) // 3, "-inf"), (700, "-inf"))):
+        j = n[r] - back
+        at = rows[0, 0, int(c.table[r, j // 16]), j % 16]
+        if whole:
+            at[0] = float(bad)
+        else:
+            at[0, 3] = float(bad)
+    _, lse, _ = c.attend()
+    led = paged.new_ledger(c.sh, c.nb, dev())
+    led.copy_(torch.rand(led.shape, generator=gen(3), device=dev())
+              .view(torch.int32))
+    want = paged.weights_of(led)[0].double()
+    slack = torch.zeros_like(want)
+    for r, x in enumerate(n):
+        a, _, k, v, seen, block, at = ref.request_rows(
+            r, c.q, c.cache, c.sh, c.nb, c.table, c.n, c.cu, 0, m)
+        block, at = (torch.tensor(t, device=dev()) for t in (block, at))
+        for g in range(2 * G):
+            q, given = c.q[a:a + m, g].double(), lse[a:a + m, g].double()
+            s = torch.matmul(q, k[:, g // G].t().contiguous()) * D ** -0.5
+            p = torch.where(seen, torch.exp(s - given[:, None]), 0.0)
+            room = ref.attend(q, k[:, g // G], v[:, g // G], D ** -0.5, seen,
+                              0.0)[5]
+            want[block, g // G, at] += p.sum(0)
+            slack[block, g // G, at] += torch.where(p > 0, p * room, 0.0).sum(0)
+    # the sums' own roundings, as weighed() counts them
+    slack += want.abs().nan_to_num(0) * ((m * G / 32 + 8) * 2.0 ** -24
+                                         + 2.0 ** -23)
+    status = word()
+    paged.lumen_paged_weigh(c.sh, c.nb, 0, c.cache, i32(c.table), i32(c.n),
+                            i32(c.cu), c.q, lse, led, status, max_new=m)
+    got = paged.weights_of(led)[0]
+    assert int(status) == 0
+    # places that no NaN reaches, of every request and head, are among those checked
+    assert want.isnan().any() and want.isfinite().any()
+    close(got, want, slack, 0.0, "weights")
