@@ -140,9 +140,12 @@ __global__ __launch_bounds__(kPlanThreads) void attend_plan_kernel(AttendArgs a)
     mine += count;
     tiles_to[i] = int(mine < a.num_units ? mine : a.num_units);
     if (count == 0) continue;
-    // steps of the request's tiles: those of the first and the last, on average
+    // steps of the request's tiles: those of the first and the last, on average.  Past
+    // the table's places the tiles are all alike, more than that average: as many as the
+    // last has, so that there are no more parts than there is room for
     const int last = whole_tile(a, q, i, count - 1).last;
-    work += uint64_t(count) * uint32_t(whole_tile(a, q, i, 0).last + last + 1) / 2;
+    work += q.n > a.cap ? uint64_t(count) * uint32_t(last)
+                        : uint64_t(count) * uint32_t(whole_tile(a, q, i, 0).last + last + 1) / 2;
     longest = last > longest ? last : longest;
   }
   int64_t upto = mine;
@@ -773,8 +776,9 @@ AttendPlan attend_plan(const lumen_kv_layout *l, int64_t cap, int32_t num_reqs, 
   p.tiles = num_q * group / p.tile_rows + (num_reqs < num_q ? num_reqs : num_q);
   p.parts = 0;
   if (cap >= kCutKeys) {
-    // a cut tile has fewer parts than one and a half times its steps over `part`, and
-    // `part` is at least five eighths of a slot's share of all steps: 2.4 for each slot
+    // a cut tile has fewer parts than one and a half times its steps over `part`; `part` is
+    // at least five eighths of a slot's share of the steps as the plan counts them, and it
+    // counts no less than three quarters of a request's: 3.2 for each slot
     p.parts = int64_t(p.slots) * 4;
     const int64_t most = p.tiles * (cap / kMinPartKeys + 2);
     if (p.parts > most) p.parts = most;

@@ -355,3 +355,26 @@ def test_what_a_workspace_holds_does_not_matter():
         ws.random_(0, 256)
         got, gl, status = c.attend(max_new=200, workspace=ws)
         assert torch.equal(got, want) and torch.equal(gl, wl) and status == 0
+
+
+def test_requests_past_a_narrow_table_repeat_themselves():
+    """A request with many more places than the table's 8,192: those that there are
+    count, and all tiles of rows that see every one of them are computed alike."""
+    pages, tiles = 512, 780
+    T = tiles * 128
+    c = Case([pages * 16], [128], 1, 1, 64, seed=11, dtype=FP)
+    c.q = c.q[:128].repeat(tiles, 1, 1)  # each tile's rows are the same ones
+    c.n, c.m, c.cu = [T], [T], np.array([0, T], np.int32)
+    out, lse, status = c.attend()
+    assert status == ref.RANGE
+    flat = slice(pages * 16 // 128, tiles)  # tiles whose rows see all places
+    out, lse = out.view(tiles, 128, 64)[flat], lse.view(tiles, 128)[flat]
+    k, v = (ref.by_slot(c.cache, c.sh, c.nb)[0, i, torch.tensor(
+        c.table[0], device=dev()).long()].reshape(-1, 64).double()
+        for i in (0, 1))
+    seen = torch.ones(128, pages * 16, dtype=torch.bool, device=dev())
+    want, slack, wl, lslack = ref.attend(c.q[:128, 0].double(), k, v, 0.125,
+                                         seen, UNIT[FP])[:4]
+    close(out[0], want, slack, UNIT[FP])
+    close(lse[0], wl, lslack, 0.0)
+    assert bool((out == out[:1]).all()) and bool((lse == lse[:1]).all())
