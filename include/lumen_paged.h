@@ -188,8 +188,8 @@ int lumen_paged_evict(const lumen_kv_layout *layout, int32_t first_layer,
  * Blocks past free_cap are not written and not counted (CAPACITY); a request with
  * lens < 0, have < 0 or pages past bt_cols gives none back (RANGE); an id outside
  * [0, num_blocks) goes to the list as it is (BLOCK_ID).  num_reqs at most
- * LUMEN_ATTN_MAX_REQS (TOO_MANY).  INVALID_ARG where d_free_now overlaps another
- * argument. */
+ * LUMEN_ATTN_MAX_REQS (TOO_MANY).  INVALID_ARG where the list, d_free_now or
+ * d_status overlaps another argument. */
 int lumen_paged_release(const int32_t *d_lens, const int32_t *d_have,
                         int32_t num_reqs, const int32_t *d_block_tables,
                         int32_t bt_cols, int32_t block_size,

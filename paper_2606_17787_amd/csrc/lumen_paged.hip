@@ -819,9 +819,10 @@ int lumen_paged_evict(const lumen_kv_layout *layout, int32_t first_layer, int32_
     return LUMEN_ERR_MISALIGNED;
   // workgroups read these while others write d_left
   const size_t words = size_t(num_reqs) * sizeof(int32_t);
-  if (overlap(d_left, words, d_lens, words) || overlap(d_left, words, d_keep, words) ||
-      overlap(d_left, words, d_recent_from, words) ||
-      overlap(d_left, words, d_block_tables, words * size_t(bt_cols)))
+  if (overlap({{d_left, words}}, {{d_lens, words},
+                                  {d_keep, words},
+                                  {d_recent_from, words},
+                                  {d_block_tables, words * size_t(bt_cols)}}))
     return LUMEN_ERR_INVALID_ARG;
   (void)hipGetLastError();
   EvictArgs a;
@@ -893,12 +894,15 @@ int lumen_paged_release(const int32_t *d_lens, const int32_t *d_have, int32_t nu
   if (!aligned(d_lens, 4) || !aligned(d_have, 4) || !aligned(d_block_tables, 4) ||
       !aligned(d_free, 4) || !aligned(d_free_count, 8) || !aligned(d_free_now, 8))
     return LUMEN_ERR_MISALIGNED;
-  // workgroups read these, or write the list, while one writes d_free_now
-  const size_t words = size_t(num_reqs) * sizeof(int32_t), now = sizeof(int64_t);
-  if (overlap(d_free_now, now, d_free_count, now) || overlap(d_free_now, now, d_lens, words) ||
-      overlap(d_free_now, now, d_have, words) ||
-      overlap(d_free_now, now, d_block_tables, words * size_t(bt_cols)) ||
-      overlap(d_free_now, now, d_free, size_t(free_cap) * sizeof(int32_t)))
+  // workgroups read these while others write the list, its count or the status word
+  const size_t words = size_t(num_reqs) * sizeof(int32_t);
+  if (overlap({{d_free, size_t(free_cap) * sizeof(int32_t)},
+               {d_free_now, sizeof(int64_t)},
+               {d_status, sizeof(int32_t)}},
+              {{d_lens, words},
+               {d_have, words},
+               {d_block_tables, words * size_t(bt_cols)},
+               {d_free_count, sizeof(int64_t)}}))
     return LUMEN_ERR_INVALID_ARG;
   int cus = 0;
   if ((st = compute_units(&cus)) != LUMEN_OK) return st;

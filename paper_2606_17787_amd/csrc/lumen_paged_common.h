@@ -3,6 +3,8 @@
 #ifndef LUMEN_PAGED_COMMON_H
 #define LUMEN_PAGED_COMMON_H
 
+#include <initializer_list>
+
 #include "lumen_attn_common.h"
 #include "lumen_paged.h"
 
@@ -115,10 +117,27 @@ struct Call {
   int32_t *status;
 };
 
-// Whether two ranges of bytes share some.
-inline bool overlap(const void *a, size_t a_bytes, const void *b, size_t b_bytes) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return a_bytes && b_bytes && (x < y ? y - x < a_bytes : x - y < b_bytes);
+// A range of bytes.
+struct Span {
+  const void *at;
+  size_t bytes;
+};
+
+inline bool overlap(const Span &a, const Span &b) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a.at), y = reinterpret_cast<uintptr_t>(b.at);
+  return a.bytes && b.bytes && (x < y ? y - x < a.bytes : x - y < b.bytes);
+}
+
+// Whether one of the ranges that a call writes shares bytes with another of them or
+// with one that it reads.
+inline bool overlap(std::initializer_list<Span> written, std::initializer_list<Span> read) {
+  for (const Span *w = written.begin(); w != written.end(); ++w) {
+    for (const Span *v = w + 1; v != written.end(); ++v)
+      if (overlap(*w, *v)) return true;
+    for (const Span &r : read)
+      if (overlap(*w, r)) return true;
+  }
+  return false;
 }
 
 // So that a step's places are counted in 32 bits.

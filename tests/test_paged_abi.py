@@ -234,6 +234,25 @@ def test_release_refuses_its_count_among_its_inputs(lib, name, bytes_):
             at["count"], 16, now, at["status"], None) == BAD
 
 
+@pytest.mark.parametrize("result,bytes_", [("free", 64), ("now", 8),
+                                           ("status", 4)])
+@pytest.mark.parametrize("name,size", [("lens", 8), ("have", 8), ("count", 8),
+                                       ("bt", 32), ("free", 64), ("now", 8),
+                                       ("status", 4)])
+def test_release_refuses_results_that_overlap(lib, result, bytes_, name, size):
+    """Its workgroups read the inputs while they write the list, its count and
+    the status word."""
+    if result == name:
+        return
+    need = {"free": 4, "now": 8, "status": 4}[result]
+    for to in (0, 4 - bytes_, size - 4):
+        at = apart("lens", "have", "bt", "free", "count", "now", "status")
+        at[result] = at[name] + (to if to % need == 0 else 0)
+        assert lib.lumen_paged_release(
+            at["lens"], at["have"], 2, at["bt"], 4, 16, 8, at["free"],
+            at["count"], 16, at["now"], at["status"], None) == BAD
+
+
 def test_binding_refuses_host_tensors_and_shapes():
     sh = CacheShape(2, 2, 128, 16, NHD)
     cache = torch.zeros(sh.pool_elems(2), dtype=torch.bfloat16)
