@@ -163,9 +163,10 @@ size_t lumen_paged_evict_workspace_bytes(const lumen_kv_layout *layout,
  * the larger weight first (NaN after everything, 0 and -0 alike), then the lower
  * place.  The kept places from d_keep[r] on move into the places under it that
  * were given up, the lowest into the lowest: rows of K and V and both words of the
- * ledger.  What lies behind is left as it is.  d_left[r]: min(n, d_keep[r]);
- * INVALID_ARG where it overlaps d_lens, d_keep, d_recent_from or the tables.  head_dim 64, 128 or 256; block_size * bt_cols at most
- * LUMEN_PAGED_MAX_PLACES.
+ * ledger.  What lies behind is left as it is.  d_left[r]: min(n, d_keep[r]).
+ * head_dim 64, 128 or 256; block_size * bt_cols at most LUMEN_PAGED_MAX_PLACES.
+ * INVALID_ARG where d_left, the status word, the workspace or the layers' cache or
+ * ledger overlaps another argument.
  *
  * A request is left alone, with d_left[r] = d_lens[r], where n or d_keep[r] is
  * negative or n passes bt_cols pages (RANGE), or where n > d_keep[r] and a block id

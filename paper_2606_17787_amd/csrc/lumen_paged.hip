@@ -817,18 +817,26 @@ int lumen_paged_evict(const lumen_kv_layout *layout, int32_t first_layer, int32_
       !aligned(d_block_tables, 4) || !aligned(d_lens, 4) || !aligned(d_keep, 4) ||
       !aligned(d_recent_from, 4) || !aligned(d_left, 4))
     return LUMEN_ERR_MISALIGNED;
-  // workgroups read these while others write d_left
+  // workgroups read these while others write
   const size_t words = size_t(num_reqs) * sizeof(int32_t);
-  if (overlap({{d_left, words}}, {{d_lens, words},
-                                  {d_keep, words},
-                                  {d_recent_from, words},
-                                  {d_block_tables, words * size_t(bt_cols)}}))
+  const size_t ledger_bytes = size_t(2 * ledger_words(layout)) * sizeof(int32_t);
+  uint8_t *const cache = static_cast<uint8_t *>(d_cache) + int64_t(first_layer) * 2 * p.half;
+  uint8_t *const ledger = static_cast<uint8_t *>(d_ledger) + int64_t(first_layer) * ledger_bytes;
+  if (overlap({{d_left, words},
+               {d_status, sizeof(int32_t)},
+               {d_workspace, plan.bytes},
+               {cache, size_t(num_layers) * 2 * p.half},
+               {ledger, size_t(num_layers) * ledger_bytes}},
+              {{d_lens, words},
+               {d_keep, words},
+               {d_recent_from, words},
+               {d_block_tables, words * size_t(bt_cols)}}))
     return LUMEN_ERR_INVALID_ARG;
   (void)hipGetLastError();
   EvictArgs a;
   a.words = ledger_words(layout);
-  a.cache = static_cast<uint8_t *>(d_cache) + int64_t(first_layer) * 2 * p.half;
-  a.ledger = static_cast<uint32_t *>(d_ledger) + int64_t(first_layer) * 2 * a.words;
+  a.cache = cache;
+  a.ledger = reinterpret_cast<uint32_t *>(ledger);
   a.half = p.half;
   a.page = p.page;
   a.slot_bytes = p.slot;

@@ -253,6 +253,24 @@ def test_release_refuses_results_that_overlap(lib, result, bytes_, name, size):
             at["count"], 16, at["now"], at["status"], None) == BAD
 
 
+@pytest.mark.parametrize("result,bytes_", [("left", 8), ("status", 4)])
+@pytest.mark.parametrize("name,size", [("lens", 8), ("keep", 8), ("frm", 8),
+                                       ("bt", 32), ("cache", 1 << 18),
+                                       ("ledger", 1 << 12), ("ws", 256),
+                                       ("left", 8), ("status", 4)])
+def test_evict_refuses_results_that_overlap(lib, result, bytes_, name, size):
+    if result == name:
+        return
+    for to in (0, 4 - bytes_, size - 4):
+        at = apart("cache", "ledger", "bt", "lens", "keep", "frm", "left", "ws",
+                   "status")
+        at[result] = at[name] + to
+        assert lib.lumen_paged_evict(
+            layout(), 0, 2, at["cache"], at["ledger"], at["bt"], 4, at["lens"],
+            at["keep"], at["frm"], 0, 2, at["left"], at["ws"], 1 << 16,
+            at["status"], None) == BAD
+
+
 def test_binding_refuses_host_tensors_and_shapes():
     sh = CacheShape(2, 2, 128, 16, NHD)
     cache = torch.zeros(sh.pool_elems(2), dtype=torch.bfloat16)
