@@ -40,7 +40,13 @@
  * to the most negative code seen while everything else is still computed.  No
  * call clears memory with a memset, so all can be captured in a graph.  A
  * workspace is not shared by calls in flight at the same time; what it holds
- * does not matter.  Results do not overlap what a call reads.  Results do not depend on timing.
+ * does not matter.  Results do not depend on timing.
+ *
+ * What a call writes (results, a layer's cache or ledger, workspace, status word)
+ * overlaps neither another such range nor one that it reads: INVALID_ARG.  There are
+ * two exceptions.  attend's d_out may be q's memory where q's rows lie as d_out's do.
+ * append does not look at k and v: they may be rows of the cache, of slots that the
+ * call does not write.
  *
  * A block that two requests' tables name (a shared prefix) can be attended to
  * by both; weigh, evict and release need the blocks of a call's requests to be
@@ -165,8 +171,6 @@ size_t lumen_paged_evict_workspace_bytes(const lumen_kv_layout *layout,
  * were given up, the lowest into the lowest: rows of K and V and both words of the
  * ledger.  What lies behind is left as it is.  d_left[r]: min(n, d_keep[r]).
  * head_dim 64, 128 or 256; block_size * bt_cols at most LUMEN_PAGED_MAX_PLACES.
- * INVALID_ARG where d_left, the status word, the workspace or the layers' cache or
- * ledger overlaps another argument.
  *
  * A request is left alone, with d_left[r] = d_lens[r], where n or d_keep[r] is
  * negative or n passes bt_cols pages (RANGE), or where n > d_keep[r] and a block id
@@ -189,8 +193,7 @@ int lumen_paged_evict(const lumen_kv_layout *layout, int32_t first_layer,
  * Blocks past free_cap are not written and not counted (CAPACITY); a request with
  * lens < 0, have < 0 or pages past bt_cols gives none back (RANGE); an id outside
  * [0, num_blocks) goes to the list as it is (BLOCK_ID).  num_reqs at most
- * LUMEN_ATTN_MAX_REQS (TOO_MANY).  INVALID_ARG where the list, d_free_now or
- * d_status overlaps another argument. */
+ * LUMEN_ATTN_MAX_REQS (TOO_MANY). */
 int lumen_paged_release(const int32_t *d_lens, const int32_t *d_have,
                         int32_t num_reqs, const int32_t *d_block_tables,
                         int32_t bt_cols, int32_t block_size,

@@ -741,11 +741,21 @@ int lumen_paged_append(const lumen_kv_layout *layout, int32_t layer, void *d_cac
   if (!aligned(d_cache, 16) || !aligned(d_slots, 8) || !aligned(d_positions, 4) ||
       !aligned(d_ledger, 4))
     return LUMEN_ERR_MISALIGNED;
+  // workgroups read these while others write
+  uint8_t *const cache = static_cast<uint8_t *>(d_cache) + int64_t(layer) * 2 * p.half;
+  int32_t *const ledger =
+      d_ledger ? static_cast<int32_t *>(d_ledger) + ledger_before(layout, layer) : nullptr;
+  const size_t words = size_t(num_tokens) * sizeof(int32_t);
+  if (overlap({{cache, size_t(2 * p.half)},
+               {ledger, ledger ? size_t(2 * ledger_words(layout)) * sizeof(int32_t) : 0},
+               {d_status, sizeof(int32_t)}},
+              {{d_slots, 2 * words}, {d_positions, d_positions ? words : 0}}))
+    return LUMEN_ERR_INVALID_ARG;
   int cus = 0;
   if ((st = compute_units(&cus)) != LUMEN_OK) return st;
   (void)hipGetLastError();
   AppendArgs a;
-  a.k = static_cast<uint8_t *>(d_cache) + int64_t(layer) * 2 * p.half;
+  a.k = cache;
   a.v = a.k + p.half;
   a.slot_limit = layout->num_blocks * layout->block_size;
   a.page = p.page;
@@ -754,9 +764,8 @@ int lumen_paged_append(const lumen_kv_layout *layout, int32_t layer, void *d_cac
   a.block_size = layout->block_size;
   a.by_block = divisor(a.block_size);
   a.heads = layout->num_kv_heads;
-  a.weights = d_ledger ? static_cast<int32_t *>(d_ledger) + 2 * layer * ledger_words(layout)
-                       : nullptr;
-  a.places = d_ledger ? a.weights + ledger_words(layout) : nullptr;
+  a.weights = ledger;
+  a.places = ledger ? ledger + ledger_words(layout) : nullptr;
   a.status = d_status;
   // rows are counted in 32 bits: a call over more of them is several launches
   const int64_t most = (int64_t(1) << 30) / (2 * a.heads);

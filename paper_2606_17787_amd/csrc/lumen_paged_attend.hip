@@ -856,8 +856,28 @@ int lumen_paged_attend(const lumen_kv_layout *layout, int32_t layer, const void 
       !aligned(d_lens, 4) || !aligned(d_cu, 4) || !aligned(d_block_tables, 4) ||
       !aligned(d_lse, 4))
     return LUMEN_ERR_MISALIGNED;
-  if (lumen_paged_attend_workspace_bytes(layout, bt_cols, num_reqs, num_tokens, max_new,
-                                         num_q_heads) > (d_workspace ? workspace_bytes : 0))
+  const size_t need = lumen_paged_attend_workspace_bytes(layout, bt_cols, num_reqs, num_tokens,
+                                                         max_new, num_q_heads);
+  if (need > (d_workspace ? workspace_bytes : 0)) return LUMEN_ERR_INVALID_ARG;
+  // Workgroups read these while others write.  Queries in their results' place are read
+  // and written by the same wavefront alone, in that order.
+  const int32_t head_dim = layout->head_dim;
+  const size_t heads = size_t(num_tokens) * size_t(num_q_heads);
+  const size_t words = size_t(num_reqs) * sizeof(int32_t);
+  const bool in_place = q->d_base == d_out &&
+                        (num_q_heads == 1 || q->head_stride == head_dim) &&
+                        (num_tokens == 1 || q->token_stride == int64_t(num_q_heads) * head_dim);
+  const Span queries = span_of(q, num_tokens, num_q_heads, head_dim);
+  if (overlap({{d_out, heads * size_t(head_dim) * 2},
+               {d_lse, d_lse ? heads * sizeof(float) : 0},
+               {d_workspace, need},
+               {d_status, sizeof(int32_t)}},
+              {{static_cast<const uint8_t *>(d_cache) + int64_t(layer) * 2 * pages.half,
+                size_t(2 * pages.half)},
+               {in_place ? nullptr : queries.at, in_place ? 0 : queries.bytes},
+               {d_block_tables, words * size_t(bt_cols)},
+               {d_lens, words},
+               {d_cu, words + sizeof(int32_t)}}))
     return LUMEN_ERR_INVALID_ARG;
   int cus = 0;
   if ((st = compute_units(&cus)) != LUMEN_OK) return st;

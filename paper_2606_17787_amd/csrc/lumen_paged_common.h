@@ -68,6 +68,11 @@ inline int64_t ledger_words(const lumen_kv_layout *l) {
   return l->num_blocks * l->num_kv_heads * l->block_size;
 }
 
+// Words of the ledger before a layer's.
+inline int64_t ledger_before(const lumen_kv_layout *l, int32_t layer) {
+  return int64_t(layer) * 2 * ledger_words(l);
+}
+
 // Places that a block table row has.
 inline int64_t places_of(const lumen_kv_layout *l, int32_t bt_cols) {
   return int64_t(bt_cols) * l->block_size;
@@ -138,6 +143,12 @@ inline bool overlap(std::initializer_list<Span> written, std::initializer_list<S
       if (overlap(*w, r)) return true;
   }
   return false;
+}
+
+// What the rows of a call's tokens take, from the first to the last.
+inline Span span_of(const lumen_attn_rows *r, int64_t tokens, int32_t heads, int32_t head_dim) {
+  return Span{r->d_base, size_t((tokens - 1) * r->token_stride +
+                                int64_t(heads - 1) * r->head_stride + head_dim) * 2};
 }
 
 // So that a step's places are counted in 32 bits.

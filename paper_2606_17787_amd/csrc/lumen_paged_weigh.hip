@@ -509,6 +509,19 @@ int lumen_paged_weigh(const lumen_kv_layout *layout, int32_t layer, const void *
   if (lumen_paged_weigh_workspace_bytes(layout, bt_cols, num_reqs, num_tokens, max_new,
                                         num_q_heads) > (d_workspace ? workspace_bytes : 0))
     return LUMEN_ERR_INVALID_ARG;
+  // workgroups read these while others write
+  float *const ledger = static_cast<float *>(d_ledger) + ledger_before(layout, layer);
+  const size_t words = size_t(num_reqs) * sizeof(int32_t);
+  if (overlap({{ledger, size_t(2 * ledger_words(layout)) * sizeof(float)},
+               {d_status, sizeof(int32_t)}},
+              {{static_cast<const uint8_t *>(d_cache) + int64_t(layer) * 2 * pages.half,
+                size_t(2 * pages.half)},
+               span_of(q, num_tokens, num_q_heads, layout->head_dim),
+               {d_lse, size_t(num_tokens) * size_t(num_q_heads) * sizeof(float)},
+               {d_block_tables, words * size_t(bt_cols)},
+               {d_lens, words},
+               {d_cu, words + sizeof(int32_t)}}))
+    return LUMEN_ERR_INVALID_ARG;
   int cus = 0;
   if ((st = compute_units(&cus)) != LUMEN_OK) return st;
   (void)hipGetLastError();
@@ -517,7 +530,7 @@ int lumen_paged_weigh(const lumen_kv_layout *layout, int32_t layer, const void *
       call_of(layout, pages, layer, d_cache, d_block_tables, bt_cols, d_lens, d_cu, num_reqs, q,
               num_tokens, max_new, num_q_heads, scale, d_status);
   a.lse = d_lse;
-  a.weights = static_cast<float *>(d_ledger) + 2 * layer * ledger_words(layout);
+  a.weights = ledger;
   const bool bf = dtype == LUMEN_ATTN_BF16;
   const int D = layout->head_dim;
   hipStream_t s = static_cast<hipStream_t>(stream);

@@ -378,3 +378,34 @@ def test_requests_past_a_narrow_table_repeat_themselves():
     close(out[0], want, slack, UNIT[FP])
     close(lse[0], wl, lslack, 0.0)
     assert bool((out == out[:1]).all()) and bool((lse == lse[:1]).all())
+
+
+@pytest.mark.parametrize("n,m,H,G,D", [
+    ([300, 20, 64], [1, 1, 1], 2, 4, 128), ([300, 90, 64], [9, 90, 3], 2, 3, 64),
+    ([9000, 700, 4000], [1, 200, 2], 2, 8, 128), ([5000], [4100], 16, 1, 128)])
+@pytest.mark.parametrize("dtype", [BF, FP])
+def test_attend_in_the_queries_place(n, m, H, G, D, dtype):
+    """Whole tiles, tiles in parts, and workgroups of eight wavefronts."""
+    c = Case(n, m, H, G, D, dtype=dtype, seed=12)
+    c.q = c.q.contiguous()
+    want, wl, _ = c.attend(max_new=max(m))
+    args = (i32(c.table), i32(c.n), i32(c.cu))
+    for _ in range(3):
+        q, lse, status = c.q.clone(), torch.zeros_like(wl), word()
+        paged.lumen_paged_attend(c.sh, c.nb, 0, c.cache, *args, q, q, status,
+                                 max_new=max(m), lse=lse)
+        assert torch.equal(q, want) and torch.equal(lse, wl)
+        assert int(status) == 0
+
+
+def test_append_of_rows_of_the_cache():
+    """Tokens of one request into slots of another, in the same layer."""
+    sh = CacheShape(1, 3, 64, 8, NHD)
+    cache = new_cache(sh, 20, BF, gen(13))
+    rows = cache.view(2, 160, 3, 64)
+    want = cache.clone().view(2, 160, 3, 64)
+    want[:, 100:150] = want[:, 10:60]
+    status = word()
+    paged.lumen_paged_append(sh, 20, 0, cache, rows[0, 10:60], rows[1, 10:60],
+                             torch.arange(100, 150, device=dev()), status)
+    assert torch.equal(rows, want) and int(status) == 0

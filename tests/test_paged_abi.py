@@ -271,6 +271,74 @@ def test_evict_refuses_results_that_overlap(lib, result, bytes_, name, size):
             at["status"], None) == BAD
 
 
+def wide_apart():
+    names = ("cache", "bt", "lens", "cu", "q", "out", "lse", "status", "ledger",
+             "ws")
+    return {name: FAKE + (i << 26) for i, name in enumerate(names)}
+
+
+@pytest.mark.parametrize("result,bytes_", [("out", 20480), ("lse", 320),
+                                           ("ws", 256), ("status", 4)])
+@pytest.mark.parametrize("name,size", [("cache", 1 << 17), ("bt", 3200),
+                                       ("lens", 8), ("cu", 12), ("q", 20480),
+                                       ("out", 20480), ("lse", 320),
+                                       ("ws", 256), ("status", 4)])
+def test_attend_refuses_results_that_overlap(lib, result, bytes_, name, size):
+    """Among the plan of the workspace, or what other workgroups read.  (Two
+    layers' cache, of which the second is attended to.)"""
+    if result == name:
+        return
+    need = {"out": 16, "ws": 16}.get(result, 4)
+    for to in (need, need - bytes_, size - need):
+        if to % need or to >= size:
+            continue
+        at = wide_apart()
+        at[result] = at[name] + to + (name == "cache") * (1 << 17)
+        assert lib.lumen_paged_attend(
+            layout(), 1, at["cache"], at["bt"], 400, at["lens"], at["cu"], 2,
+            rows(at["q"], 1024, 128), 10, 10, 0, 8, 0.1, at["out"], at["lse"],
+            at["ws"], 1 << 26, at["status"], None) == BAD, to
+
+
+@pytest.mark.parametrize("result,bytes_", [("ledger", 2048), ("status", 4)])
+@pytest.mark.parametrize("name,size", [("cache", 1 << 17), ("bt", 3200),
+                                       ("lens", 8), ("cu", 12), ("q", 20480),
+                                       ("lse", 320), ("ledger", 2048),
+                                       ("status", 4)])
+def test_weigh_refuses_results_that_overlap(lib, result, bytes_, name, size):
+    if result == name:
+        return
+    for to in (0, 4 - bytes_, size - 4):
+        at = wide_apart()
+        # the second layer's words and rows
+        at[result] = at[name] + to + {"cache": 1 << 17, "ledger": 2048}.get(
+            name, 0) - 2048 * (result == "ledger")
+        assert lib.lumen_paged_weigh(
+            layout(), 1, at["cache"], at["bt"], 400, at["lens"], at["cu"], 2,
+            rows(at["q"], 1024, 128), 10, 10, 0, 8, 0.1, at["lse"],
+            at["ledger"], None, 0, at["status"], None) == BAD, to
+
+
+@pytest.mark.parametrize("result,bytes_", [("cache", 1 << 17), ("ledger", 2048),
+                                           ("status", 4)])
+@pytest.mark.parametrize("name,size", [("slots", 24), ("pos", 12),
+                                       ("ledger", 2048), ("status", 4),
+                                       ("cache", 1 << 17)])
+def test_append_refuses_results_that_overlap(lib, result, bytes_, name, size):
+    if result == name:
+        return
+    need = {"cache": 16}.get(result, 4)
+    for to in (0, need - bytes_, size - need):
+        if to % need or to >= size:
+            continue
+        at = apart("cache", "k", "v", "slots", "pos", "ledger", "status")
+        layer = {"cache": 1 << 17, "ledger": 2048}  # from a layer to the next
+        at[result] = at[name] + to + layer.get(name, 0) - layer.get(result, 0)
+        assert lib.lumen_paged_append(
+            layout(), 1, at["cache"], rows(at["k"], 256), rows(at["v"], 256),
+            at["slots"], at["pos"], 3, at["ledger"], at["status"], None) == BAD
+
+
 def test_binding_refuses_host_tensors_and_shapes():
     sh = CacheShape(2, 2, 128, 16, NHD)
     cache = torch.zeros(sh.pool_elems(2), dtype=torch.bfloat16)
