@@ -107,20 +107,23 @@ size_t lumen_paged_attend_workspace_bytes(const lumen_kv_layout *layout,
  * is taken to have too; d_out [num_tokens][num_q_heads][D] of dtype, contiguous,
  * 16-byte aligned; d_lse [num_tokens][num_q_heads] floats, or NULL.  head_dim 64
  * or 128; scale above 0, scale * log2(e) finite; max_new: at least the most new
- * tokens of a request (the host's, which picks a form by it); num_tokens * G at
- * most LUMEN_PAGED_MAX_ROWS.  Sizes that would need a launch of 2^32 threads or
- * more are refused (UNSUPPORTED).
+ * tokens of a request (requests are held to it; it chooses no form here);
+ * num_tokens * G at most LUMEN_PAGED_MAX_ROWS.  Sizes that would need a launch of
+ * 2^32 threads or more are refused (UNSUPPORTED).
+ *
+ * From 1,024 places in a table row on (block_size * bt_cols) long requests are cut
+ * into parts, which takes two more kernels, whatever the requests hold.
  *
  * A request whose bounds fall outside [0, num_tokens], end before they begin or
  * hold more than max_new tokens is skipped (RANGE), its rows not written, as
  * those of tokens in no request.  Requests must not share queries.  A negative
  * length counts as 0 (RANGE).  Places in pages past bt_cols or from 2^31 - 256 on
- * (RANGE), or with a block id outside [0, num_blocks) (BLOCK_ID), are left out; a row that sees none is
- * zeros, its lse -infinity.  What the cache holds past a request's places, or in
- * places that a query does not see, does not reach its row, NaN and infinities
- * included; a NaN or infinity among the values it sees does, and a row with a
- * score of NaN or +infinity, or with none but -infinity, is NaN.  lse is NaN for the
- * first two and -infinity for the third. */
+ * (RANGE), or with a block id outside [0, num_blocks) (BLOCK_ID), are left out; a
+ * row that sees none is zeros, its lse -infinity.  What the cache holds past a
+ * request's places, or in places that a query does not see, does not reach its row,
+ * NaN and infinities included; a NaN or infinity among the values it sees does, and a
+ * row with a score of NaN or +infinity, or with none but -infinity, is NaN.  lse is
+ * NaN for the first two and -infinity for the third. */
 int lumen_paged_attend(const lumen_kv_layout *layout, int32_t layer,
                        const void *d_cache, const int32_t *d_block_tables,
                        int32_t bt_cols, const int32_t *d_lens,
@@ -131,8 +134,7 @@ int lumen_paged_attend(const lumen_kv_layout *layout, int32_t layer,
                        void *d_workspace, size_t workspace_bytes,
                        int32_t *d_status, lumen_stream_t stream);
 
-/* Bytes of workspace a weigh call needs (0 for calls that need none, and for
- * sizes it refuses). */
+/* Bytes of workspace a weigh call needs: 0 for all, at present. */
 size_t lumen_paged_weigh_workspace_bytes(const lumen_kv_layout *layout,
                                          int32_t bt_cols, int32_t num_reqs,
                                          int64_t num_tokens, int32_t max_new,
@@ -146,7 +148,12 @@ size_t lumen_paged_weigh_workspace_bytes(const lumen_kv_layout *layout,
  * queries of a request can be the last ones of those attended to alone (a window
  * of a prompt): its bounds in d_cu then hold just these.  Weights of places that no
  * query sees are not written.  The rest is as for attend; a query with NaN in
- * its scores or lse makes the weights that it adds to NaN. */
+ * its scores or lse makes the weights that it adds to NaN.
+ *
+ * max_new * G chooses the form: up to 128 of these rows a wavefront holds all of a
+ * request's, with more they come tile by tile, which single tokens pay for (256 of
+ * them around 2,048 places: 957 us against 310).  A table row's places choose how
+ * many of them a workgroup takes, whatever the requests hold. */
 int lumen_paged_weigh(const lumen_kv_layout *layout, int32_t layer,
                       const void *d_cache, const int32_t *d_block_tables,
                       int32_t bt_cols, const int32_t *d_lens,

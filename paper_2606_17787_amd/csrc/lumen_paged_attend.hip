@@ -762,7 +762,7 @@ int attend_waves(const lumen_kv_layout *l, int32_t num_reqs, int64_t num_q, int 
 }
 
 AttendPlan attend_plan(const lumen_kv_layout *l, int64_t cap, int32_t num_reqs, int64_t num_q,
-                       int32_t max_new, int32_t q_heads, int cus) {
+                       int32_t q_heads, int cus) {
   AttendPlan p;
   const int group = q_heads / l->num_kv_heads;
   p.waves = attend_waves(l, num_reqs, num_q, group);
@@ -823,7 +823,7 @@ size_t lumen_paged_attend_workspace_bytes(const lumen_kv_layout *layout, int32_t
       check_queries(layout, bt_cols, num_reqs, num_tokens, max_new, num_q_heads) != LUMEN_OK)
     return 0;
   const AttendPlan p = attend_plan(layout, places_of(layout, bt_cols), num_reqs, num_tokens,
-                                   max_new, num_q_heads, kMaxUnits);
+                                   num_q_heads, kMaxUnits);
   return too_many_threads(p, layout->num_kv_heads) ? 0 : p.bytes;
 }
 
@@ -845,8 +845,8 @@ int lumen_paged_attend(const lumen_kv_layout *layout, int32_t layer, const void 
   if ((st = check_rows(q, num_tokens)) != LUMEN_OK) return st;
   const int32_t kv_heads = layout->num_kv_heads;
   const int64_t cap = places_of(layout, bt_cols);
-  if (too_many_threads(attend_plan(layout, cap, num_reqs, num_tokens, max_new, num_q_heads,
-                                   kMaxUnits), kv_heads))
+  if (too_many_threads(attend_plan(layout, cap, num_reqs, num_tokens, num_q_heads, kMaxUnits),
+                       kv_heads))
     return LUMEN_ERR_UNSUPPORTED;
   if (num_reqs == 0 || num_tokens == 0) return LUMEN_OK;
   if (!d_lens || !d_cu || !d_out || (!d_block_tables && bt_cols > 0) ||
@@ -881,8 +881,7 @@ int lumen_paged_attend(const lumen_kv_layout *layout, int32_t layer, const void 
     return LUMEN_ERR_INVALID_ARG;
   int cus = 0;
   if ((st = compute_units(&cus)) != LUMEN_OK) return st;
-  const AttendPlan p =
-      attend_plan(layout, cap, num_reqs, num_tokens, max_new, num_q_heads, cus);
+  const AttendPlan p = attend_plan(layout, cap, num_reqs, num_tokens, num_q_heads, cus);
   (void)hipGetLastError();
   AttendArgs a;
   static_cast<Call &>(a) =
