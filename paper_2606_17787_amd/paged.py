@@ -216,7 +216,7 @@ def new_attend_workspace(shape, block_tables, lens, q,
 
 def new_weigh_workspace(shape, block_tables, lens, q,
                         max_new=None) -> Optional[torch.Tensor]:
-    """Workspace for weigh calls of these sizes; None where they take none."""
+    """Workspace for weigh calls of these sizes: None, at present they take none."""
     return _new_workspace("lumen_paged_weigh_workspace_bytes", shape,
                           block_tables, lens, q, max_new)
 
@@ -263,14 +263,14 @@ def _attend_args(shape, num_blocks, layer, cache, block_tables, lens, cu, q,
         _attn._status(status))
 
 
-def _own(new, stream, workspace, *sizes):
-    """The caller's workspace, or one of the call's own, on its stream."""
+def _own_workspace(stream, workspace, *sizes):
+    """The caller's workspace, or one of the attend call's own, on its stream."""
     if workspace is not None:
         return workspace
     if stream is None:
-        return new(*sizes)
+        return new_attend_workspace(*sizes)
     with torch.cuda.stream(stream):
-        return new(*sizes)
+        return new_attend_workspace(*sizes)
 
 
 def lumen_paged_attend(shape, num_blocks: int, layer: int,
@@ -288,8 +288,8 @@ def lumen_paged_attend(shape, num_blocks: int, layer: int,
     at least the most new tokens of a request (None: all).  scale None:
     D ** -0.5.  workspace None: one is allocated for the call, on the stream it
     runs on."""
-    workspace = _own(new_attend_workspace, stream, workspace, shape,
-                     block_tables, lens, q, max_new)
+    workspace = _own_workspace(stream, workspace, shape, block_tables, lens, q,
+                               max_new)
     _call("lumen_paged_attend",
           _attend_args(shape, num_blocks, layer, cache, block_tables, lens, cu,
                        q, out, status, max_new, lse, scale, workspace), stream)
@@ -301,19 +301,14 @@ def prepare_attend(shape, num_blocks, layer, cache, block_tables, lens, cu, q,
     """lumen_paged_attend with its arguments checked once; workspace None: one
     is allocated and kept, on the current stream, so the object must not be in
     flight twice at a time, and a graph that holds its calls needs it alive."""
-    ws = _own(new_attend_workspace, None, workspace, shape, block_tables, lens,
-              q, max_new)
+    ws = _own_workspace(None, workspace, shape, block_tables, lens, q, max_new)
     args = _attend_args(shape, num_blocks, layer, cache, block_tables, lens,
                         cu, q, out, status, max_new, lse, scale, ws)
     keep = (cache, block_tables, lens, cu, q, out, status, lse, ws)
-    return _with_workspace("lumen_paged_attend", args, keep, workspace, ws)
-
-
-def _with_workspace(name, args, keep, given, workspace):
-    _lib()
-    if given is None and workspace is not None:
-        return _attn._OwnWorkspaceCall(name, args, keep, workspace)
-    return _prepared(name, args, keep)
+    if workspace is None and ws is not None:
+        _lib()
+        return _attn._OwnWorkspaceCall("lumen_paged_attend", args, keep, ws)
+    return _prepared("lumen_paged_attend", args, keep)
 
 
 def _weigh_args(shape, num_blocks, layer, cache, block_tables, lens, cu, q,
@@ -334,9 +329,10 @@ def lumen_paged_weigh(shape, num_blocks: int, layer: int, cache: torch.Tensor,
                       stream: Optional[torch.cuda.Stream] = None) -> None:
     """Add the attention weights of each request's last tokens, q and lse as
     attend had and gave them (or the last ones of each request alone, with a cu
-    of their own), to the places that they see in the ledger."""
-    workspace = _own(new_weigh_workspace, stream, workspace, shape,
-                     block_tables, lens, q, max_new)
+    of their own), to the places that they see in the ledger.  max_new, at least
+    the most tokens of a request, chooses the form: None stands for all tokens of
+    the call, and costs a batch of single tokens up to three times their time.  No
+    workspace is needed."""
     _call("lumen_paged_weigh",
           _weigh_args(shape, num_blocks, layer, cache, block_tables, lens, cu,
                       q, lse, ledger, status, max_new, scale, workspace),
@@ -346,14 +342,13 @@ def lumen_paged_weigh(shape, num_blocks: int, layer: int, cache: torch.Tensor,
 def prepare_weigh(shape, num_blocks, layer, cache, block_tables, lens, cu, q,
                   lse, ledger, status, max_new=None, scale=None,
                   workspace=None) -> "_kv.PreparedCall":
-    """lumen_paged_weigh with its arguments checked once; the workspace as in
-    prepare_attend."""
-    ws = _own(new_weigh_workspace, None, workspace, shape, block_tables, lens,
-              q, max_new)
-    args = _weigh_args(shape, num_blocks, layer, cache, block_tables, lens, cu,
-                       q, lse, ledger, status, max_new, scale, ws)
-    keep = (cache, block_tables, lens, cu, q, lse, ledger, status, ws)
-    return _with_workspace("lumen_paged_weigh", args, keep, workspace, ws)
+    """lumen_paged_weigh with its arguments checked once."""
+    return _prepared("lumen_paged_weigh",
+                     _weigh_args(shape, num_blocks, layer, cache, block_tables,
+                                 lens, cu, q, lse, ledger, status, max_new,
+                                 scale, workspace),
+                     (cache, block_tables, lens, cu, q, lse, ledger, status,
+                      workspace))
 
 
 def lumen_paged_evict_workspace_bytes(shape, num_layers: int, bt_cols: int,
