@@ -36,8 +36,8 @@ struct AppendArgs {
 
 // Rows of K and V as they are, 16 bytes a lane, D/8 lanes a row; a lane keeps its
 // head of K or V for all of its tokens.  Bound by bytes: 4 D a token and head in
-// and as many out.  16,411 tokens of 8 heads with D 128 take 30 us, 4.5 TB/s, 256 take 4,
-// of which the launch and two dependent reads are all.
+// and as many out.  For 16,411 tokens of 8 heads with D 128 the kernel takes 24.7 us, 5.5
+// TB/s, of a pass's 30; for 256 it takes 3 of 4, the launch and two dependent reads.
 template <int D>
 __global__ __launch_bounds__(kRowThreads) void append_kernel(AppendArgs a) {
   constexpr uint32_t kLanes = D / 8, kRows = kRowThreads / kLanes;
@@ -200,10 +200,12 @@ __device__ __forceinline__ void move_places(const EvictArgs &a, const Item &it, 
 // belong together.  D is 0 where evict_move_kernel moves them; otherwise this
 // workgroup does, with the two lists in LDS.
 //
-// Bound by what comes one after the other in a workgroup: the table, the words, two or
-// three digits' counts, the lists, the rows.  64 requests of 2,064 places, 2,048 of them
-// kept, in four layers of 8 heads: 41 us with the moves, for 34 MB of words and as many
-// of rows.  16 prompts around 8,192 tokens to 1,024 in two layers: 76 us.
+// Bound by vector instructions first, then by what comes one after the other in a
+// workgroup: the table, the words, two or three digits' counts, the lists, the rows.  64
+// requests of 2,064 places, 2,048 of them kept, in four layers of 8 heads: 41 us with the
+// moves, for 34 MB of words and as many of rows; 1,780 vector instructions a wavefront are
+// 57 thousand cycles a SIMD, 26 us of these.  16 prompts around 8,192 tokens to 1,024 in
+// two layers: 76 us.
 template <int kThreads, int kPer, int D>
 __global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictArgs a) {
   constexpr int kWaves = kThreads / kWave;
@@ -606,7 +608,9 @@ int evict_plan(const lumen_kv_layout *l, int32_t layers, int32_t bt_cols, int32_
 // workgroups share a compute unit, so that one counts while another waits.  With the
 // ledger's restoring copy, 256 threads take 54 us for 64 requests of 2,064 places in
 // four layers of 8 heads, 1,024 threads of 8 places 115 and of 32 places 175; for 8
-// requests of 4,096 in eight layers 116, 118 and 132.
+// requests of 4,096 in eight layers 116, 118 and 132.  `cap` is what a table row has, for
+// what the requests hold is not known here: these 64 take 51 us with a table of 2,064
+// places, 112 with 8,192, 172 with 32,768 and 252 with 131,072.
 template <int D>
 void (*select_kernel(int64_t cap, int *threads))(EvictArgs) {
   *threads = cap <= 256 * 16 ? 256 : 1024;

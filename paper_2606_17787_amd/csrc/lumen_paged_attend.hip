@@ -741,10 +741,13 @@ struct AttendPlan {
 // its size needs no device.
 constexpr int kMaxUnits = 256;
 
-// Places of a request from which on tiles may be cut.  That takes two more kernels, of
-// 12 us together: single tokens of 1 request with 1,100, 1,500 and 2,000 places take 23,
-// 24 and 23 us with them and 28, 35 and 44 without, of 16 requests 30 and 39 against 29
-// and 46 (1,100, 2,000), of 100 requests with 2,000 each 172 against 170.
+// Places of a table row from which on tiles may be cut.  That takes two more kernels, of
+// 10 to 19 us together (the plan 5.8 to 9.7, the join 4.6 to 9.1): single tokens of 1
+// request with 1,100, 1,500 and 2,000 places take 23, 24 and 23 us with them and 28, 35
+// and 44 without, of 16 requests 30 and 39 against 29 and 46 (1,100, 2,000), of 100
+// requests with 2,000 each 172 against 170.  How many places the requests hold is not
+// known here: 8 of around 230 take 11.8 us with a table of 480 places and 19 to 20 with
+// one of 1,024 or more.
 constexpr int kCutKeys = 1024;
 
 // Wavefronts of a workgroup.  Eight share a tile of places among twice the rows and

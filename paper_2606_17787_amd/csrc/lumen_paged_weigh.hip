@@ -546,6 +546,10 @@ int lumen_paged_weigh(const lumen_kv_layout *layout, int32_t layer, const void *
     const int low = a.block_size & -a.block_size;
     a.chunk = kEntries * (low < 16 ? low : 16);
     if (a.chunk > kMostPlaces16) a.chunk = kMostPlaces16;
+    // (The table's places count, which the requests need not fill: empty stretches cost
+    // their launch.  One token behind 1,000 places with a table of 1,008, 8,192, 32,768 and
+    // 131,072 places takes 5.9, 5.6, 8.2 and 12.9 us, 256 around 2,048 with 8,208, 32,768
+    // and 131,072 310, 428 and 780.)
     // Smaller stretches where these would not fill the chip: one token behind 1,000 and
     // 16,384 places 5.7 and 11.2 us against 13.2 and 14.0, 32 tokens of 4 requests with
     // 8,000 places 25.7 against 28.6.  (256 requests around 2,048 places take 383 us in
