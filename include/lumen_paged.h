@@ -56,9 +56,11 @@
  *
  * Arithmetic.  Scores, their maxima, all sums, lse and the ledger's weights
  * are held in 32 bits.  attend rounds its weights to the type of the inputs for
- * the products with V (one part in 2^9 or 2^12 each).  The sum that rows are
- * divided by is of the weights before that in bf16 and after it in fp16; lse's is
- * before.  weigh rounds nothing but its sums.
+ * the products with V (one part in 2^9 or 2^12 each; in fp16 those under some 2^-21
+ * of their row's largest lose bits, under 2^-32 they are 0, as under 2^-118 in bf16:
+ * an infinity among the values there makes its element NaN or infinite).  The sum
+ * that rows are divided by is of the weights before that in bf16 and after it in
+ * fp16; lse's is before.  weigh rounds nothing but its sums.
  */
 #ifndef LUMEN_PAGED_H
 #define LUMEN_PAGED_H

@@ -409,3 +409,38 @@ def test_append_of_rows_of_the_cache():
     paged.lumen_paged_append(sh, 20, 0, cache, rows[0, 10:60], rows[1, 10:60],
                              torch.arange(100, 150, device=dev()), status)
     assert torch.equal(rows, want) and int(status) == 0
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("m", [1, 60])
+@pytest.mark.parametrize("down", [10, 40, 200])
+def test_infinite_values_with_the_smallest_weights(dtype, m, down):
+    """Where a weight is too small for its type an infinite value still shows, in
+    its own element alone."""
+    c = Case([400, 70], [m, m], 1, 2, 64, dtype=dtype, seed=14)
+    rows = ref.by_slot(c.cache, c.sh, c.nb)[0]
+    c.q[:] = 0
+    c.q[:, :, 0] = 1
+    keys = rows[0]
+    keys[keys.isfinite()] = 0
+    keys[int(c.table[0, 4]), 7, 0, 0] = -down  # seen by all, not in a last step
+    base, lse, _ = c.attend(scale=0.6931471805599453)
+    rows[1, int(c.table[0, 4]), 7, 0, 9] = float("inf")
+    got, again, status = c.attend(scale=0.6931471805599453)
+    assert status == 0 and torch.equal(lse, again)
+    hit = torch.zeros_like(got, dtype=torch.bool)
+    hit[:m, :, 9] = True
+    assert torch.equal(got[~hit], base[~hit]) and base.isfinite().all()
+    assert not (got[hit].isfinite() | (got[hit] == float("-inf"))).any()
+    if down < 20:
+        assert (got[hit] == float("inf")).all()
+
+
+@pytest.mark.parametrize("G", [16, 33, 64, 96, 130, 200])
+@pytest.mark.parametrize("m", [1, 5, 40])
+def test_many_query_heads_of_one(G, m):
+    """More heads than a tile of rows has, and counts that divide none."""
+    n = [m, 300, 130, 1700]
+    c = Case(n, [m] * 4, 1, G, 64 if G % 2 else 128, dtype=FP, seed=G)
+    c.check(max_new=m)
+    assert check_weigh(c, max_new=m) == 0
